@@ -342,6 +342,127 @@ RCD_API rcd_status rcd_objective_class_static(rcd_ctx *ctx, const void *S_dev, r
                                       int64_t ldS, const int32_t *assignment_dev, int32_t W,
                                       void *part_values_dev, void *total_dev, void *cuda_stream);
 
+/* ---- from hidden states to features (no counterpart in the paper, whose features come from an auto-encoder) ------ */
+
+/* The features of samples that a language model has read are rows of its residual stream, normalised and projected.  The
+ * calls below make them: a root-mean-square norm whose output is what RCD_FEAT_BF16 or RCD_FEAT_I8 asks for, a matrix
+ * product with its epilogue, and both ones' gradients.  Conventions of all of them:
+ *   - rows lie `ld...` ELEMENTS apart (at least the row's length); rows that start on 16 bytes are fastest, any start that
+ *     suits the type is taken;
+ *   - a call with no rows writes nothing but gradients summed over the rows, as zeros;
+ *   - an output overlaps no other argument, but for the one exception stated;
+ *   - everything is only enqueued, captured calls included; no call keeps anything for the next. */
+typedef enum { RCD_ELEM_I8 = 0, RCD_ELEM_BF16 = 1, RCD_ELEM_F16 = 2, RCD_ELEM_F32 = 3 } rcd_elem;
+
+/* Root-mean-square norm of every row, in fp32:
+ *   h = x + residual,  t = h * weight,  rstd = 1 / sqrt(mean(h^2) + eps), 0 where mean(h^2) + eps is 0,  y = t * rstd.
+ * Output (y_type) BF16, F16, F32: y rounded once.  (L2-normalised rows, as RCD_FEAT_BF16 wants them: eps 0 and a weight of
+ * d^-1/2.)  Output I8, scale 0: a scale per row, y = q * scales[row], q = round(t * (127 / a)) with a the row's largest |t|,
+ * scales[row] = rstd * a / 127; a row with an infinity or a NaN gets scale NaN and zeros.  Output I8, scale > 0: that scale for
+ * every row, q = round(t * rstd / scale) within [-127, 127], halves to even, NaN as 0: rows on a common scale, as
+ * RCD_FEAT_I8 wants them; the mean is then taken in fp64, so that q depends on no order of summation.
+ * Squares are summed in fp32 otherwise; a sum beyond its range gives rstd 0. */
+typedef struct {
+    int64_t rows, d;                    /* d from 1 to 16384 */
+    rcd_elem x_type;                    /* BF16, F16 or F32: of x, residual and sum */
+    const void *x_dev;                  /* [rows][d] */
+    int64_t ldx;
+    const void *residual_dev_or_null;   /* [rows][d] */
+    int64_t ld_residual;
+    const void *weight_dev_or_null;     /* [d] */
+    rcd_elem weight_type;               /* BF16, F16 or F32 */
+    float eps;                          /* >= 0 */
+    void *sum_dev_or_null;              /* out [rows][d]: h, rounded; may be x or residual themselves (same rows and ld) */
+    int64_t ld_sum;
+    rcd_elem y_type;
+    void *y_dev;                        /* out [rows][d] */
+    int64_t ldy;
+    float scale;                        /* I8: 0, or the one scale (1 / scale finite) */
+    float *scales_dev_or_null;          /* I8 with scale 0: out [rows]; otherwise null */
+} rcd_norm_args;
+RCD_API rcd_status rcd_rms_norm(rcd_ctx *ctx, const rcd_norm_args *args, void *cuda_stream);
+
+/* Rows to int8 with a scale each, without the norm (rstd 1 above): weights and activations of an int8 product. */
+RCD_API rcd_status rcd_quantize_rows(rcd_ctx *ctx, const void *x_dev, rcd_elem x_type, int64_t rows, int64_t d, int64_t ldx,
+                                     int8_t *q_dev, int64_t ldq, float *scales_dev, void *cuda_stream);
+
+/* Gradients of y = h * rstd * weight (h: what rcd_rms_norm wrote as sum, or its x) from dy:
+ *   g = dy * weight,  dx = rstd * (g - h * rstd^2 * mean(g h)) + dsum  (x's gradient and the residual's alike),
+ *   dweight = sum over the rows of dy * h * rstd, fp32.
+ * dsum is the gradient that reaches h along the residual stream.  Where mean(h^2) + eps is 0, rstd is 0 and so are both. */
+typedef struct {
+    int64_t rows, d;                    /* d from 1 to 16384 */
+    rcd_elem type;                      /* BF16, F16 or F32: of dy, h, dsum and dx */
+    const void *dy_dev;
+    int64_t ld_dy;
+    const void *h_dev;
+    int64_t ld_h;
+    const void *weight_dev_or_null;
+    rcd_elem weight_type;
+    float eps;
+    const void *dsum_dev_or_null;
+    int64_t ld_dsum;
+    void *dx_dev;                       /* out [rows][d] */
+    int64_t ld_dx;
+    float *dweight_dev_or_null;         /* out [d]; the same bits on every run */
+} rcd_norm_back_args;
+RCD_API rcd_status rcd_rms_norm_backward_workspace_bytes(rcd_ctx *ctx, const rcd_norm_back_args *args, size_t *bytes_out);
+RCD_API rcd_status rcd_rms_norm_backward(rcd_ctx *ctx, const rcd_norm_back_args *args, void *workspace_dev, size_t workspace_bytes,
+                                         void *cuda_stream);
+
+/* Activations: GELU is z * Phi(z) (the normal distribution), GELU_TANH its tanh approximation, SILU z / (1 + exp(-z)). */
+typedef enum { RCD_ACT_NONE = 0, RCD_ACT_RELU = 1, RCD_ACT_GELU = 2, RCD_ACT_GELU_TANH = 3, RCD_ACT_SILU = 4 } rcd_activation;
+
+/* y = act(z) + residual,  z = x w^T + bias;  with int8 x and w, z = (x w^T) * x_scales[row] * w_scales[column] + bias.
+ * Products are summed in fp32 (int8: exactly, in int32), the epilogue is fp32, y and preact are rounded once. */
+typedef struct {
+    int64_t rows, n, k;                 /* each at most 2^31 - 1; int8: 16384 k < 2^31 */
+    rcd_elem type;                      /* I8, BF16 or F16: of x and w */
+    const void *x_dev;                  /* [rows][k] */
+    int64_t ldx;
+    const void *w_dev;                  /* [n][k] */
+    int64_t ldw;
+    const float *x_scales_dev_or_null;  /* I8 only: [rows]; null: 1 */
+    const float *w_scales_dev_or_null;  /* I8 only: [n]; null: 1 */
+    const float *bias_dev_or_null;      /* [n] */
+    rcd_activation activation;
+    const void *residual_dev_or_null;   /* [rows][n], y's type */
+    int64_t ld_residual;
+    rcd_elem y_type;                    /* BF16, F16 or F32: of y, residual and preact */
+    void *y_dev;                        /* out [rows][n] */
+    int64_t ldy;
+    void *preact_dev_or_null;           /* out [rows][n]: z, what the backward pass reads */
+    int64_t ld_preact;
+} rcd_linear_args;
+RCD_API rcd_status rcd_linear_workspace_bytes(rcd_ctx *ctx, const rcd_linear_args *args, size_t *bytes_out);
+RCD_API rcd_status rcd_linear(rcd_ctx *ctx, const rcd_linear_args *args, void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
+
+/* Gradients of rcd_linear without scales, from dy:  dz = dy * act'(preact),  dx = dz w,  dw = dz^T x,  dbias = sum over the rows
+ * of dz (of the residual: dy itself).  With an activation dz is rounded to `type` for the products, as a tensor-core
+ * operand has to be; dbias takes it unrounded. */
+typedef struct {
+    int64_t rows, n, k;
+    rcd_elem type;                      /* BF16 or F16: of dy, preact, x, w and dx */
+    const void *dy_dev;                 /* [rows][n] */
+    int64_t ld_dy;
+    const void *x_dev;                  /* [rows][k]; null if dw is */
+    int64_t ldx;
+    const void *w_dev;                  /* [n][k]; null if dx is */
+    int64_t ldw;
+    rcd_activation activation;
+    const void *preact_dev_or_null;     /* [rows][n]; null with RCD_ACT_NONE */
+    int64_t ld_preact;
+    void *dx_dev_or_null;               /* out [rows][k] */
+    int64_t ld_dx;
+    rcd_elem dw_type;                   /* `type`, or F32 */
+    void *dw_dev_or_null;               /* out [n][k] */
+    int64_t ld_dw;
+    float *dbias_dev_or_null;           /* out [n] */
+} rcd_linear_back_args;
+RCD_API rcd_status rcd_linear_backward_workspace_bytes(rcd_ctx *ctx, const rcd_linear_back_args *args, size_t *bytes_out);
+RCD_API rcd_status rcd_linear_backward(rcd_ctx *ctx, const rcd_linear_back_args *args, void *workspace_dev, size_t workspace_bytes,
+                                       void *cuda_stream);
+
 /* ---- yardsticks (measurement only; no counterpart in the paper) ------------------------------ */
 
 /* A read-only sweep with the access pattern of the dense gain sweep (one CTA of 512 threads per SM, 128-bit loads

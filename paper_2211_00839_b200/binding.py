@@ -28,6 +28,11 @@ RCD_OBJ_FACILITY = 0
 RCD_OBJ_GRAPH_CUT = 1
 RCD_FORM_LAUNCHES, RCD_FORM_BARRIERS, RCD_FORM_ASYNC, RCD_FORM_CLASS_PER_CTA, RCD_FORM_CLUSTER, RCD_FORM_ROUNDS, RCD_FORM_CUT_CHAIN, RCD_FORM_SMALL, RCD_FORM_CUT_STEPS = range(1, 10)
 
+RCD_ELEM_I8, RCD_ELEM_BF16, RCD_ELEM_F16, RCD_ELEM_F32 = range(4)
+RCD_ACT_NONE, RCD_ACT_RELU, RCD_ACT_GELU, RCD_ACT_GELU_TANH, RCD_ACT_SILU = range(5)
+# int8 features made by `normalize`: rows of root mean square 1 on a scale that cuts them off at four times that
+RCD_FEATURE_SCALE = 4.0 / 127.0
+
 STATUS_NAMES = {0: "RCD_OK", 1: "RCD_ERR_INVALID_ARG", 2: "RCD_ERR_UNSUPPORTED", 3: "RCD_ERR_WORKSPACE_TOO_SMALL",
                 4: "RCD_ERR_CUDA", 5: "RCD_ERR_TIMEOUT", 6: "RCD_ERR_INTERNAL"}
 
@@ -38,6 +43,8 @@ EXPORTS = ["rcd_create", "rcd_destroy", "rcd_last_error", "rcd_version", "rcd_sy
            "rcd_partition_host_workspace_bytes", "rcd_partition_host", "rcd_objective_workspace_bytes",
            "rcd_objective", "rcd_objective_class_static",
            "rcd_worker_lists_workspace_bytes", "rcd_worker_lists", "rcd_batch_sizes", "rcd_batch_sizes_rule",
+           "rcd_rms_norm", "rcd_quantize_rows", "rcd_rms_norm_backward_workspace_bytes", "rcd_rms_norm_backward",
+           "rcd_linear_workspace_bytes", "rcd_linear", "rcd_linear_backward_workspace_bytes", "rcd_linear_backward",
            "rcd_yardstick_read", "rcd_yardstick_mma"]
 
 
@@ -65,6 +72,33 @@ class RcdProfile(C.Structure):
                 ("lazy_sweeps", C.c_int64), ("lazy_misses", C.c_int64), ("lazy_rows", C.c_int64),
                 ("lazy_rows_skipped", C.c_int64), ("incremental_updates", C.c_int64), ("incremental_rows", C.c_int64), ("threshold_pass_ns", C.c_int64), ("threshold_pass_bytes", C.c_int64), ("noted_picks", C.c_int64),
                 ("greedy_form", C.c_int64), ("round_lists", C.c_int64), ("round_tiles", C.c_int64)]
+
+
+class RcdNormArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int64), ("x_type", C.c_int), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("weight", C.c_void_p), ("weight_type", C.c_int),
+                ("eps", C.c_float), ("sum", C.c_void_p), ("ld_sum", C.c_int64), ("y_type", C.c_int), ("y", C.c_void_p),
+                ("ldy", C.c_int64), ("scale", C.c_float), ("scales", C.c_void_p)]
+
+
+class RcdNormBackArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int64), ("type", C.c_int), ("dy", C.c_void_p), ("ld_dy", C.c_int64),
+                ("h", C.c_void_p), ("ld_h", C.c_int64), ("weight", C.c_void_p), ("weight_type", C.c_int), ("eps", C.c_float),
+                ("dsum", C.c_void_p), ("ld_dsum", C.c_int64), ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dweight", C.c_void_p)]
+
+
+class RcdLinearArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("type", C.c_int), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("w", C.c_void_p), ("ldw", C.c_int64), ("x_scales", C.c_void_p), ("w_scales", C.c_void_p), ("bias", C.c_void_p),
+                ("activation", C.c_int), ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("y_type", C.c_int),
+                ("y", C.c_void_p), ("ldy", C.c_int64), ("preact", C.c_void_p), ("ld_preact", C.c_int64)]
+
+
+class RcdLinearBackArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("type", C.c_int), ("dy", C.c_void_p), ("ld_dy", C.c_int64),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("activation", C.c_int),
+                ("preact", C.c_void_p), ("ld_preact", C.c_int64), ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dw_type", C.c_int),
+                ("dw", C.c_void_p), ("ld_dw", C.c_int64), ("dbias", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -98,6 +132,14 @@ def _load() -> C.CDLL:
     lib.rcd_worker_lists.argtypes = [vp, vp, i64, i32, vp, vp, vp, sz, vp]
     lib.rcd_batch_sizes.argtypes = [i64, vp, i32, vp]
     lib.rcd_batch_sizes_rule.argtypes = [i64, vp, i32, C.c_int, vp]
+    lib.rcd_rms_norm.argtypes = [vp, C.POINTER(RcdNormArgs), vp]
+    lib.rcd_quantize_rows.argtypes = [vp, vp, C.c_int, i64, i64, i64, vp, i64, vp, vp]
+    lib.rcd_rms_norm_backward_workspace_bytes.argtypes = [vp, C.POINTER(RcdNormBackArgs), C.POINTER(sz)]
+    lib.rcd_rms_norm_backward.argtypes = [vp, C.POINTER(RcdNormBackArgs), vp, sz, vp]
+    lib.rcd_linear_workspace_bytes.argtypes = [vp, C.POINTER(RcdLinearArgs), C.POINTER(sz)]
+    lib.rcd_linear.argtypes = [vp, C.POINTER(RcdLinearArgs), vp, sz, vp]
+    lib.rcd_linear_backward_workspace_bytes.argtypes = [vp, C.POINTER(RcdLinearBackArgs), C.POINTER(sz)]
+    lib.rcd_linear_backward.argtypes = [vp, C.POINTER(RcdLinearBackArgs), vp, sz, vp]
     lib.rcd_yardstick_read.argtypes = [vp, vp, sz, i32, vp]
     lib.rcd_yardstick_mma.argtypes = [vp, C.c_int, i32, C.POINTER(C.c_double), vp]
     for name in EXPORTS:
@@ -154,6 +196,19 @@ def _dtype_code(t) -> int:
     if t.dtype == torch.bfloat16:
         return RCD_FEAT_BF16
     raise TypeError("features must be torch.int8 or torch.bfloat16, got %s" % t.dtype)
+
+
+_ELEM = {}
+
+
+def _elem(dtype, name: str) -> int:
+    if not _ELEM:
+        torch = _torch()
+        _ELEM.update({torch.int8: RCD_ELEM_I8, torch.bfloat16: RCD_ELEM_BF16, torch.float16: RCD_ELEM_F16, torch.float32: RCD_ELEM_F32})
+    code = _ELEM.get(dtype)
+    if code is None:
+        raise TypeError("%s must be int8, bfloat16, float16 or float32, got %s" % (name, dtype))
+    return code
 
 
 def features_to_torch(features: np.ndarray, device=None, pin: bool = False):
@@ -380,6 +435,221 @@ class Context:
                                       C.c_void_p(values.data_ptr()), C.c_void_p(total.data_ptr()),
                                       C.c_void_p(ws.data_ptr()), ws.numel(), self._stream()))
         return values, total
+
+
+    # -- from hidden states to features
+    def _rows(self, t, name: str, d: Optional[int] = None, rows: Optional[int] = None, dtype=None):
+        """A tensor [..., d] on this context's device as (tensor to keep alive, rows, d, elements between rows)."""
+        if t.device != self.torch_device:
+            raise ValueError("%s is on %s, the context on %s" % (name, t.device, self.torch_device))
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+        if t.dim() != 2:
+            if t.dim() == 0:
+                raise ValueError("%s has no dimension" % name)
+            t = t.reshape(-1, t.shape[-1]) if t.shape[-1] else t.reshape(0, 0)
+        r, n = t.shape
+        if (d is not None and n != d) or (rows is not None and r != rows):
+            raise ValueError("%s has shape %s, expected %s rows of %s" % (name, tuple(t.shape), r if rows is None else rows, n if d is None else d))
+        s0, s1 = t.stride()
+        if (n > 1 and s1 != 1) or (r > 1 and s0 < n):
+            t = t.contiguous()
+            s0 = n
+        return t, r, n, (s0 if s0 > n else n)
+
+    def _vector(self, t, name: str, n: int, dtype=None):
+        if t.device != self.torch_device:
+            raise ValueError("%s is on %s, the context on %s" % (name, t.device, self.torch_device))
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+        if t.dim() != 1 or t.shape[0] != n:
+            raise ValueError("%s has shape %s, expected (%d,)" % (name, tuple(t.shape), n))
+        return t if t.stride(0) == 1 or n <= 1 else t.contiguous()
+
+    def _out(self, t, name: str, shape, dtype):
+        """A caller's output: it is written in place, so nothing about it is put right."""
+        if t.device != self.torch_device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+            raise ValueError("%s must be %s of shape %s on %s" % (name, dtype, tuple(shape), self.torch_device))
+        if t.dim() == 1:
+            if t.stride(0) != 1 and t.shape[0] > 1:
+                raise ValueError("%s must be dense" % name)
+            return t.shape[0]
+        if t.dim() > 2 and not t.is_contiguous():
+            raise ValueError("%s must be dense" % name)
+        s0, s1 = t.stride()[-2:]
+        if (t.shape[-1] > 1 and s1 != 1) or (t.shape[-2] > 1 and s0 < t.shape[-1]):
+            raise ValueError("%s: the elements of a row must lie next to each other" % name)
+        return max(s0, t.shape[-1])
+
+    def _scratch(self, nbytes: int):
+        """A workspace of this call alone: a captured graph keeps its own, whatever other calls do."""
+        return _torch().empty(nbytes, dtype=_torch().uint8, device=self.torch_device) if nbytes else None
+
+    def rcd_rms_norm(self, x, residual=None, weight=None, eps: float = 1e-6, out_dtype=None, scale: Optional[float] = None,
+                     want_sum: bool = False, out=None, sum_out=None):
+        """y = h * weight / sqrt(mean(h^2) + eps), h = x + residual, for rows [..., d] in bfloat16, float16 or float32.
+
+        ``out_dtype`` (default: x's) may be int8: with a scale per row, or all rows on the one ``scale``.  Returns
+        (y, scales [rows] | None, h rounded to x's type | None).  ``out`` and ``sum_out`` take y and h in place of new tensors;
+        ``sum_out`` may be ``x`` or ``residual`` itself."""
+        torch = _torch()
+        a = RcdNormArgs()
+        kept, rows, d, a.ldx = self._rows(x, "x")
+        a.rows, a.d, a.x_type, a.x = rows, d, _elem(x.dtype, "x"), kept.data_ptr()
+        keep = [kept]
+        if residual is not None:
+            r, _, _, a.ld_residual = self._rows(residual, "residual", d, rows, x.dtype)
+            a.residual = r.data_ptr()
+            keep.append(r)
+        if weight is not None:
+            w = self._vector(weight, "weight", d)
+            a.weight, a.weight_type = w.data_ptr(), _elem(w.dtype, "weight")
+            keep.append(w)
+        a.eps = eps
+        kind = (x.dtype if out_dtype is None else out_dtype) if out is None else out.dtype
+        a.y_type = _elem(kind, "out_dtype")
+        y = torch.empty(x.shape, dtype=kind, device=self.torch_device) if out is None else out
+        a.ldy = d if out is None else self._out(out, "out", x.shape, kind if out_dtype is None else out_dtype)
+        a.y = y.data_ptr()
+        scales = total = None
+        if scale is not None:
+            if not scale > 0.0:
+                raise ValueError("scale must be positive")
+            a.scale = scale
+        elif a.y_type == RCD_ELEM_I8:
+            scales = torch.empty(rows, dtype=torch.float32, device=self.torch_device)
+            a.scales = scales.data_ptr()
+        if want_sum or sum_out is not None:
+            total = torch.empty(x.shape, dtype=x.dtype, device=self.torch_device) if sum_out is None else sum_out
+            a.ld_sum = d if sum_out is None else self._out(sum_out, "sum_out", x.shape, x.dtype)
+            a.sum = total.data_ptr()
+        self._check(lib.rcd_rms_norm(self._h, C.byref(a), self._stream()))
+        return y, scales, total
+
+    def rcd_quantize_rows(self, x):
+        """Rows [..., d] to (int8 of the same shape, scales [rows] float32): x is about q * scale of its row."""
+        torch = _torch()
+        kept, rows, d, ld = self._rows(x, "x")
+        q = torch.empty(x.shape, dtype=torch.int8, device=self.torch_device)
+        scales = torch.empty(rows, dtype=torch.float32, device=self.torch_device)
+        self._check(lib.rcd_quantize_rows(self._h, kept.data_ptr(), _elem(x.dtype, "x"), rows, d, ld, q.data_ptr(), d,
+                                          scales.data_ptr(), self._stream()))
+        return q, scales
+
+    def rcd_rms_norm_backward(self, dy, h, weight=None, eps: float = 1e-6, dsum=None, want_dweight: bool = True):
+        """Gradients of ``rcd_rms_norm``'s y from dy: (dx, which is the residual's gradient too, dweight [d] float32 | None).
+
+        ``h``: the sum that ``rcd_rms_norm`` returned, or its x; ``dsum``: the gradient that reaches h from elsewhere."""
+        torch = _torch()
+        a = RcdNormBackArgs()
+        hk, rows, d, a.ld_h = self._rows(h, "h")
+        yk, _, _, a.ld_dy = self._rows(dy, "dy", d, rows, h.dtype)
+        a.rows, a.d, a.type, a.h, a.dy, a.eps = rows, d, _elem(h.dtype, "h"), hk.data_ptr(), yk.data_ptr(), eps
+        keep = [hk, yk]
+        if weight is not None:
+            w = self._vector(weight, "weight", d)
+            a.weight, a.weight_type = w.data_ptr(), _elem(w.dtype, "weight")
+            keep.append(w)
+        if dsum is not None:
+            s, _, _, a.ld_dsum = self._rows(dsum, "dsum", d, rows, h.dtype)
+            a.dsum = s.data_ptr()
+            keep.append(s)
+        dx = torch.empty(h.shape, dtype=h.dtype, device=self.torch_device)
+        a.dx, a.ld_dx = dx.data_ptr(), d
+        dw = None
+        if weight is not None and want_dweight:
+            dw = torch.empty(d, dtype=torch.float32, device=self.torch_device)
+            a.dweight = dw.data_ptr()
+        need = C.c_size_t()
+        self._check(lib.rcd_rms_norm_backward_workspace_bytes(self._h, C.byref(a), C.byref(need)))
+        ws = self._scratch(need.value)
+        self._check(lib.rcd_rms_norm_backward(self._h, C.byref(a), ws.data_ptr() if ws is not None else None, need.value, self._stream()))
+        return dx, dw
+
+    def rcd_linear(self, x, w, bias=None, residual=None, activation: int = RCD_ACT_NONE, x_scales=None, w_scales=None,
+                   out_dtype=None, want_preact: bool = False, out=None):
+        """act(x w^T + bias) + residual for x [..., k] and w [n, k] in bfloat16, float16 or int8 (x_scales [rows], w_scales [n]).
+
+        bias: float32 [n]; residual: [..., n] in the output's type; ``out_dtype``: default x's type, bfloat16 for int8.
+        Returns (y [..., n], the values before the activation | None)."""
+        torch = _torch()
+        a = RcdLinearArgs()
+        xk, rows, k, a.ldx = self._rows(x, "x")
+        wk, n, _, a.ldw = self._rows(w, "w", k, None, x.dtype)
+        if w.dim() != 2:
+            raise ValueError("w must be [n, k]")
+        a.rows, a.n, a.k, a.type, a.x, a.w, a.activation = rows, n, k, _elem(x.dtype, "x"), xk.data_ptr(), wk.data_ptr(), activation
+        keep = [xk, wk]
+        if out is not None:
+            kind = out.dtype
+        else:
+            kind = out_dtype if out_dtype is not None else torch.bfloat16 if x.dtype == torch.int8 else x.dtype
+        a.y_type = _elem(kind, "out_dtype")
+        shape = (*x.shape[:-1], n)
+        y = torch.empty(shape, dtype=kind, device=self.torch_device) if out is None else out
+        a.ldy = n if out is None else self._out(out, "out", shape, kind if out_dtype is None else out_dtype)
+        a.y = y.data_ptr()
+        if bias is not None:
+            b = self._vector(bias, "bias", n, torch.float32)
+            a.bias = b.data_ptr()
+            keep.append(b)
+        if x_scales is not None:
+            b = self._vector(x_scales, "x_scales", rows, torch.float32)
+            a.x_scales = b.data_ptr()
+            keep.append(b)
+        if w_scales is not None:
+            b = self._vector(w_scales, "w_scales", n, torch.float32)
+            a.w_scales = b.data_ptr()
+            keep.append(b)
+        if residual is not None:
+            r, _, _, a.ld_residual = self._rows(residual, "residual", n, rows, kind)
+            a.residual = r.data_ptr()
+            keep.append(r)
+        pre = None
+        if want_preact:
+            pre = torch.empty(shape, dtype=kind, device=self.torch_device)
+            a.preact, a.ld_preact = pre.data_ptr(), n
+        need = C.c_size_t()
+        self._check(lib.rcd_linear_workspace_bytes(self._h, C.byref(a), C.byref(need)))
+        ws = self._scratch(need.value)
+        self._check(lib.rcd_linear(self._h, C.byref(a), ws.data_ptr() if ws is not None else None, need.value, self._stream()))
+        return y, pre
+
+    def rcd_linear_backward(self, dy, x, w, preact=None, activation: int = RCD_ACT_NONE, dw_dtype=None, want_dx: bool = True,
+                            want_dw: bool = True, want_dbias: bool = True):
+        """Gradients of ``rcd_linear`` (bfloat16 or float16, no scales) from dy [..., n]: (dx [..., k], dw [n, k], dbias [n] float32),
+        None where not wanted.  ``preact``: the values before the activation that ``rcd_linear`` returned; the residual's gradient is dy.
+        ``dw_dtype``: default x's type, or float32."""
+        torch = _torch()
+        a = RcdLinearBackArgs()
+        xk, rows, k, a.ldx = self._rows(x, "x")
+        wk, n, _, a.ldw = self._rows(w, "w", k, None, x.dtype)
+        if w.dim() != 2:
+            raise ValueError("w must be [n, k]")
+        yk, _, _, a.ld_dy = self._rows(dy, "dy", n, rows, x.dtype)
+        a.rows, a.n, a.k, a.type, a.x, a.w, a.dy, a.activation = rows, n, k, _elem(x.dtype, "x"), xk.data_ptr(), wk.data_ptr(), yk.data_ptr(), activation
+        keep = [xk, wk, yk]
+        if preact is not None:
+            z, _, _, a.ld_preact = self._rows(preact, "preact", n, rows, x.dtype)
+            a.preact = z.data_ptr()
+            keep.append(z)
+        dx = dw = db = None
+        if want_dx:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=self.torch_device)
+            a.dx, a.ld_dx = dx.data_ptr(), k
+        kind = x.dtype if dw_dtype is None else dw_dtype
+        a.dw_type = _elem(kind, "dw_dtype")
+        if want_dw:
+            dw = torch.empty((n, k), dtype=kind, device=self.torch_device)
+            a.dw, a.ld_dw = dw.data_ptr(), k
+        if want_dbias:
+            db = torch.empty(n, dtype=torch.float32, device=self.torch_device)
+            a.dbias = db.data_ptr()
+        need = C.c_size_t()
+        self._check(lib.rcd_linear_backward_workspace_bytes(self._h, C.byref(a), C.byref(need)))
+        ws = self._scratch(need.value)
+        self._check(lib.rcd_linear_backward(self._h, C.byref(a), ws.data_ptr() if ws is not None else None, need.value, self._stream()))
+        return dx, dw, db
 
 
 def rcd_worker_lists(ctx: Context, assignment, W: int):

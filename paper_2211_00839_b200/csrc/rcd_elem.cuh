@@ -1,0 +1,90 @@
+// Elements of the operators between hidden states and features: loads that widen to fp32, stores that round once.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "rcd_internal.h"
+
+namespace rcd {
+
+inline int64_t elem_bytes(rcd_elem t) { return t == RCD_ELEM_I8 ? 1 : t == RCD_ELEM_F32 ? 4 : 2; }
+inline bool elem_is_float(rcd_elem t) { return t == RCD_ELEM_BF16 || t == RCD_ELEM_F16 || t == RCD_ELEM_F32; }
+
+// The last byte of `rows` rows and whether two such ranges share one (an output may not overlap an input).
+inline bool ranges_meet(const void *a, int64_t aRows, int64_t aLd, int64_t aLen, int64_t aBytes,
+                        const void *b, int64_t bRows, int64_t bLd, int64_t bLen, int64_t bBytes)
+{
+    if (!a || !b || aRows <= 0 || bRows <= 0 || aLen <= 0 || bLen <= 0) return false;
+    const uintptr_t a0 = (uintptr_t)a, a1 = a0 + (uintptr_t)(((aRows - 1) * aLd + aLen) * aBytes);
+    const uintptr_t b0 = (uintptr_t)b, b1 = b0 + (uintptr_t)(((bRows - 1) * bLd + bLen) * bBytes);
+    return a0 < b1 && b0 < a1;
+}
+// Whether every row of a matrix starts on `align` bytes (null: nothing to load).
+inline bool rows_aligned(const void *p, int64_t ld, int64_t bytes, int64_t align)
+{
+    return !p || (((uintptr_t)p) % align == 0 && ld * bytes % align == 0);
+}
+
+#ifdef __CUDACC__
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+// VEC neighbouring elements, in as few accesses of up to 16 bytes as their size allows.
+template <typename T, int VEC> struct alignas(sizeof(T) * VEC < 16 ? sizeof(T) * VEC : 16) Pack { T v[VEC]; };
+template <int VEC, typename T>
+__device__ __forceinline__ void load_pack(float (&out)[VEC], const T *p)
+{
+    const Pack<T, VEC> x = *reinterpret_cast<const Pack<T, VEC> *>(p);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) out[i] = to_float(x.v[i]);
+}
+template <int VEC, typename T>
+__device__ __forceinline__ void store_pack(T *p, const float (&x)[VEC])
+{
+    Pack<T, VEC> o;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) o.v[i] = from_float<T>(x[i]);
+    *reinterpret_cast<Pack<T, VEC> *>(p) = o;
+}
+template <int VEC>
+__device__ __forceinline__ void load_typed(float (&out)[VEC], const void *p, int64_t i, rcd_elem type)
+{
+    if (type == RCD_ELEM_BF16) load_pack<VEC>(out, (const __nv_bfloat16 *)p + i);
+    else if (type == RCD_ELEM_F16) load_pack<VEC>(out, (const __half *)p + i);
+    else load_pack<VEC>(out, (const float *)p + i);
+}
+template <int VEC>
+__device__ __forceinline__ void store_typed(void *p, int64_t i, rcd_elem type, const float (&x)[VEC])
+{
+    if (type == RCD_ELEM_BF16) store_pack<VEC>((__nv_bfloat16 *)p + i, x);
+    else if (type == RCD_ELEM_F16) store_pack<VEC>((__half *)p + i, x);
+    else store_pack<VEC>((float *)p + i, x);
+}
+// The greater of two, a NaN if either is one.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+__device__ __forceinline__ float warp_sum(float x)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+__device__ __forceinline__ double warp_sum(double x)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+#endif
+
+}  // namespace rcd
