@@ -416,7 +416,7 @@ typedef enum { RCD_ACT_NONE = 0, RCD_ACT_RELU = 1, RCD_ACT_GELU = 2, RCD_ACT_GEL
 /* y = act(z) + residual,  z = x w^T + bias;  with int8 x and w, z = (x w^T) * x_scales[row] * w_scales[column] + bias.
  * Products are summed in fp32 (int8: exactly, in int32), the epilogue is fp32, y and preact are rounded once. */
 typedef struct {
-    int64_t rows, n, k;                 /* each at most 2^31 - 1; int8: 16384 k < 2^31 */
+    int64_t rows, n, k;                 /* each at most 2^30; int8: 16384 k < 2^31 */
     rcd_elem type;                      /* I8, BF16 or F16: of x and w */
     const void *x_dev;                  /* [rows][k] */
     int64_t ldx;

@@ -1,5 +1,5 @@
 // Matrix product with bias, activation and residual in its epilogue (rcd_linear) and its gradients: argument checks, the order of
-// the launches, the pass that takes dy through the activation's derivative, and a plain kernel for the product.
+// the launches, and the pass that takes dy through the activation's derivative.  (The products: rcd_linear_tc.cu.)
 //
 //   z = x w^T [* sx[row] * sw[column]] + b,  y = act(z) + r
 //   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = sum over rows of dz
@@ -9,67 +9,6 @@
 namespace rcd {
 
 namespace {
-
-constexpr int kTile = 64, kSlab = 16;
-
-struct PlainParams {
-    Product p;
-    int64_t aRow, aK, bRow, bK;            // elements between neighbours along m or n, and along k
-    int32_t *status;
-};
-
-// 64 x 64 outputs per CTA, 4 x 4 per thread: any sizes, strides and types.
-template <typename T, typename Acc>
-__global__ void __launch_bounds__(256) product_plain_kernel(const __grid_constant__ PlainParams q)
-{
-    __shared__ Acc As[kSlab][kTile + 1], Bs[kSlab][kTile + 1];
-    const Product &p = q.p;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const T *A = (const T *)p.a.p, *B = (const T *)p.b.p;
-    if (blockIdx.x + blockIdx.y + threadIdx.x == 0) *(volatile int32_t *)q.status = 0;
-    for (int64_t m0 = (int64_t)blockIdx.y * kTile; m0 < p.M; m0 += (int64_t)gridDim.y * kTile) {
-        const int64_t n0 = (int64_t)blockIdx.x * kTile;
-        Acc acc[4][4] = {};
-        for (int64_t k0 = 0; k0 < p.K; k0 += kSlab) {
-            for (int i = threadIdx.x; i < kTile * kSlab; i += 256) {
-                const int r = i / kSlab, k = i % kSlab;
-                auto get = [&](const T *X, int64_t row, int64_t rows, int64_t sRow, int64_t sK) {
-                    if (row >= rows || k0 + k >= p.K) return (Acc)0;
-                    if constexpr (sizeof(T) == 1) return (Acc)X[row * sRow + (k0 + k) * sK];
-                    else return (Acc)to_float(X[row * sRow + (k0 + k) * sK]);
-                };
-                As[k][r] = get(A, m0 + r, p.M, q.aRow, q.aK);
-                Bs[k][r] = get(B, n0 + r, p.N, q.bRow, q.bK);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < kSlab; ++k)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] += As[k][ty * 4 + i] * Bs[k][tx * 4 + j];
-            __syncthreads();
-        }
-        for (int i = 0; i < 4; ++i)
-            for (int j = 0; j < 4; ++j) {
-                const int64_t m = m0 + ty * 4 + i, n = n0 + tx * 4 + j;
-                if (m >= p.M || n >= p.N) continue;
-                const Epilogue &e = p.out;
-                float z[1] = {(float)acc[i][j]};
-                if (e.xs) z[0] *= e.xs[m];
-                if (e.ws) z[0] *= e.ws[n];
-                if (e.bias) z[0] += e.bias[n];
-                if (e.z) store_typed<1>(e.z, m * e.ldz + n, e.type, z);
-                float y[1] = {activate(z[0], e.act)};
-                if (e.residual) {
-                    float r[1];
-                    load_typed<1>(r, e.residual, m * e.ldr + n, e.type);
-                    y[0] += r[0];
-                }
-                store_typed<1>(e.y, m * e.ldy + n, e.type, y);
-            }
-    }
-}
 
 // dz = dy * act'(z), rounded to the products' type, and the sums of its columns over this CTA's rows.
 constexpr int kSlopeRows = 64;
@@ -109,8 +48,9 @@ __global__ void __launch_bounds__(1024) column_sums_kernel(const float *__restri
 
 rcd_status check_sizes(rcd_ctx *ctx, int64_t rows, int64_t n, int64_t k)
 {
-    if (rows < 0 || rows > 0x7fffffffLL || n < 0 || n > 0x7fffffffLL) return fail(ctx, RCD_ERR_INVALID_ARG, "rows=%lld or n=%lld out of range", (long long)rows, (long long)n);
-    if (k <= 0 || k > 0x7fffffffLL) return fail(ctx, RCD_ERR_INVALID_ARG, "k=%lld must be from 1 to 2^31 - 1", (long long)k);
+    constexpr int64_t most = 1LL << 30;
+    if (rows < 0 || rows > most || n < 0 || n > most) return fail(ctx, RCD_ERR_INVALID_ARG, "rows=%lld or n=%lld out of range", (long long)rows, (long long)n);
+    if (k <= 0 || k > most) return fail(ctx, RCD_ERR_INVALID_ARG, "k=%lld must be from 1 to 2^30", (long long)k);
     return RCD_OK;
 }
 rcd_status check_act(rcd_ctx *ctx, rcd_activation act)
@@ -244,26 +184,6 @@ rcd_status check_rows(rcd_ctx *ctx, const char *name, const void *p, int64_t row
 rcd_status launch_column_sums(rcd_ctx *ctx, const float *partial, int64_t rows, int64_t d, float *out, cudaStream_t st)
 {
     column_sums_kernel<<<(unsigned)((d + 31) / 32), 1024, 0, st>>>(partial, (int32_t)rows, d, out);
-    ctx->kernelLaunches++;
-    RCD_CUDA(ctx, cudaGetLastError());
-    return RCD_OK;
-}
-
-size_t product_workspace(const rcd_ctx *, const Product &) { return 0; }
-
-rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *, cudaStream_t st)
-{
-    PlainParams q{};
-    q.p = p;
-    q.aRow = p.a.across ? 1 : p.a.ld;
-    q.aK = p.a.across ? p.a.ld : 1;
-    q.bRow = p.b.across ? 1 : p.b.ld;
-    q.bK = p.b.across ? p.b.ld : 1;
-    q.status = ctx->statusOwn;
-    const dim3 grid((unsigned)((p.N + kTile - 1) / kTile), (unsigned)std::min<int64_t>((p.M + kTile - 1) / kTile, 65535));
-    if (p.type == RCD_ELEM_I8) product_plain_kernel<int8_t, int32_t><<<grid, 256, 0, st>>>(q);
-    else if (p.type == RCD_ELEM_BF16) product_plain_kernel<__nv_bfloat16, float><<<grid, 256, 0, st>>>(q);
-    else product_plain_kernel<__half, float><<<grid, 256, 0, st>>>(q);
     ctx->kernelLaunches++;
     RCD_CUDA(ctx, cudaGetLastError());
     return RCD_OK;
