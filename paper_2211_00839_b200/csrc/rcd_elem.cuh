@@ -66,6 +66,77 @@ __device__ __forceinline__ void store_typed(void *p, int64_t i, rcd_elem type, c
     else if (type == RCD_ELEM_F16) store_pack<VEC>((__half *)p + i, x);
     else store_pack<VEC>((float *)p + i, x);
 }
+// Two fp32 numbers in 64 bits: sm_100 adds, multiplies and fuses them in one instruction, each rounded as alone.
+struct Two { unsigned long long v; };
+__device__ __forceinline__ Two two(float lo, float hi)
+{
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 parts(Two x)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
+    return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) { Two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ Two add2(Two a, Two b) { Two r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+__device__ __forceinline__ Two widen(uint32_t x, __nv_bfloat16) { return two(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+__device__ __forceinline__ Two widen(uint32_t x, __half)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&x));
+    return two(f.x, f.y);
+}
+__device__ __forceinline__ uint32_t narrow(Two x, __nv_bfloat16)
+{
+    const float2 f = parts(x);
+    const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t *>(&b);
+}
+__device__ __forceinline__ uint32_t narrow(Two x, __half)
+{
+    const float2 f = parts(x);
+    const __half2 b = __floats2half2_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t *>(&b);
+}
+// 2 P neighbouring elements as pairs; 16-byte accesses where there are as many bytes.
+template <int P, typename T>
+__device__ __forceinline__ void load_twos(Two (&o)[P], const T *p)
+{
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (P % 2 == 0) {
+#pragma unroll
+            for (int i = 0; i < P / 2; ++i) {
+                const float4 x = reinterpret_cast<const float4 *>(p)[i];
+                o[2 * i] = two(x.x, x.y);
+                o[2 * i + 1] = two(x.z, x.w);
+            }
+        }
+    } else {
+        Pack<uint32_t, P> x = *reinterpret_cast<const Pack<uint32_t, P> *>(p);
+#pragma unroll
+        for (int i = 0; i < P; ++i) o[i] = widen(x.v[i], T());
+    }
+}
+template <int P, typename T>
+__device__ __forceinline__ void store_twos(T *p, const Two (&x)[P])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < P / 2; ++i) {
+            const float2 a = parts(x[2 * i]), b = parts(x[2 * i + 1]);
+            reinterpret_cast<float4 *>(p)[i] = make_float4(a.x, a.y, b.x, b.y);
+        }
+    } else {
+        Pack<uint32_t, P> o;
+#pragma unroll
+        for (int i = 0; i < P; ++i) o.v[i] = narrow(x[i], T());
+        *reinterpret_cast<Pack<uint32_t, P> *>(p) = o;
+    }
+}
+
 // The greater of two, a NaN if either is one.
 __device__ __forceinline__ float max_nan(float a, float b)
 {

@@ -269,7 +269,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             }
             // after an abort: let the copies already issued land (a pair's report to CTA 0, so by time: some 2 ms)
             if (*(volatile int32_t *)&sh.abort)
-                for (uint32_t spin = 0; spin < (1u << 15); ++spin) __nanosleep(64);
+                let_copies_land();
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer (a pair's first CTA, for both) ----------------
@@ -430,7 +430,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         }
         if (lane == 0) bulk_wait();
         if (!ok || *(volatile int32_t *)&sh.abort)                    // a residual may be on its way
-            for (uint32_t spin = 0; spin < (1u << 15); ++spin) __nanosleep(64);
+            let_copies_land();
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();

@@ -6,7 +6,7 @@
 // Both are bound by memory: every input is read once and every output written once.  A row belongs to a group of 32 to 512
 // threads that keep it in registers (up to 32 elements each) from its load to its store; what the group has to agree on (a sum and a
 // maximum; two sums) is one reduction by shuffles, and above a warp one exchange in shared memory.
-#include "rcd_linear.h"
+#include "rcd_norm.cuh"
 
 namespace rcd {
 
@@ -15,18 +15,71 @@ namespace {
 constexpr int kRowThreads = 512;           // at most: 128 registers each
 constexpr int kMostWidth = 16384;          // that many threads with 32 elements each
 
-struct NormParams {
-    int64_t rows;
-    int32_t d, group;                      // threads per row
-    const void *x, *r, *w;
-    int64_t ldx, ldr, lds, ldy;
-    rcd_elem wType, yType;
-    float eps, invScale;                   // invScale > 0: 8 bits on one scale
-    bool normalize;
-    void *sum, *y;
-    float *scales;
-    int32_t *status;
-};
+// A thread's part of a row's sum of squares and of its largest |t|; h becomes t = h w.
+// One scale: the sum in 64 bits, whose rounding to rstd's 32 no order of summation changes (a value next to a border
+// between two integers falls on the same side every time).
+template <int VEC, int NV>
+__device__ __forceinline__ void row_sums(const NormParams &p, float (&h)[NV][VEC], int tid, int G, double &sum, float &a)
+{
+    if (p.normalize) {
+        if (p.invScale > 0.0f) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum += (double)h[c][i] * (double)h[c][i];
+        } else {
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) s[i & 3] = fmaf(h[c][i], h[c][i], s[i & 3]);
+            sum = (double)((s[0] + s[1]) + (s[2] + s[3]));
+        }
+    }
+    if (p.w) {
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int col = (c * G + tid) * VEC;
+            if (col < p.d) {
+                float w[VEC];
+                load_typed<VEC>(w, p.w, col, p.wType);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) h[c][i] *= w[i];
+            }
+        }
+    }
+    if (p.yType == RCD_ELEM_I8 && p.invScale == 0.0f) {
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) a = max_nan(a, fabsf(h[c][i]));
+    }
+}
+// t, the row's sum of squares and its largest |t| -> the row's output.
+template <typename T, int VEC, int NV>
+__device__ __forceinline__ void finish_row(const NormParams &p, float (&h)[NV][VEC], int64_t row, int tid, int G, double sum, float a)
+{
+    const bool rowScale = p.yType == RCD_ELEM_I8 && p.invScale == 0.0f;
+    float rstd;
+    if (p.invScale > 0.0f) rstd = rstd_of(sum, p);
+    else rstd = rstd_of((float)sum, p);
+    const float inv = rowScale ? row_scale(a, rstd, tid == 0 ? p.scales + row : nullptr) : p.invScale;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int col = (c * G + tid) * VEC;
+        if (col >= p.d) continue;
+        if (p.yType == RCD_ELEM_I8) {
+            Pack<int8_t, VEC> q;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) q.v[i] = to_int8<true>(rowScale ? h[c][i] * inv : (h[c][i] * rstd) * inv);
+            *reinterpret_cast<Pack<int8_t, VEC> *>((int8_t *)p.y + row * p.ldy + col) = q;
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) h[c][i] *= rstd;
+            store_typed<VEC>(p.y, row * p.ldy + col, p.yType, h[c]);
+        }
+    }
+}
 
 template <typename T, int VEC, int NV>
 __global__ void __launch_bounds__(kRowThreads) rms_norm_kernel(const __grid_constant__ NormParams p)
@@ -37,8 +90,6 @@ __global__ void __launch_bounds__(kRowThreads) rms_norm_kernel(const __grid_cons
     const int64_t row = (int64_t)blockIdx.x * (blockDim.x / G) + threadIdx.x / G;
     if (blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)p.status = 0;
     const bool mine = row < p.rows;
-    const bool rowScale = p.yType == RCD_ELEM_I8 && p.invScale == 0.0f;
-
     float h[NV][VEC];
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
@@ -56,46 +107,11 @@ __global__ void __launch_bounds__(kRowThreads) rms_norm_kernel(const __grid_cons
             if (p.sum) store_pack<VEC>((T *)p.sum + row * p.lds + col, h[c]);
         }
     }
-    // One scale: the mean in 64 bits, whose rounding to rstd's 32 no order of summation changes (a value next to a border
-    // between two integers falls on the same side every time).
-    float rstd = 1.0f, a = 0.0f;
     double sum64 = 0.0;
-    if (p.normalize) {
-        if (p.invScale > 0.0f) {
-#pragma unroll
-            for (int c = 0; c < NV; ++c)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) sum64 += (double)h[c][i] * (double)h[c][i];
-        } else {
-            float s = 0.0f;
-#pragma unroll
-            for (int c = 0; c < NV; ++c)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) s = fmaf(h[c][i], h[c][i], s);
-            sum64 = (double)s;
-        }
-    }
-    if (p.w) {
-#pragma unroll
-        for (int c = 0; c < NV; ++c) {
-            const int col = (c * G + tid) * VEC;
-            if (col < p.d) {
-                float w[VEC];
-                load_typed<VEC>(w, p.w, col, p.wType);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) h[c][i] *= w[i];
-            }
-        }
-    }
-    if (rowScale) {
-#pragma unroll
-        for (int c = 0; c < NV; ++c)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) a = max_nan(a, fabsf(h[c][i]));
-    }
+    float a = 0.0f;
+    row_sums<VEC, NV>(p, h, tid, G, sum64, a);
     sum64 = warp_sum(sum64);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
+    a = warp_max_nan(a);
     if (G > 32) {
         if (lane == 0) { shSum[warp] = sum64; shMax[warp] = a; }
         __syncthreads();
@@ -104,53 +120,8 @@ __global__ void __launch_bounds__(kRowThreads) rms_norm_kernel(const __grid_cons
         a = 0.0f;
         for (int k = 0; k < G / 32; ++k) { sum64 += shSum[first + k]; a = max_nan(a, shMax[first + k]); }
     }
-    if (!mine) return;
-    if (p.normalize) {
-        if (p.invScale > 0.0f) {
-            const double v = sum64 / (double)p.d + (double)p.eps;
-            rstd = v > 0.0 ? (float)(1.0 / sqrt(v)) : v == 0.0 ? 0.0f : (float)v;
-        } else {
-            const float v = (float)sum64 / (float)p.d + p.eps;
-            rstd = v > 0.0f ? 1.0f / sqrtf(v) : v == 0.0f ? 0.0f : v;
-        }
-    }
-    float inv = 0.0f;
-    if (rowScale) {
-        const bool fine = a < INFINITY;                        // (not so for a NaN)
-        if (fine && a > 0.0f) inv = fminf(127.0f / a, 3.402823466e38f);
-        if (tid == 0) p.scales[row] = fine ? rstd * a / 127.0f : NAN;
-    }
-#pragma unroll
-    for (int c = 0; c < NV; ++c) {
-        const int col = (c * G + tid) * VEC;
-        if (col >= p.d) continue;
-        if (p.yType == RCD_ELEM_I8) {
-            Pack<int8_t, VEC> q;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float v = rowScale ? h[c][i] * inv : (h[c][i] * rstd) * p.invScale;
-                q.v[i] = (int8_t)max(-127, min(127, __float2int_rn(v)));          // (NaN: 0)
-            }
-            *reinterpret_cast<Pack<int8_t, VEC> *>((int8_t *)p.y + row * p.ldy + col) = q;
-        } else {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) h[c][i] *= rstd;
-            store_typed<VEC>(p.y, row * p.ldy + col, p.yType, h[c]);
-        }
-    }
+    if (mine) finish_row<T, VEC, NV>(p, h, row, tid, G, sum64, a);
 }
-
-struct NormBackParams {
-    int64_t rows;
-    int32_t d, group;
-    const void *dy, *h, *w, *dsum;
-    int64_t ldDy, ldH, ldDsum, ldDx;
-    rcd_elem wType;
-    float eps;
-    void *dx;
-    float *partial;                        // [groups of the launch][d], or null
-    int32_t *status;
-};
 
 template <typename T, int VEC, int NV>
 __global__ void __launch_bounds__(kRowThreads) rms_norm_back_kernel(const __grid_constant__ NormBackParams p)
@@ -234,13 +205,6 @@ __global__ void __launch_bounds__(kRowThreads) rms_norm_back_kernel(const __grid
                 if (col + i < p.d) to[col + i] = dw[c][i];
         }
     }
-}
-
-int pow2_at_least(int64_t x)
-{
-    int g = 32;
-    while (g < x) g *= 2;
-    return g;
 }
 
 // Threads per row and accesses per thread (a power of two of them): few rows get as many threads as the row has pieces, since then only
@@ -351,7 +315,11 @@ rcd_status norm_rows(rcd_ctx *ctx, const rcd_norm_args &a, bool normalize, cudaS
     const bool vectors = a.d % vec == 0 && rows_aligned(p.x, p.ldx, xb, 16) && rows_aligned(p.r, p.ldr, xb, 16) && rows_aligned(p.sum, p.lds, xb, 16) &&
                          rows_aligned(p.y, p.ldy, yb, std::min<int64_t>(16, vec * yb)) &&
                          rows_aligned(p.w, 0, 1, p.w ? std::min<int64_t>(16, vec * elem_bytes(a.weight_type)) : 1);
-    if (a.x_type == RCD_ELEM_BF16) launch_norm_type<__nv_bfloat16>(p, vectors, ctx->smCount, st);
+    const Ring ring = vectors ? ring_shape(a.d, xb, a.residual_dev_or_null ? 2 : 1, false) : Ring{};
+    if (vectors && ring_pays(ctx, a.rows, ring)) {
+        RCD_TRY(launch_norm_ring(ctx, p, a.x_type, ring, st));
+    }
+    else if (a.x_type == RCD_ELEM_BF16) launch_norm_type<__nv_bfloat16>(p, vectors, ctx->smCount, st);
     else if (a.x_type == RCD_ELEM_F16) launch_norm_type<__half>(p, vectors, ctx->smCount, st);
     else launch_norm_type<float>(p, vectors, ctx->smCount, st);
     ctx->kernelLaunches++;
@@ -360,14 +328,23 @@ rcd_status norm_rows(rcd_ctx *ctx, const rcd_norm_args &a, bool normalize, cudaS
 }
 
 // The backward pass runs as many CTAs as fit the SMs at once, each with its share of the rows.
-struct BackShape { RowShape s; int threads, ctas; bool vectors; int64_t partialRows; };
+struct BackShape { RowShape s; int threads, ctas; bool vectors, useRing; Ring ring; int64_t partialRows; };
 BackShape back_shape(const rcd_ctx *ctx, const rcd_norm_back_args &a)
 {
-    BackShape b;
+    BackShape b{};
     const int64_t eb = elem_bytes(a.type), vec = 16 / eb;
     b.vectors = a.d % vec == 0 && rows_aligned(a.dy_dev, a.ld_dy, eb, 16) && rows_aligned(a.h_dev, a.ld_h, eb, 16) && rows_aligned(a.dsum_dev_or_null, a.ld_dsum, eb, 16) &&
                 rows_aligned(a.dx_dev, a.ld_dx, eb, 16) &&
                 rows_aligned(a.weight_dev_or_null, 0, 1, a.weight_dev_or_null ? std::min<int64_t>(16, vec * elem_bytes(a.weight_type)) : 1);
+    if (b.vectors) {
+        b.ring = ring_shape(a.d, eb, a.dsum_dev_or_null ? 3 : 2, true);
+        // (weights of the rows' type or fp32)
+        b.useRing = ring_pays(ctx, a.rows, b.ring) && (!a.weight_dev_or_null || a.weight_type == a.type || a.weight_type == RCD_ELEM_F32);
+        if (b.useRing) {
+            b.partialRows = ring_ctas(ctx, a.rows, b.ring);
+            return b;
+        }
+    }
     b.s = b.vectors ? row_shape(a.rows, a.d, (int)vec, (int)(32 / vec), 1, ctx->smCount) : row_shape(a.rows, a.d, 1, 32, 8, ctx->smCount);
     b.threads = std::max(256, b.s.group);
     const int perCta = b.threads / b.s.group;
@@ -480,7 +457,10 @@ extern "C" rcd_status rcd_rms_norm_backward(rcd_ctx *ctx, const rcd_norm_back_ar
     p.dx = a.dx_dev;
     p.partial = a.dweight_dev_or_null ? (float *)workspace_dev : nullptr;
     p.status = ctx->statusOwn;
-    if (a.type == RCD_ELEM_BF16) launch_back_type<__nv_bfloat16>(p, b, st);
+    if (b.useRing) {
+        RCD_TRY(launch_norm_back_ring(ctx, p, a.type, b.ring, st));
+    }
+    else if (a.type == RCD_ELEM_BF16) launch_back_type<__nv_bfloat16>(p, b, st);
     else if (a.type == RCD_ELEM_F16) launch_back_type<__half>(p, b, st);
     else launch_back_type<float>(p, b, st);
     ctx->kernelLaunches++;

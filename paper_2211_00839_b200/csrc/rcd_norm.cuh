@@ -1,0 +1,178 @@
+// What the translation units of rcd_rms_norm and its gradients share.
+#pragma once
+
+#include <type_traits>
+
+#include "rcd_linear.h"
+#include "rcd_tc.cuh"
+
+namespace rcd {
+
+struct NormParams {
+    int64_t rows;
+    int32_t d, group;                      // threads per row
+    const void *x, *r, *w;
+    int64_t ldx, ldr, lds, ldy;
+    rcd_elem wType, yType;
+    float eps, invScale;                   // invScale > 0: 8 bits on one scale
+    bool normalize;
+    void *sum, *y;
+    float *scales;
+    int32_t *status;
+};
+
+struct NormBackParams {
+    int64_t rows;
+    int32_t d, group;
+    const void *dy, *h, *w, *dsum;
+    int64_t ldDy, ldH, ldDsum, ldDx;
+    rcd_elem wType;
+    float eps;
+    void *dx;
+    float *partial;                        // [groups of the launch][d], or null
+    int32_t *status;
+};
+
+inline int pow2_at_least(int64_t x)
+{
+    int g = 32;
+    while (g < x) g *= 2;
+    return g;
+}
+
+#ifdef __CUDACC__
+__device__ __forceinline__ float warp_max_nan(float a)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
+    return a;
+}
+__device__ __forceinline__ float rstd_of(float sum, const NormParams &p)
+{
+    if (!p.normalize) return 1.0f;
+    const float v = sum / (float)p.d + p.eps;
+    return v > 0.0f ? 1.0f / sqrtf(v) : v == 0.0f ? 0.0f : v;
+}
+__device__ __forceinline__ float rstd_of(double sum, const NormParams &p)
+{
+    if (!p.normalize) return 1.0f;
+    const double v = sum / (double)p.d + (double)p.eps;
+    return v > 0.0 ? (float)(1.0 / sqrt(v)) : v == 0.0 ? 0.0f : (float)v;
+}
+// 127 / a, and the row's scale.
+__device__ __forceinline__ float row_scale(float a, float rstd, float *scale)
+{
+    const bool fine = a < INFINITY;                            // (not so for a NaN)
+    if (scale) *scale = fine ? rstd * a / 127.0f : NAN;
+    return fine && a > 0.0f ? fminf(127.0f / a, 3.402823466e38f) : 0.0f;
+}
+// To the nearest integer, halves to even; a NaN is 0.  (With a scale per row nothing is above 127.)
+template <bool kCut>
+__device__ __forceinline__ int8_t to_int8(float x)
+{
+    const int q = __float2int_rn(x);
+    return (int8_t)(kCut ? max(-127, min(127, q)) : q);
+}
+// ---- many rows: every group of warps draws its rows through a ring of its own in shared memory ----
+//
+// With a row per CTA the loads stop while the row is reduced and stored, and CTAs come and go: 3.7 TB/s.  Here one CTA per SM stays;
+// the first lane of a group (1 to 16 warps, up to 32 elements per lane) orders whole rows by bulk copies (cp.async.bulk, an mbarrier per
+// slot) one to four rows ahead, so that some 150 KB per SM are always on their way.  A slot is ordered again as soon as its row lies in
+// registers (forward) or has been gone through twice (backward).
+constexpr int kRingWarps = 16;
+constexpr int kRingStages = 4;
+constexpr int kRingBytes = 200 * 1024;
+constexpr uint32_t kSpinLimit = 1u << 22;               // polls of ~64 ns: a quarter of a second
+
+struct Ring { int warpsPerRow, groups, stages, slotBytes; };
+
+struct RingShared {
+    uint64_t bar[kRingWarps][kRingStages];
+    float4 part[2][kRingWarps];
+    int32_t abort;
+};
+
+// Bounded.  When it runs out the CTA goes on with what is there and says so in the status word: its groups stay in step.
+__device__ __forceinline__ void ring_wait(uint64_t *bar, uint32_t parity, RingShared *sh)
+{
+    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+        if (mbar_test(bar, parity)) return;
+        if (spin > 64) {
+            if (*(volatile int32_t *)&sh->abort) return;
+            __nanosleep(64);
+        }
+    }
+    atomicExch(&sh->abort, 1);
+}
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 :: "r"(smem_addr(dst)), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void group_barrier(int group, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "r"(threads) : "memory"); }
+
+__device__ __forceinline__ void ring_begin(RingShared *sh, const Ring &ring, int32_t *status)
+{
+    if (blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)status = 0;        // (no wait runs out for a quarter of a second)
+    if (threadIdx.x == 0) {
+        for (int g = 0; g < ring.groups; ++g)
+            for (int k = 0; k < ring.stages; ++k) mbar_init(&sh->bar[g][k], 1);
+        sh->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+}
+// After an expired wait: what was ordered lands before the CTA leaves.
+__device__ __forceinline__ void ring_end(RingShared *sh, int32_t *status)
+{
+    __syncthreads();
+    if (*(volatile int32_t *)&sh->abort) {
+        let_copies_land();
+        if (threadIdx.x == 0) atomicOr(status, kDevTimeout);
+    }
+}
+
+#endif
+
+// The ring's shape for rows of `streams` inputs of d elements: up to 32 elements per lane, as many warps as leave every group two slots.
+inline Ring ring_shape(int64_t d, int64_t eb, int streams, bool sums)
+{
+    Ring g;
+    const int64_t vec = 16 / eb, mostPerLane = 32 / vec;
+    g.warpsPerRow = pow2_at_least((d / vec + mostPerLane - 1) / mostPerLane) / 32;
+    g.slotBytes = (int)(((int64_t)streams * d * eb + 127) / 128 * 128);
+    int warps = kRingWarps;
+    auto slots = [&]() { return kRingBytes / g.slotBytes / (warps / g.warpsPerRow); };
+    while (warps > 4 && warps / 2 >= g.warpsPerRow && slots() < 2) warps -= warps > 8 && (warps - 4) % g.warpsPerRow == 0 ? 4 : warps / 2;
+    // (the groups' sums of columns take the ring's place at the end)
+    while (sums && warps / 2 >= g.warpsPerRow && warps / g.warpsPerRow * d * 4 > kRingBytes) warps /= 2;
+    g.groups = warps / g.warpsPerRow;
+    g.stages = std::max(1, std::min(kRingStages, slots()));
+    return g;
+}
+// The ring pays from some rows per group on (16384 x 4096 ...)
+inline bool ring_pays(const rcd_ctx *ctx, int64_t rows, const Ring &g) { return rows >= 2LL * ctx->smCount * g.groups; }
+
+template <typename Kernel, typename Params>
+rcd_status launch_ring(rcd_ctx *ctx, Kernel *kernel, const Params &p, const Ring &g, int ctas, size_t bytes, cudaStream_t st)
+{
+    RCD_CUDA(ctx, allow_shared(kernel, 220 * 1024));
+    kernel<<<ctas, 32 * g.groups * g.warpsPerRow, bytes, st>>>(p, g);
+    return RCD_OK;
+}
+inline int ring_ctas(const rcd_ctx *ctx, int64_t rows, const Ring &g) { return (int)std::min<int64_t>(ctx->smCount, (rows + g.groups - 1) / g.groups); }
+
+// Accesses per lane and row, as the kernels are built for: 2 or 4 of 16-bit elements, 4 or 8 of fp32.
+template <int VEC, typename Go>
+rcd_status by_accesses(int64_t d, const Ring &g, Go go)
+{
+    constexpr int kFew = 16 / VEC, kMany = 32 / VEC;
+    const int64_t per = (d / VEC + 32 * g.warpsPerRow - 1) / (32 * g.warpsPerRow);
+    return per <= kFew ? go(std::integral_constant<int, kFew>()) : go(std::integral_constant<int, kMany>());
+}
+
+// The launches for many rows (rcd_norm_ring.cu, rcd_norm_ring_back.cu).
+rcd_status launch_norm_ring(rcd_ctx *ctx, const NormParams &p, rcd_elem type, const Ring &g, cudaStream_t st);
+rcd_status launch_norm_back_ring(rcd_ctx *ctx, const NormBackParams &p, rcd_elem type, const Ring &g, cudaStream_t st);
+
+}  // namespace rcd

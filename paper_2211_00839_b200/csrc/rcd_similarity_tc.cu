@@ -613,7 +613,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1) sim_p
             }
             // after an abort: let the copies already issued land (they report to CTA 0, so by time: some 2 ms)
             if (*(volatile int32_t *)&sh.abort)
-                for (uint32_t spin = 0; spin < (1u << 15); ++spin) __nanosleep(64);
+                let_copies_land();
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer: CTA 0, for both ----------------

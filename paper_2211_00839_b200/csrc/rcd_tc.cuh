@@ -48,6 +48,13 @@ __device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, i
                  :: "r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(smem_addr(bar)) : "memory");
 }
 
+// Some 2 ms, for copies in flight when a CTA gives up.  (Not unrolled: as 32768 instructions it took the compiler ten seconds.)
+__device__ __forceinline__ void let_copies_land()
+{
+#pragma unroll 1
+    for (uint32_t spin = 0; spin < (1u << 15); ++spin) __nanosleep(64);
+}
+
 // Shared-memory matrix descriptor: K-major operand, 128-byte swizzle, rows 128 bytes apart,
 // groups of 8 rows 1024 bytes apart.
 __device__ __forceinline__ uint64_t make_smem_desc(uint32_t addr)
