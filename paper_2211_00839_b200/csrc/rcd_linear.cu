@@ -10,24 +10,50 @@ namespace rcd {
 
 namespace {
 
-// dz = dy * act'(z), rounded to the products' type, and the sums of its columns over this CTA's rows.
+// dz = dy * act'(z), rounded to the products' type, and the sums of its columns over this CTA's rows.  Bound by memory: 16-byte accesses
+// where rows allow it, 32 threads along a row, 8 rows at a time; a thread's sums meet those of the other seven in shared memory.
 constexpr int kSlopeRows = 64;
-template <typename T>
+template <typename T, int VEC>
 __global__ void __launch_bounds__(256) slope_kernel(const T *__restrict__ dy, int64_t ldDy, const T *__restrict__ z, int64_t ldZ, int64_t rows, int64_t n, int act,
                                                     T *__restrict__ dz, int64_t ldDz, float *__restrict__ partial)
 {
-    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (col >= n) return;
+    __shared__ float sh[8][32 * VEC + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t col0 = (int64_t)blockIdx.x * 32 * VEC, col = col0 + lane * VEC;
     const int64_t chunks = (rows + kSlopeRows - 1) / kSlopeRows;
     for (int64_t chunk = blockIdx.y; chunk < chunks; chunk += gridDim.y) {
-        float s = 0.0f;
-        for (int64_t r = chunk * kSlopeRows; r < min(rows, (chunk + 1) * kSlopeRows); ++r) {
-            float d = to_float(dy[r * ldDy + col]);
-            if (z) d *= activation_slope(to_float(z[r * ldZ + col]), act);
-            if (dz) dz[r * ldDz + col] = from_float<T>(d);
-            s += d;
+        float s[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s[i] = 0.0f;
+        if (col < n) {
+#pragma unroll 4
+            for (int k = 0; k < kSlopeRows / 8; ++k) {
+                const int64_t r = chunk * kSlopeRows + k * 8 + warp;
+                if (r >= rows) break;
+                float d[VEC];
+                load_pack<VEC>(d, dy + r * ldDy + col);
+                if (z) {
+                    float x[VEC];
+                    load_pack<VEC>(x, z + r * ldZ + col);
+                    slopes<VEC>(d, x, act);
+                }
+                if (dz) store_pack<VEC>(dz + r * ldDz + col, d);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) s[i] += d[i];
+            }
         }
-        if (partial) partial[chunk * n + col] = s;
+        if (partial) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sh[warp][lane * VEC + i] = s[i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < 32 * VEC && col0 + c < n; c += 256) {
+                float o = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o += sh[k][c];
+                partial[chunk * n + col0 + c] = o;
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -258,10 +284,12 @@ extern "C" rcd_status rcd_linear_backward(rcd_ctx *ctx, const rcd_linear_back_ar
     const BackPlan b = back_plan(ctx, a, ws);
     if (b.slope || b.sums) {
         float *partial = b.sums ? (float *)(ws + b.partial) : nullptr;
-        const dim3 grid((unsigned)((a.n + 255) / 256), (unsigned)std::min<int64_t>(b.chunks, 65535));
+        const int64_t per = rows_aligned(a.dy_dev, a.ld_dy, eb, 16) && rows_aligned(a.preact_dev_or_null, a.ld_preact, eb, 16) && a.n % 8 == 0 ? 256 : 32;
+        const dim3 grid((unsigned)((a.n + per - 1) / per), (unsigned)std::min<int64_t>(b.chunks, 65535));
         auto run = [&](auto t) {
             using T = decltype(t);
-            slope_kernel<T><<<grid, 256, 0, st>>>((const T *)a.dy_dev, a.ld_dy, (const T *)a.preact_dev_or_null, a.ld_preact, a.rows, a.n, (int)a.activation,
+            auto *kernel = per == 256 ? slope_kernel<T, 8> : slope_kernel<T, 1>;
+            kernel<<<grid, 256, 0, st>>>((const T *)a.dy_dev, a.ld_dy, (const T *)a.preact_dev_or_null, a.ld_preact, a.rows, a.n, (int)a.activation,
                                                   b.slope ? (T *)(ws + b.dz) : nullptr, b.ldDz, partial);
         };
         if (a.type == RCD_ELEM_BF16) run(__nv_bfloat16());

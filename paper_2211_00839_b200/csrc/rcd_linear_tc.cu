@@ -164,23 +164,6 @@ __device__ __forceinline__ void add_row(const unsigned char *piece, int row, int
         }
     }
 }
-template <int kAct>
-__device__ __forceinline__ void activate_all(float (&v)[32])
-{
-#pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = activate(v[j], kAct);
-}
-__device__ __forceinline__ void activate_by(float (&v)[32], int act)
-{
-    switch (act) {
-    case RCD_ACT_RELU: activate_all<RCD_ACT_RELU>(v); break;
-    case RCD_ACT_GELU: activate_all<RCD_ACT_GELU>(v); break;
-    case RCD_ACT_GELU_TANH: activate_all<RCD_ACT_GELU_TANH>(v); break;
-    case RCD_ACT_SILU: activate_all<RCD_ACT_SILU>(v); break;
-    default: break;
-    }
-}
-
 // Unit of work -> row tile, first column, piece of the k axis.  Column tiles are neighbours: the CTAs at work share a few row tiles of A
 // and all of B.
 struct Unit { int m, n, split; };
@@ -394,7 +377,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                             for (int j = 0; j < 32; ++j) z[j] += biases[j];
                         }
                         if (e.z) put_row(zPiece, lane, h / 8, z, e.type);
-                        activate_by(z, e.act);
+                        activate(z, e.act);
                         if (e.residual) add_row(yPiece, lane, h / 8, z, e.type);
                     }
                     put_row(yPiece, lane, h / 8, z, e.type);
@@ -497,8 +480,7 @@ __global__ void __launch_bounds__(256) join_kernel(const void *__restrict__ part
             for (int j = 0; j < 4 && n + j < N; ++j) { const float o[1] = {v[j]}; store_typed<1>(base, m * ld2 + n + j, e.type, o); }
     };
     if (e.z) put(e.z, e.ldz, z);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) z[j] = activate(z[j], e.act);
+    activate(z, e.act);
     if (e.residual) {
         float r[4] = {0, 0, 0, 0};
         if (whole(e.residual, e.ldr)) load_typed<4>(r, e.residual, m * e.ldr + n, e.type);
