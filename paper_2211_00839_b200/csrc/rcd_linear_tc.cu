@@ -32,7 +32,7 @@ constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kPiece = 32 * 128;                        // an epilogue warp's piece of the output: 32 rows of 128 bytes
 constexpr int kStaging = kEpiWarps * 2 * kPiece;
 constexpr int kColumnBytes = kEpiWarps * 2 * 32 * 4;    // 32 biases and 32 scales per warp
-constexpr uint32_t kSpinLimit = 1u << 22;               // polls of ~64 ns: a quarter of a second
+constexpr uint32_t kWaitTurns = 1u << 16;               // of at most 20 us: a second or so
 constexpr int kMostShared = 227 * 1024;
 
 struct __align__(8) Shared {
@@ -53,22 +53,26 @@ struct TcParams {
     int32_t *status;
 };
 
+// (Suspended by the hardware up to 20 us at a time: polls with pauses cost the ring half a slab's time at every turn.)
 __device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Shared *sh)
 {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+    for (uint32_t turn = 0; turn < kWaitTurns; ++turn) {
         uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity), "r"(20000) : "memory");
         if (ok) return true;
-        if (spin > 64) {
-            if (*(volatile int32_t *)&sh->abort) return false;
-            __nanosleep(64);
-        }
+        if (*(volatile int32_t *)&sh->abort) return false;
     }
     atomicExch(&sh->abort, 1);
     return false;
 }
-// The same for a whole warp, which goes on together or gives up together.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t mine;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(mine));
+    return mine != 0;
+}
+// wait_for a whole warp, which goes on together or gives up together.
 __device__ __forceinline__ bool warp_wait_for(uint64_t *bar, uint32_t parity, Shared *sh)
 {
     return __all_sync(0xffffffffu, wait_for(bar, parity, sh));
@@ -217,19 +221,22 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
-        if (lane == 0) {
-            uint32_t it = 0;
-            bool ok = true;
-            const int slabElems = kInt8 ? kSlab : kSlab / 2;
-            const uint32_t bytes = (uint32_t)(kPair ? 2 : 1) * (uint32_t)(kABytes + nMine * kSlab);
-            for (int u = first; u < p.units && ok; u += step) {
-                const Unit t = unit_of(p, u);
-                const int m0 = t.m * rowsPerTile + rank * kRows, n0 = t.n + rank * nMine;
-                const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
-                for (int kb = t.split * p.slabsPerSplit; kb < end; ++kb, ++it) {
-                    const int s = it % p.stages;
-                    if (!wait_for(&sh.empty[s], ((it / p.stages) & 1) ^ 1, &sh)) { ok = false; break; }
-                    unsigned char *a = tiles + (size_t)s * p.stageBytes, *b = a + kABytes;
+        // (The whole warp goes through the loop, one lane issues: addresses stay in uniform registers, which is where these instructions
+        // want them.  With the loop inside one lane's branch a slab took the issuer 600 cycles whatever its size.)
+        const bool leader = elect_one();
+        int s = 0;
+        uint32_t phase = 1;
+        bool ok = true;
+        const int slabElems = kInt8 ? kSlab : kSlab / 2;
+        const uint32_t bytes = (uint32_t)(kPair ? 2 : 1) * (uint32_t)(kABytes + nMine * kSlab);
+        for (int u = first; u < p.units && ok; u += step) {
+            const Unit t = unit_of(p, u);
+            const int m0 = t.m * rowsPerTile + rank * kRows, n0 = t.n + rank * nMine;
+            const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
+            for (int kb = t.split * p.slabsPerSplit; kb < end; ++kb) {
+                if (!warp_wait_for(&sh.empty[s], phase, &sh)) { ok = false; break; }
+                unsigned char *a = tiles + s * p.stageBytes, *b = a + kABytes;
+                if (leader) {
                     if (rank == 0) mbar_expect_tx(&sh.full[s], bytes);
                     uint32_t bar = smem_addr(&sh.full[s]);
                     if constexpr (kPair) bar = leader_addr(&sh.full[s]);
@@ -249,42 +256,52 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                         load(b, &mapB, kb * slabElems, n0);
                     }
                 }
+                __syncwarp();
+                if (++s == p.stages) { s = 0; phase ^= 1; }
             }
-            // after an abort: let the copies already issued land (a pair's report to CTA 0, so by time: some 2 ms)
-            if (*(volatile int32_t *)&sh.abort)
-                let_copies_land();
         }
+        // after an abort: let the copies already issued land (a pair's report to CTA 0, so by time)
+        if (*(volatile int32_t *)&sh.abort) let_copies_land();
     } else if (warp == 1) {
         // ---------------- MMA issuer (a pair's first CTA, for both) ----------------
-        if (lane == 0 && rank == 0) {
-            uint32_t it = 0, nt = 0;
+        if (rank == 0) {
+            const bool leader = elect_one();
+            int s = 0;
+            uint32_t phase = 0, nt = 0;
             bool ok = true;
+            const uint32_t tile0 = smem_addr(tiles);
             for (int u = first; u < p.units && ok; u += step, ++nt) {
                 const Unit t = unit_of(p, u);
                 const uint32_t buf = nt & 1;
-                if (!wait_for(&sh.accEmpty[buf], ((nt >> 1) & 1) ^ 1, &sh)) { ok = false; break; }
+                if (!warp_wait_for(&sh.accEmpty[buf], ((nt >> 1) & 1) ^ 1, &sh)) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t tmemD = tmemBase + buf * 256;
                 const int begin = t.split * p.slabsPerSplit, end = min(p.slabs, begin + p.slabsPerSplit);
-                for (int kb = begin; kb < end; ++kb, ++it) {
-                    const int s = it % p.stages;
-                    if (!wait_for(&sh.full[s], (it / p.stages) & 1, &sh)) { ok = false; break; }
+                for (int kb = begin; kb < end; ++kb) {
+                    if (!warp_wait_for(&sh.full[s], phase, &sh)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t aAddr = smem_addr(tiles + (size_t)s * p.stageBytes), bAddr = aAddr + kABytes;
+                    const uint32_t aAddr = tile0 + (uint32_t)(s * p.stageBytes), bAddr = aAddr + kABytes;
                     const uint64_t descA = kAcrossA ? across_desc(aAddr) : make_smem_desc(aAddr);
                     const uint64_t descB = kAcrossB ? across_desc(bAddr) : make_smem_desc(bAddr);
                     // one MMA takes 32 bytes of k per row, or 16 rows of k of 128 bytes each
                     constexpr uint64_t kStepA = kAcrossA ? 128 : 2, kStepB = kAcrossB ? 128 : 2;
+                    if (leader) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if constexpr (kPair) pair_mma<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
-                        else mma_issue<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
+                        for (int k = 0; k < 4; ++k) {
+                            if constexpr (kPair) pair_mma<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
+                            else mma_issue<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
+                        }
+                        if constexpr (kPair) pair_commit(&sh.empty[s]);
+                        else mma_commit(&sh.empty[s]);
                     }
-                    if constexpr (kPair) pair_commit(&sh.empty[s]);
-                    else mma_commit(&sh.empty[s]);
+                    __syncwarp();
+                    if (++s == p.stages) { s = 0; phase ^= 1; }
                 }
-                if constexpr (kPair) pair_commit(&sh.accFull[buf]);
-                else mma_commit(&sh.accFull[buf]);
+                if (leader) {
+                    if constexpr (kPair) pair_commit(&sh.accFull[buf]);
+                    else mma_commit(&sh.accFull[buf]);
+                }
+                __syncwarp();
             }
         }
     } else {
