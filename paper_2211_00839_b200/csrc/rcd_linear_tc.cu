@@ -28,6 +28,7 @@ constexpr int kBox = 64 * kSlab;                        // 8 KB: 64 k rows of 64
 constexpr int kABytes = kRows * kSlab;
 constexpr int kMostStages = 8;
 constexpr int kEpiWarps = 8;
+constexpr int kChunkSlabs = 8;                          // 512 k of 16 bits
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kPiece = 32 * 128;                        // an epilogue warp's piece of the output: 32 rows of 128 bytes
 constexpr int kStaging = kEpiWarps * 2 * kPiece;
@@ -45,7 +46,7 @@ struct __align__(8) Shared {
 constexpr int kFixedShared = kStaging + kColumnBytes + (int)sizeof(Shared);
 
 struct TcParams {
-    int32_t M, N, tilesN, tiles, units, slabs, slabsPerSplit, tn, stages, stageBytes, rowsPart;
+    int32_t M, N, tilesN, tiles, units, slabs, slabsPerSplit, chunk, tn, stages, stageBytes, rowsPart;
     uint32_t idesc;
     Epilogue e;
     bool raw;                                           // accumulators as they are, into e.y: [split][rowsPart][ldy]
@@ -181,7 +182,7 @@ __device__ __forceinline__ Unit unit_of(const TcParams &p, int u)
     return t;
 }
 
-template <bool kInt8, bool kAcrossA, bool kAcrossB, bool kPair>
+template <bool kInt8, bool kAcrossA, bool kAcrossB, bool kChunks, bool kPair>
 __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUtensorMap &mapB, const CUtensorMap &mapY, const CUtensorMap &mapZ, const CUtensorMap &mapR, const TcParams &p)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -270,38 +271,41 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             uint32_t phase = 0, nt = 0;
             bool ok = true;
             const uint32_t tile0 = smem_addr(tiles);
-            for (int u = first; u < p.units && ok; u += step, ++nt) {
+            for (int u = first; u < p.units && ok; u += step) {
                 const Unit t = unit_of(p, u);
-                const uint32_t buf = nt & 1;
-                if (!warp_wait_for(&sh.accEmpty[buf], ((nt >> 1) & 1) ^ 1, &sh)) { ok = false; break; }
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t tmemD = tmemBase + buf * 256;
-                const int begin = t.split * p.slabsPerSplit, end = min(p.slabs, begin + p.slabsPerSplit);
-                for (int kb = begin; kb < end; ++kb) {
-                    if (!warp_wait_for(&sh.full[s], phase, &sh)) { ok = false; break; }
+                const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
+                for (int begin = t.split * p.slabsPerSplit; begin < end && ok; begin += p.chunk, ++nt) {
+                    const uint32_t buf = nt & 1;
+                    if (!warp_wait_for(&sh.accEmpty[buf], ((nt >> 1) & 1) ^ 1, &sh)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t aAddr = tile0 + (uint32_t)(s * p.stageBytes), bAddr = aAddr + kABytes;
-                    const uint64_t descA = kAcrossA ? across_desc(aAddr) : make_smem_desc(aAddr);
-                    const uint64_t descB = kAcrossB ? across_desc(bAddr) : make_smem_desc(bAddr);
-                    // one MMA takes 32 bytes of k per row, or 16 rows of k of 128 bytes each
-                    constexpr uint64_t kStepA = kAcrossA ? 128 : 2, kStepB = kAcrossB ? 128 : 2;
-                    if (leader) {
+                    const uint32_t tmemD = tmemBase + buf * 256;
+                    const int stop = min(end, begin + p.chunk);
+                    for (int kb = begin; kb < stop; ++kb) {
+                        if (!warp_wait_for(&sh.full[s], phase, &sh)) { ok = false; break; }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t aAddr = tile0 + (uint32_t)(s * p.stageBytes), bAddr = aAddr + kABytes;
+                        const uint64_t descA = kAcrossA ? across_desc(aAddr) : make_smem_desc(aAddr);
+                        const uint64_t descB = kAcrossB ? across_desc(bAddr) : make_smem_desc(bAddr);
+                        // one MMA takes 32 bytes of k per row, or 16 rows of k of 128 bytes each
+                        constexpr uint64_t kStepA = kAcrossA ? 128 : 2, kStepB = kAcrossB ? 128 : 2;
+                        if (leader) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if constexpr (kPair) pair_mma<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
-                            else mma_issue<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
+                            for (int k = 0; k < 4; ++k) {
+                                if constexpr (kPair) pair_mma<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
+                                else mma_issue<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
+                            }
+                            if constexpr (kPair) pair_commit(&sh.empty[s]);
+                            else mma_commit(&sh.empty[s]);
                         }
-                        if constexpr (kPair) pair_commit(&sh.empty[s]);
-                        else mma_commit(&sh.empty[s]);
+                        __syncwarp();
+                        if (++s == p.stages) { s = 0; phase ^= 1; }
+                    }
+                    if (leader) {
+                        if constexpr (kPair) pair_commit(&sh.accFull[buf]);
+                        else mma_commit(&sh.accFull[buf]);
                     }
                     __syncwarp();
-                    if (++s == p.stages) { s = 0; phase ^= 1; }
                 }
-                if (leader) {
-                    if constexpr (kPair) pair_commit(&sh.accFull[buf]);
-                    else mma_commit(&sh.accFull[buf]);
-                }
-                __syncwarp();
             }
         }
     } else {
@@ -335,97 +339,152 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         uint32_t nt = 0, turn = 0;
         if (p.tmaR && lane == 0) fetch(first, half, 0);
         bool ok = true;
-        for (int u = first; u < p.units && ok; u += step, ++nt) {
-            const Unit t = unit_of(p, u);
-            const uint32_t buf = nt & 1;
-            if (!warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh)) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t tmemRow = tmemBase + buf * 256 + ((uint32_t)(q * 32) << 16);
-            const int64_t rawRow = (int64_t)t.split * p.rowsPart;
-            for (int k = half; k < pieces; k += 2) {
-                Piece o;
-                if (!piece_of(u, k, &o)) continue;
-                unsigned char *const yPiece = mine + (alternate ? (turn & 1) * kPiece : 0);
-                unsigned char *const zPiece = mine + kPiece;
-                // what was stored from these buffers has been read out of them
-                if (lane == 0) bulk_wait_read();
-                __syncwarp();
-                if (p.tmaR) {
-                    if (alternate && lane == 0) fetch(u, k + 2, (turn & 1) ^ 1);
-                    // (with z in the other buffer the residual is fetched when the last piece has left)
-                    if (!warp_wait_for(&sh.residual[ew][alternate ? turn & 1 : 0], alternate ? (turn >> 1) & 1 : turn & 1, &sh)) { ok = false; break; }
-                } else if (e.residual) {
-                    if (e.type == RCD_ELEM_F32) move_piece<true>(yPiece, (float *)e.residual + (int64_t)o.row * e.ldr + o.col, e.ldr, p.M - o.row, p.N - o.col);
-                    else move_piece<true>(yPiece, (uint16_t *)e.residual + (int64_t)o.row * e.ldr + o.col, e.ldr, p.M - o.row, p.N - o.col);
-                    __syncwarp();
-                }
-                const int row = o.row + lane;
-                const float sx = e.xs && row < p.M ? e.xs[row] : 1.0f;
-                for (int h = 0; h < wide; h += 32) {
-                    uint32_t v[32];
-                    tmem_load_32cols(tmemRow + (uint32_t)(k * wide + h), v);
-                    const int col = o.col + h + lane;
-                    if (!p.raw && (e.bias || e.ws)) {
-                        __syncwarp();
-                        biases[lane] = e.bias && col < p.N ? e.bias[col] : 0.0f;
-                        scales[lane] = e.ws && col < p.N ? e.ws[col] : 1.0f;
-                        __syncwarp();
-                    }
-                    tmem_load_wait();
-                    float z[32];
-                    if (p.raw) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);        // (integers stay what they are)
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) z[j] = kInt8 ? (float)(int32_t)v[j] : __uint_as_float(v[j]);
-                        if constexpr (kInt8) {
-                            if (e.xs) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) z[j] *= sx;
-                            }
-                            if (e.ws) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) z[j] *= scales[j];
-                            }
-                        }
-                        if (e.bias) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) z[j] += biases[j];
-                        }
-                        if (e.z) put_row(zPiece, lane, h / 8, z, e.type);
-                        activate(z, e.act);
-                        if (e.residual) add_row(yPiece, lane, h / 8, z, e.type);
-                    }
-                    put_row(yPiece, lane, h / 8, z, e.type);
-                }
-                if (p.tmaY || p.tmaZ) proxy_fence();
-                __syncwarp();
-                auto send = [&](bool byTma, const CUtensorMap *map, unsigned char *piece, void *to, int64_t ld, int64_t rowBase) {
-                    if (byTma) {
-                        if (lane == 0) tma_store_2d(map, piece, o.col, (int)rowBase + o.row);
-                    } else if (e.type == RCD_ELEM_F32) {
-                        move_piece<false>(piece, (float *)to + (rowBase + o.row) * ld + o.col, ld, p.M - o.row, p.N - o.col);
-                    } else {
-                        move_piece<false>(piece, (uint16_t *)to + (rowBase + o.row) * ld + o.col, ld, p.M - o.row, p.N - o.col);
-                    }
-                };
-                send(p.tmaY, &mapY, yPiece, e.y, e.ldy, p.raw ? rawRow : 0);
-                if (e.z) send(p.tmaZ, &mapZ, zPiece, e.z, e.ldz, 0);
-                if (lane == 0) bulk_commit();
-                __syncwarp();
-                if (p.tmaR && !alternate && lane == 0) {
-                    bulk_wait_read();
-                    fetch(u, k + 2, 0);
-                }
-                ++turn;
+        unsigned char *yPiece = mine;
+        unsigned char *const zPiece = mine + kPiece;
+        // a piece's place in shared memory is free, and the residual lies there
+        auto begin_piece = [&](int u, int k, const Piece &o) {
+            yPiece = mine + (alternate ? (turn & 1) * kPiece : 0);
+            if (lane == 0) bulk_wait_read();                          // (what was stored from it has been read out of it)
+            __syncwarp();
+            if (p.tmaR) {
+                if (alternate && lane == 0) fetch(u, k + 2, (turn & 1) ^ 1);
+                // (with z in the other buffer the residual is fetched when the last piece has left)
+                return warp_wait_for(&sh.residual[ew][alternate ? turn & 1 : 0], alternate ? (turn >> 1) & 1 : turn & 1, &sh);
             }
-            // hand the accumulator back
+            if (e.residual) {
+                if (e.type == RCD_ELEM_F32) move_piece<true>(yPiece, (float *)e.residual + (int64_t)o.row * e.ldr + o.col, e.ldr, p.M - o.row, p.N - o.col);
+                else move_piece<true>(yPiece, (uint16_t *)e.residual + (int64_t)o.row * e.ldr + o.col, e.ldr, p.M - o.row, p.N - o.col);
+                __syncwarp();
+            }
+            return true;
+        };
+        // biases and scales of 32 columns, for all lanes
+        auto columns_of = [&](int col) {
+            if (p.raw || !(e.bias || e.ws)) return;
+            __syncwarp();
+            biases[lane] = e.bias && col + lane < p.N ? e.bias[col + lane] : 0.0f;
+            scales[lane] = e.ws && col + lane < p.N ? e.ws[col + lane] : 1.0f;
+            __syncwarp();
+        };
+        // 32 columns of the lane's row, from column h of the piece on
+        auto finish = [&](float (&z)[32], float sx, int h) {
+            if (!p.raw) {
+                if constexpr (kInt8) {
+                    if (e.xs) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] *= sx;
+                    }
+                    if (e.ws) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] *= scales[j];
+                    }
+                }
+                if (e.bias) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[j] += biases[j];
+                }
+                if (e.z) put_row(zPiece, lane, h / 8, z, e.type);
+                activate(z, e.act);
+                if (e.residual) add_row(yPiece, lane, h / 8, z, e.type);
+            }
+            put_row(yPiece, lane, h / 8, z, e.type);
+        };
+        auto end_piece = [&](int u, int k, const Piece &o, int rowBase) {
+            if (p.tmaY || p.tmaZ) proxy_fence();
+            __syncwarp();
+            auto send = [&](bool byTma, const CUtensorMap *map, unsigned char *piece, void *to, int64_t ld, int base) {
+                if (byTma) {
+                    if (lane == 0) tma_store_2d(map, piece, o.col, base + o.row);
+                } else if (e.type == RCD_ELEM_F32) {
+                    move_piece<false>(piece, (float *)to + ((int64_t)base + o.row) * ld + o.col, ld, p.M - o.row, p.N - o.col);
+                } else {
+                    move_piece<false>(piece, (uint16_t *)to + ((int64_t)base + o.row) * ld + o.col, ld, p.M - o.row, p.N - o.col);
+                }
+            };
+            send(p.tmaY, &mapY, yPiece, e.y, e.ldy, rowBase);
+            if (e.z) send(p.tmaZ, &mapZ, zPiece, e.z, e.ldz, 0);
+            if (lane == 0) bulk_commit();
+            __syncwarp();
+            if (p.tmaR && !alternate && lane == 0) {
+                bulk_wait_read();
+                fetch(u, k + 2, 0);
+            }
+            ++turn;
+        };
+        // hands an accumulator back
+        auto release = [&](uint32_t buf) {
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
                 if constexpr (kPair) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(leader_addr(&sh.accEmpty[buf])) : "memory");
                 else mbar_arrive(&sh.accEmpty[buf]);
+            }
+        };
+        for (int u = first; u < p.units && ok; u += step) {
+            const Unit t = unit_of(p, u);
+            const int rowBase = p.raw ? t.split * p.rowsPart : 0;
+            const int row = t.m * rowsPerTile + rank * kRows + q * 32 + lane;
+            const float sx = kInt8 && e.xs && row < p.M ? e.xs[row] : 1.0f;
+            const uint32_t lanes = (uint32_t)(q * 32) << 16;
+            if constexpr (kChunks) {
+                // The tensor cores cut an fp32 sum off where they cannot hold it, towards zero: 1e-9 of the result per product, 9e-6 after
+                // 8192.  fp32 outputs therefore take their sums in chunks of 512, added up here with rounding (below 6e-7 whatever k is).
+                // The sums are a lane's 128 registers; the next chunk is computed meanwhile.
+                float sum[4][32];
+                const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
+                for (int begin = t.split * p.slabsPerSplit; begin < end && ok; begin += p.chunk, ++nt) {
+                    const uint32_t buf = nt & 1;
+                    if (!warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const bool fresh = begin == t.split * p.slabsPerSplit;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int k = half + 2 * i;
+                        if (k < pieces) {
+                            uint32_t v[32];
+                            tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)(k * 32), v);
+                            tmem_load_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sum[i][j] = fresh ? __uint_as_float(v[j]) : sum[i][j] + __uint_as_float(v[j]);
+                        }
+                    }
+                    release(buf);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int k = half + 2 * i;
+                    Piece o;
+                    if (ok && k < pieces && piece_of(u, k, &o)) {
+                        ok = begin_piece(u, k, o);
+                        if (ok) {
+                            columns_of(o.col);
+                            finish(sum[i], sx, 0);
+                            end_piece(u, k, o, rowBase);
+                        }
+                    }
+                }
+            } else {
+                const uint32_t buf = nt & 1;
+                if (!warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int k = half; k < pieces; k += 2) {
+                    Piece o;
+                    if (!piece_of(u, k, &o)) continue;
+                    if (!begin_piece(u, k, o)) { ok = false; break; }
+                    for (int h = 0; h < wide; h += 32) {
+                        uint32_t v[32];
+                        tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)(k * wide + h), v);
+                        columns_of(o.col + h);
+                        tmem_load_wait();
+                        float z[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] = kInt8 && !p.raw ? (float)(int32_t)v[j] : __uint_as_float(v[j]);      // (raw integers stay what they are)
+                        finish(z, sx, h);
+                    }
+                    end_piece(u, k, o, rowBase);
+                }
+                release(buf);
+                ++nt;
             }
         }
         if (lane == 0) bulk_wait();
@@ -445,15 +504,15 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
 
 #define RCD_PRODUCT_ARGS const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapY, \
                          const __grid_constant__ CUtensorMap mapZ, const __grid_constant__ CUtensorMap mapR, const __grid_constant__ TcParams p
-template <bool kInt8, bool kAcrossA, bool kAcrossB>
+template <bool kInt8, bool kAcrossA, bool kAcrossB, bool kChunks = false>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(RCD_PRODUCT_ARGS)
 {
-    product_body<kInt8, kAcrossA, kAcrossB, false>(mapA, mapB, mapY, mapZ, mapR, p);
+    product_body<kInt8, kAcrossA, kAcrossB, kChunks, false>(mapA, mapB, mapY, mapZ, mapR, p);
 }
-template <bool kInt8, bool kAcrossA, bool kAcrossB>
+template <bool kInt8, bool kAcrossA, bool kAcrossB, bool kChunks = false>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_pair_kernel(RCD_PRODUCT_ARGS)
 {
-    product_body<kInt8, kAcrossA, kAcrossB, true>(mapA, mapB, mapY, mapZ, mapR, p);
+    product_body<kInt8, kAcrossA, kAcrossB, kChunks, true>(mapA, mapB, mapY, mapZ, mapR, p);
 }
 
 // Joins the pieces of the k axis in their order, then the epilogue: four columns per thread.
@@ -660,6 +719,8 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     q.slabs = (int32_t)plan.slabs;
     q.slabsPerSplit = plan.slabsPerSplit;
     q.tn = plan.tn;
+    const bool chunks = !i8 && p.out.type == RCD_ELEM_F32 && plan.slabsPerSplit > kChunkSlabs;
+    q.chunk = chunks ? kChunkSlabs : q.slabs;
     q.stageBytes = kABytes + (plan.pair ? plan.tn / 2 : plan.tn) * kSlab;
     q.stages = std::min(kMostStages, (kMostShared - kFixedShared) / q.stageBytes);
     q.idesc = (i8 ? (2u << 4) | (1u << 7) | (1u << 10)                                     // S8 x S8 -> S32
@@ -688,18 +749,13 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     const int grid = std::min(slots, q.units) * (plan.pair ? 2 : 1);
     const int order = i8 ? 0 : !p.a.across && !p.b.across ? 1 : !p.a.across ? 2 : 3;
     if (p.a.across && !p.b.across) return fail(ctx, RCD_ERR_INTERNAL, "no product takes these orders");
-    rcd_status rs;
-    if (plan.pair) {
-        rs = order == 0   ? run_product(ctx, product_pair_kernel<true, false, false>, 0, grid, smem, maps, q, st)
-             : order == 1 ? run_product(ctx, product_pair_kernel<false, false, false>, 1, grid, smem, maps, q, st)
-             : order == 2 ? run_product(ctx, product_pair_kernel<false, false, true>, 2, grid, smem, maps, q, st)
-                          : run_product(ctx, product_pair_kernel<false, true, true>, 3, grid, smem, maps, q, st);
-    } else {
-        rs = order == 0   ? run_product(ctx, product_kernel<true, false, false>, 4, grid, smem, maps, q, st)
-             : order == 1 ? run_product(ctx, product_kernel<false, false, false>, 5, grid, smem, maps, q, st)
-             : order == 2 ? run_product(ctx, product_kernel<false, false, true>, 6, grid, smem, maps, q, st)
-                          : run_product(ctx, product_kernel<false, true, true>, 7, grid, smem, maps, q, st);
-    }
+    auto run = [&](auto *single, auto *pair, int bit) { return plan.pair ? run_product(ctx, pair, bit, grid, smem, maps, q, st) : run_product(ctx, single, bit + 1, grid, smem, maps, q, st); };
+    const rcd_status rs = order == 0              ? run(product_kernel<true, false, false>, product_pair_kernel<true, false, false>, 0)
+                          : order == 1 && chunks  ? run(product_kernel<false, false, false, true>, product_pair_kernel<false, false, false, true>, 2)
+                          : order == 1            ? run(product_kernel<false, false, false>, product_pair_kernel<false, false, false>, 4)
+                          : order == 2            ? run(product_kernel<false, false, true>, product_pair_kernel<false, false, true>, 6)
+                          : chunks                ? run(product_kernel<false, true, true, true>, product_pair_kernel<false, true, true, true>, 8)
+                                                  : run(product_kernel<false, true, true>, product_pair_kernel<false, true, true>, 10);
     if (rs != RCD_OK || !q.raw) return rs;
     const int64_t threads = p.M * ((p.N + 3) / 4);
     if (i8) join_kernel<true><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(ws + plan.partAt, plan.splits, (int32_t)p.M, plan.rowsPart, (int32_t)p.N, plan.ldPart, p.out);
