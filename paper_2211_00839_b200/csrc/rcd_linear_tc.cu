@@ -106,16 +106,26 @@ __device__ __forceinline__ void move_piece(unsigned char *piece, T *at, int64_t 
     constexpr int kCols = 128 / sizeof(T);
     const int lane = threadIdx.x & 31;
     rows = min(rows, 32);
-    for (int r = 0; r < rows; ++r)
+    // (eight rows' accesses under way at once)
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        T v[8][kCols / 32];
+        auto each = [&](auto go) {
 #pragma unroll
-        for (int c0 = 0; c0 < kCols; c0 += 32) {
-            const int c = c0 + lane;
-            T *s = reinterpret_cast<T *>(piece + piece_at(r, c * (int)sizeof(T) / 16) + c * (int)sizeof(T) % 16);
-            if (c < cols) {
-                if constexpr (kLoad) *s = at[(int64_t)r * ld + c];
-                else at[(int64_t)r * ld + c] = *s;
-            }
+            for (int r = 0; r < 8; ++r)
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    const int row = r0 + r, col = c * 32 + lane;
+                    if (row < rows && col < cols) go(v[r][c], *reinterpret_cast<T *>(piece + piece_at(row, col * (int)sizeof(T) / 16) + col * (int)sizeof(T) % 16), at[(int64_t)row * ld + col]);
+                }
+        };
+        if constexpr (kLoad) {
+            each([](T &x, T &, T &there) { x = there; });
+            each([](T &x, T &here, T &) { here = x; });
+        } else {
+            each([](T &x, T &here, T &) { x = here; });
+            each([](T &x, T &, T &there) { there = x; });
         }
+    }
 }
 
 // 32 fp32 values to one row's 64 or 128 bytes of a piece, from 16-byte chunk `chunk` on.
@@ -358,12 +368,24 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             }
             return true;
         };
-        // biases and scales of 32 columns, for all lanes
-        auto columns_of = [&](int col) {
-            if (p.raw || !(e.bias || e.ws)) return;
+        // The biases and scales of the warp's columns of a tile, 32 at a time (up to four times): asked for before the tile is ready, since
+        // memory takes longer to answer than 32 columns take to finish; and those of one time to all lanes.
+        const bool anyColumns = !p.raw && (e.bias || e.ws);
+        float bias4[4], scale4[4];
+        auto ask_columns = [&](const Unit &t) {
+            if (!anyColumns) return;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int col = t.n + (wide == 64 ? (half + 2 * (c >> 1)) * 64 + (c & 1) * 32 : (half + 2 * c) * 32) + lane;
+                bias4[c] = e.bias && col < p.N ? e.bias[col] : 0.0f;
+                scale4[c] = e.ws && col < p.N ? e.ws[col] : 1.0f;
+            }
+        };
+        auto columns_of = [&](int c) {
+            if (!anyColumns) return;
             __syncwarp();
-            biases[lane] = e.bias && col + lane < p.N ? e.bias[col + lane] : 0.0f;
-            scales[lane] = e.ws && col + lane < p.N ? e.ws[col + lane] : 1.0f;
+            biases[lane] = c == 0 ? bias4[0] : c == 1 ? bias4[1] : c == 2 ? bias4[2] : bias4[3];
+            scales[lane] = c == 0 ? scale4[0] : c == 1 ? scale4[1] : c == 2 ? scale4[2] : scale4[3];
             __syncwarp();
         };
         // 32 columns of the lane's row, from column h of the piece on
@@ -376,12 +398,18 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                     }
                     if (e.ws) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) z[j] *= scales[j];
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 w = reinterpret_cast<const float4 *>(scales)[j / 4];
+                            z[j] *= w.x; z[j + 1] *= w.y; z[j + 2] *= w.z; z[j + 3] *= w.w;
+                        }
                     }
                 }
                 if (e.bias) {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) z[j] += biases[j];
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 b = reinterpret_cast<const float4 *>(biases)[j / 4];
+                        z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
+                    }
                 }
                 if (e.z) put_row(zPiece, lane, h / 8, z, e.type);
                 activate(z, e.act);
@@ -426,6 +454,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             const int row = t.m * rowsPerTile + rank * kRows + q * 32 + lane;
             const float sx = kInt8 && e.xs && row < p.M ? e.xs[row] : 1.0f;
             const uint32_t lanes = (uint32_t)(q * 32) << 16;
+            ask_columns(t);
             if constexpr (kChunks) {
                 // The tensor cores cut an fp32 sum off where they cannot hold it, towards zero: 1e-9 of the result per product, 9e-6 after
                 // 8192.  fp32 outputs therefore take their sums in chunks of 512, added up here with rounding (below 6e-7 whatever k is).
@@ -457,7 +486,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                     if (ok && k < pieces && piece_of(u, k, &o)) {
                         ok = begin_piece(u, k, o);
                         if (ok) {
-                            columns_of(o.col);
+                            columns_of(i);
                             finish(sum[i], sx, 0);
                             end_piece(u, k, o, rowBase);
                         }
@@ -474,7 +503,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                     for (int h = 0; h < wide; h += 32) {
                         uint32_t v[32];
                         tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)(k * wide + h), v);
-                        columns_of(o.col + h);
+                        columns_of(wide == 64 ? (k - half) + h / 32 : (k - half) / 2);
                         tmem_load_wait();
                         float z[32];
 #pragma unroll
