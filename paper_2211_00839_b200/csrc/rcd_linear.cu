@@ -168,7 +168,7 @@ struct BackPlan {
     size_t dz, partial, dxWork, dwWork, bytes;
     Product dx, dw;
 };
-BackPlan back_plan(const rcd_ctx *ctx, const rcd_linear_back_args &a, unsigned char *base)
+BackPlan back_plan(rcd_ctx *ctx, const rcd_linear_back_args &a, unsigned char *base)
 {
     BackPlan b{};
     b.slope = a.activation != RCD_ACT_NONE && (a.dx_dev_or_null || a.dw_dev_or_null);

@@ -1,6 +1,8 @@
 // What the translation units of rcd_linear and rcd_linear_backward share.
 #pragma once
 
+#include <type_traits>
+
 #include "rcd_elem.cuh"
 
 namespace rcd {
@@ -27,8 +29,12 @@ struct Product {
     Epilogue out;
 };
 
-size_t product_workspace(const rcd_ctx *ctx, const Product &p);
+size_t product_workspace(rcd_ctx *ctx, const Product &p);
 rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaStream_t st);
+
+// The product of at most 32 rows (rcd_linear_few.cu), and whether it takes one: no workspace.
+bool few_rows(const Product &p);
+rcd_status launch_few_rows(rcd_ctx *ctx, const Product &p, cudaStream_t st);
 
 // out[c] = sum over the rows of partial[rows][d], in a fixed order
 rcd_status launch_column_sums(rcd_ctx *ctx, const float *partial, int64_t rows, int64_t d, float *out, cudaStream_t st);

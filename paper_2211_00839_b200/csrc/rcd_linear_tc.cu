@@ -628,12 +628,12 @@ bool mappable(const Operand &o, int64_t eb) { return ((uintptr_t)o.p) % 16 == 0 
 // Which tile, and into how many pieces the k axis is cut: the least of an estimate in cycles.  A slab costs an SM its share of the
 // tensor pipe (128 x 256 x 128 bytes: 512 cycles) or what its operands take from L2 (some 56 bytes a cycle), a tile its epilogue behind the
 // last slab; pieces cost the join's launch and their way through L2.
-Plan plan_product(const rcd_ctx *ctx, const Product &p)
+Plan make_plan(const rcd_ctx *ctx, const Product &p, bool packA, bool packB)
 {
     Plan best{};
     const int64_t eb = elem_bytes(p.type);
-    best.packA = !mappable(p.a, eb);
-    best.packB = !mappable(p.b, eb);
+    best.packA = packA;
+    best.packB = packB;
     const int64_t slabElems = kSlab / eb;
     const int64_t slabs = (p.K + slabElems - 1) / slabElems;
     double least = 1e300;
@@ -680,6 +680,26 @@ Plan plan_product(const rcd_ctx *ctx, const Product &p)
     return best;
 }
 
+// A call asks three times (workspace twice, launch), a program the same sizes over and over: the last eight answers are kept, by
+// sizes, types and orders alone.
+struct PlanCache {
+    struct Entry { int64_t M, N, K, ldA, ldB; int how; Plan plan; } of[8];
+    unsigned next;
+};
+const Plan &plan_product(rcd_ctx *ctx, const Product &p)
+{
+    static_assert(sizeof(PlanCache) <= sizeof(ctx->productPlans) && std::is_trivially_copyable<PlanCache>::value, "the context has room for it");
+    PlanCache &c = *reinterpret_cast<PlanCache *>(ctx->productPlans);      // (zeros at first: how 0 is nobody's)
+    const int64_t eb = elem_bytes(p.type);
+    const bool packA = !mappable(p.a, eb), packB = !mappable(p.b, eb);
+    const int how = 1 | (int)p.type << 1 | (int)p.a.across << 3 | (int)p.b.across << 4 | (int)packA << 5 | (int)packB << 6;
+    for (const PlanCache::Entry &e : c.of)
+        if (e.how == how && e.M == p.M && e.N == p.N && e.K == p.K && e.ldA == p.a.ld && e.ldB == p.b.ld) return e.plan;
+    PlanCache::Entry &e = c.of[c.next++ % 8];
+    e = {p.M, p.N, p.K, p.a.ld, p.b.ld, how, make_plan(ctx, p, packA, packB)};
+    return e.plan;
+}
+
 rcd_status encode(rcd_ctx *ctx, CUtensorMap *map, CUtensorMapDataType type, const void *p, int64_t inner, int64_t outer, int64_t ldBytes, int boxInner, int boxOuter)
 {
     EncodeTiledFn fn = encode_tiled_fn();
@@ -715,10 +735,11 @@ rcd_status run_product(rcd_ctx *ctx, Kernel *kernel, int bit, int grid, size_t s
 
 }  // namespace
 
-size_t product_workspace(const rcd_ctx *ctx, const Product &p) { return plan_product(ctx, p).bytes; }
+size_t product_workspace(rcd_ctx *ctx, const Product &p) { return few_rows(p) ? 0 : plan_product(ctx, p).bytes; }
 
 rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaStream_t st)
 {
+    if (few_rows(p)) return launch_few_rows(ctx, p, st);
     const Plan plan = plan_product(ctx, p);
     unsigned char *ws = (unsigned char *)workspace;
     const int64_t eb = elem_bytes(p.type);
