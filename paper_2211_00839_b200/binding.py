@@ -6,7 +6,8 @@ compiled library is missing, importing this module raises; there is no CPU
 fallback of any kind.
 
 The functions keep the names of the C entry points (``rcd_similarity``,
-``rcd_partition``, ``rcd_partition_host``, ``rcd_objective``, ``rcd_quotas``);
+``rcd_partition``, ``rcd_partition_host``, ``rcd_objective``, ``rcd_quotas``,
+``rcd_rms_norm``, ``rcd_linear`` and their ``_backward``, ...);
 ``Context`` wraps ``rcd_create`` / ``rcd_destroy``.
 """
 from __future__ import annotations
@@ -286,7 +287,9 @@ class Context:
             raise RcdError(st, lib.rcd_last_error(self._h).decode())
 
     def _stream(self):
-        return C.c_void_p(_torch().cuda.current_stream(self.torch_device).cuda_stream)
+        # (the raw handle where this torch gives it: a Stream object is a tenth of a small call's time)
+        raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)
+        return C.c_void_p(raw(self.device) if raw is not None else _torch().cuda.current_stream(self.torch_device).cuda_stream)
 
     def workspace(self, nbytes: int):
         """A cached uint8 device tensor of at least ``nbytes`` (torch's allocator aligns it to 512 bytes)."""
@@ -353,12 +356,29 @@ class Context:
         self._check(fn(self._h, code, N, d, L, M_max, W, C.byref(out)))
         return int(out.value)
 
+    def features(self, hidden, kind: int = RCD_FEAT_BF16, scale: float = RCD_FEATURE_SCALE):
+        """Rows as they come (bfloat16, float16 or float32 [N, d]) to what a partition reads, by ``rcd_rms_norm`` without eps:
+        ``RCD_FEAT_BF16`` L2-normalised rows (products are cosines), ``RCD_FEAT_I8`` rows of root mean square 1 as int8 on the one
+        ``scale`` (cut off at 127 of it).  A row of zeros stays one."""
+        torch = _torch()
+        if hidden.dim() != 2:
+            raise ValueError("features are rows: [N, d], got %s" % (tuple(hidden.shape),))
+        if kind == RCD_FEAT_I8:
+            return self.rcd_rms_norm(hidden, eps=0.0, out_dtype=torch.int8, scale=scale)[0]
+        if kind != RCD_FEAT_BF16:
+            raise ValueError("kind must be RCD_FEAT_I8 or RCD_FEAT_BF16")
+        unit = torch.full((hidden.shape[1],), float(hidden.shape[1]) ** -0.5, dtype=torch.float32, device=self.torch_device)
+        return self.rcd_rms_norm(hidden, weight=unit, eps=0.0, out_dtype=torch.bfloat16)[0]
+
     def rcd_partition(self, features, labels, capacities: Sequence[float], L: int, M_max: Optional[int] = None,
-                      want_order: bool = True, want_values: bool = True):
+                      want_order: bool = True, want_values: bool = True, normalize: Optional[int] = None):
         """Device tensors in, device tensors out: (assignment[N] int32, order[N] int32 | None, part_values[L,W] | None).
 
+        ``normalize`` (RCD_FEAT_BF16 or RCD_FEAT_I8): the features are rows as they come, see ``features``.
         Enqueues on the current torch stream; call ``sync_status()`` (or synchronise) before reading."""
         torch = _torch()
+        if normalize is not None:
+            features = self.features(features, normalize)
         features = features.contiguous()
         labels = labels.contiguous()
         assert labels.dtype == torch.int32 and labels.is_cuda and features.is_cuda
@@ -414,9 +434,11 @@ class Context:
                                                self._stream()))
         return assignment, order, values
 
-    def rcd_objective(self, features, labels, assignment, W: int, L: int, M_max: Optional[int] = None):
-        """f(A_j^l) from the plain definition for a given assignment -> (part_values[L,W], total[1])."""
+    def rcd_objective(self, features, labels, assignment, W: int, L: int, M_max: Optional[int] = None, normalize: Optional[int] = None):
+        """f(A_j^l) from the plain definition for a given assignment -> (part_values[L,W], total[1]); ``normalize`` as for rcd_partition."""
         torch = _torch()
+        if normalize is not None:
+            features = self.features(features, normalize)
         features = features.contiguous()
         labels = labels.contiguous()
         assignment = assignment.contiguous()
@@ -435,7 +457,6 @@ class Context:
                                       C.c_void_p(values.data_ptr()), C.c_void_p(total.data_ptr()),
                                       C.c_void_p(ws.data_ptr()), ws.numel(), self._stream()))
         return values, total
-
 
     # -- from hidden states to features
     def _rows(self, t, name: str, d: Optional[int] = None, rows: Optional[int] = None, dtype=None):
@@ -711,3 +732,23 @@ def rcd_partition_host(ctx: Context, features, labels, capacities, L, **kw):
 
 def rcd_objective(ctx: Context, features, labels, assignment, W, L, **kw):
     return ctx.rcd_objective(features, labels, assignment, W, L, **kw)
+
+
+def rcd_rms_norm(ctx: Context, x, **kw):
+    return ctx.rcd_rms_norm(x, **kw)
+
+
+def rcd_rms_norm_backward(ctx: Context, dy, h, **kw):
+    return ctx.rcd_rms_norm_backward(dy, h, **kw)
+
+
+def rcd_quantize_rows(ctx: Context, x):
+    return ctx.rcd_quantize_rows(x)
+
+
+def rcd_linear(ctx: Context, x, w, **kw):
+    return ctx.rcd_linear(x, w, **kw)
+
+
+def rcd_linear_backward(ctx: Context, dy, x, w, **kw):
+    return ctx.rcd_linear_backward(dy, x, w, **kw)

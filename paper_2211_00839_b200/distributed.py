@@ -118,11 +118,12 @@ def partition_sharded_tensors(features, labels, capacities: Sequence[float], L: 
     return out
 
 
-def partition_sharded_gpu(ctx, features, labels, capacities: Sequence[float], L: int, group=None):
+def partition_sharded_gpu(ctx, features, labels, capacities: Sequence[float], L: int, group=None, normalize: Optional[int] = None):
     """Class-sharded partition with the CUDA library as every rank's partitioner (``ctx``: this rank's
     ``binding.Context``; ``features`` / ``labels``: the whole dataset on this rank's GPU).  One NCCL all-gather of
-    4-byte (index, block) pairs at the end; nothing is exchanged while the greedy loops run."""
+    4-byte (index, block) pairs at the end; nothing is exchanged while the greedy loops run.  ``normalize``: the features are
+    rows as they come; every rank normalises those of its own classes (``Context.features``)."""
     def on_this_gpu(f, y, caps, nclasses):
-        assignment, _, _ = ctx.rcd_partition(f, y, caps, nclasses, want_order=False, want_values=False)
+        assignment, _, _ = ctx.rcd_partition(f, y, caps, nclasses, want_order=False, want_values=False, normalize=normalize)
         return assignment
     return partition_sharded_tensors(features, labels, capacities, L, on_this_gpu, group=group)
