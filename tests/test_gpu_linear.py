@@ -61,7 +61,8 @@ def rounded(z, dtype):
 # rows 1 to past several tiles, widths and depths around 8, 16, 32, 64, 128 and 256, odd ones among them
 SIZES = [(1, 1, 1), (1, 2048, 2048), (1, 16, 8), (1, 333, 77), (2, 64, 64), (3, 130, 72), (5, 1000, 520), (8, 512, 1024), (9, 256, 64), (16, 48, 4096), (17, 512, 200),
          (31, 129, 65), (32, 1024, 512), (64, 320, 640), (65, 256, 128), (100, 8, 16), (127, 127, 127), (128, 128, 64), (129, 257, 65), (200, 64, 64),
-         (256, 512, 256), (300, 1, 33), (333, 777, 1001), (500, 520, 2048), (1300, 333, 777), (700, 2048, 512), (2100, 1300, 192), (5000, 64, 512)]
+         (256, 512, 256), (300, 1, 33), (333, 777, 1001), (500, 520, 2048), (1300, 333, 777), (700, 2048, 512), (2100, 1300, 192), (5000, 64, 512),
+         (20000, 512, 256), (12000, 1288, 72)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -91,6 +92,10 @@ def test_exact_products(rcd, ctx, m, n, k, dtype, pad, shift):
             y, pre = ctx.rcd_linear(x, w, bias=b, residual=r, activation=rcd.RCD_ACT_RELU, out_dtype=out, want_preact=True)
             zb = z + b.double()
             assert torch.equal(pre, rounded(zb, out)) and torch.equal(y, rounded(zb.clamp(min=0) + r.double(), out))
+            y, pre = ctx.rcd_linear(x, w, bias=b, residual=r, activation=rcd.RCD_ACT_RELU, out_dtype=out)
+            assert pre is None and torch.equal(y, rounded(zb.clamp(min=0) + r.double(), out))
+            y, pre = ctx.rcd_linear(x, w, bias=b, out_dtype=out, want_preact=True)
+            assert torch.equal(pre, rounded(zb, out)) and torch.equal(y, pre)
     ctx.sync_status()
 
 

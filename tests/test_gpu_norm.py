@@ -75,9 +75,11 @@ def reference(x, r, w, eps):
 
 
 SIZES = [(1, 1), (2, 7), (5, 32), (3, 100), (1, 2048), (33, 512), (1300, 64), (7, 1001), (9, 4096), (2, 4100), (3, 9000), (2, 16384), (3, 16383), (1500, 640)]
+# enough rows for the ring in shared memory: one to sixteen warps per row, rows that leave lanes without elements, a last turn not all groups have
+MANY = [(7200, 64), (7105, 72), (8001, 512), (7111, 1000), (3700, 2048), (3600, 2056), (1900, 4096), (1000, 8192), (700, 16384), (650, 9000)]
 
 
-@pytest.mark.parametrize("n,d", SIZES)
+@pytest.mark.parametrize("n,d", SIZES + MANY)
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("pad,shift,residual,weight", [(0, 0, True, "same"), (8, 0, False, "fp32"), (3, 1, True, None), (0, 1, False, "same")])
 def test_norm(ctx, n, d, dtype, pad, shift, residual, weight):
@@ -110,9 +112,9 @@ def steps_of(x, r, w, eps, scale=None):
     return torch.round(t * inv).to(torch.int8), a[:, 0]
 
 
-@pytest.mark.parametrize("n,d", SIZES)
+@pytest.mark.parametrize("n,d", SIZES + MANY)
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("pad,residual,weight", [(0, True, True), (5, False, False)])
+@pytest.mark.parametrize("pad,residual,weight", [(0, True, True), (5, False, False), (8, False, True)])
 def test_int8(ctx, n, d, dtype, pad, residual, weight):
     """The integers are the stepwise arithmetic's, bit for bit; the scales carry rstd's few roundings."""
     import torch
@@ -134,11 +136,11 @@ def test_int8(ctx, n, d, dtype, pad, residual, weight):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("d", [1, 48, 513, 2048])
-def test_rows_of_zeros_and_special_values(ctx, dtype, d):
+@pytest.mark.parametrize("d,rows_behind", [(1, 0), (48, 0), (513, 0), (2048, 0), (48, 8000), (2048, 8000)])
+def test_rows_of_zeros_and_special_values(ctx, dtype, d, rows_behind):
     import torch
     t = kind(dtype)
-    x = torch.ones(8, d, device="cuda", dtype=t)
+    x = torch.ones(8 + rows_behind, d, device="cuda", dtype=t)
     x[1] = 0
     x[2, d // 2] = float("nan")
     x[3, d - 1] = float("inf")
@@ -217,7 +219,7 @@ def gradients(dy, h, w, eps, dsum):
     return dx if dsum is None else dx + dsum.double(), (dy * h * rstd).sum(0)
 
 
-@pytest.mark.parametrize("n,d", SIZES + [(3000, 2048), (2000, 1000)])
+@pytest.mark.parametrize("n,d", SIZES + MANY + [(3000, 2048), (2000, 1000)])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("pad,weight,dsum", [(0, "same", True), (0, "fp32", False), (3, None, True), (16, "same", False)])
 def test_backward(ctx, n, d, dtype, pad, weight, dsum):
