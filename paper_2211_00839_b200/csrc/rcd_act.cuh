@@ -50,7 +50,7 @@ __device__ __forceinline__ float slope_as(float z)
     if constexpr (kAct == RCD_ACT_GELU) return 0.5f * (1.0f + erf_as(z * kRootHalf)) + z * exp2_fast(-0.5f * kLog2e * z * z) * kRootInv2Pi;
     if constexpr (kAct == RCD_ACT_GELU_TANH) {
         const float t = tanh_exp(kTanhScale * (z + kTanhCube * z * z * z));
-        return 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * kTanhScale * (1.0f + 3.0f * kTanhCube * z * z);
+        return 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * kTanhScale * (1.0f + 3.0f * kTanhCube * fminf(z * z, 1e30f));     // (0 times that, not times infinity)
     }
     if constexpr (kAct == RCD_ACT_SILU) {
         const float s = logistic(z);

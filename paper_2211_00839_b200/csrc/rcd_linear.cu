@@ -12,7 +12,7 @@ namespace {
 
 // dz = dy * act'(z), rounded to the products' type, and the sums of its columns over this CTA's rows.  Bound by memory: 16-byte accesses
 // where rows allow it, 32 threads along a row, 8 rows at a time; a thread's sums meet those of the other seven in shared memory.
-constexpr int kSlopeRows = 64;
+constexpr int kSlopeRows = 32;
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) slope_kernel(const T *__restrict__ dy, int64_t ldDy, const T *__restrict__ z, int64_t ldZ, int64_t rows, int64_t n, int act,
                                                     T *__restrict__ dz, int64_t ldDz, float *__restrict__ partial)
@@ -26,21 +26,32 @@ __global__ void __launch_bounds__(256) slope_kernel(const T *__restrict__ dy, in
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s[i] = 0.0f;
         if (col < n) {
-#pragma unroll 4
-            for (int k = 0; k < kSlopeRows / 8; ++k) {
-                const int64_t r = chunk * kSlopeRows + k * 8 + warp;
-                if (r >= rows) break;
-                float d[VEC];
-                load_pack<VEC>(d, dy + r * ldDy + col);
-                if (z) {
-                    float x[VEC];
-                    load_pack<VEC>(x, z + r * ldZ + col);
-                    slopes<VEC>(d, x, act);
-                }
-                if (dz) store_pack<VEC>(dz + r * ldDz + col, d);
+            // (a thread's four rows are all asked for before the first is worked on)
+            constexpr int kMine = kSlopeRows / 8;
+            Pack<T, VEC> g[kMine], x[kMine];
+            const int64_t row0 = chunk * kSlopeRows + warp;
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) s[i] += d[i];
-            }
+            for (int k = 0; k < kMine; ++k)
+                if (row0 + 8 * k < rows) {
+                    g[k] = *reinterpret_cast<const Pack<T, VEC> *>(dy + (row0 + 8 * k) * ldDy + col);
+                    if (z) x[k] = *reinterpret_cast<const Pack<T, VEC> *>(z + (row0 + 8 * k) * ldZ + col);
+                }
+#pragma unroll
+            for (int k = 0; k < kMine; ++k)
+                if (row0 + 8 * k < rows) {
+                    float d[VEC];
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) d[i] = to_float(g[k].v[i]);
+                    if (z) {
+                        float o[VEC];
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) o[i] = to_float(x[k].v[i]);
+                        slopes<VEC>(d, o, act);
+                    }
+                    if (dz) store_pack<VEC>(dz + (row0 + 8 * k) * ldDz + col, d);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) s[i] += d[i];
+                }
         }
         if (partial) {
 #pragma unroll
@@ -188,6 +199,7 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_linear_back_args &a, unsigned char *b
     b.dw.a = {dzRows.p, dzRows.ld, true};
     b.dw.b = {a.x_dev, a.ldx, true};
     b.dw.out.y = a.dw_dev_or_null; b.dw.out.ldy = a.ld_dw; b.dw.out.type = a.dw_type;
+    b.dw.later = a.dx_dev_or_null != nullptr;
     b.dxWork = b.dwWork = work;            // (one product after the other: the same memory)
     size_t most = 0;
     if (a.dx_dev_or_null) most = std::max(most, product_workspace(ctx, b.dx));
@@ -282,6 +294,7 @@ extern "C" rcd_status rcd_linear_backward(rcd_ctx *ctx, const rcd_linear_back_ar
     }
     unsigned char *ws = (unsigned char *)workspace_dev;
     const BackPlan b = back_plan(ctx, a, ws);
+    if (!a.dx_dev_or_null && !a.dw_dev_or_null) RCD_CUDA(ctx, cudaMemsetAsync(ctx->statusOwn, 0, sizeof(int32_t), st));     // (no product does)
     if (b.slope || b.sums) {
         float *partial = b.sums ? (float *)(ws + b.partial) : nullptr;
         const int64_t per = rows_aligned(a.dy_dev, a.ld_dy, eb, 16) && rows_aligned(a.preact_dev_or_null, a.ld_preact, eb, 16) && a.n % 8 == 0 ? 256 : 32;

@@ -27,6 +27,7 @@ struct Product {
     int64_t M, N, K;
     Operand a, b;
     Epilogue out;
+    bool later;                            // a launch before it in the same call has reported to the status word
 };
 
 size_t product_workspace(rcd_ctx *ctx, const Product &p);

@@ -50,7 +50,7 @@ struct TcParams {
     uint32_t idesc;
     Epilogue e;
     bool raw;                                           // accumulators as they are, into e.y: [split][rowsPart][ldy]
-    bool tmaY, tmaZ, tmaR;
+    bool tmaY, tmaZ, tmaR, clearStatus;
     int32_t *status;
 };
 
@@ -204,7 +204,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
     const int first = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, step = kPair ? (int)(gridDim.x >> 1) : (int)gridDim.x;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)p.status = 0;      // (no wait runs out for a quarter of a second)
+    if (p.clearStatus && blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)p.status = 0;      // (no wait runs out for a second)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMostStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
@@ -786,6 +786,7 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
         q.rowsPart = (int32_t)plan.rowsPart;
     }
     q.status = ctx->statusOwn;
+    q.clearStatus = !p.later;
     const int64_t yb = elem_bytes(q.e.type);
     auto output = [&](const void *base, int64_t ld, int64_t rows, bool *use, CUtensorMap *map) {
         *use = base && rows_aligned(base, ld, yb, 16) && ld * yb < (1LL << 40);

@@ -337,3 +337,34 @@ def test_refusals(rcd, ctx):
     assert run() == 1
     assert rcd.lib.rcd_linear(None, C.byref(a), None, 0, None) == 1
     ctx.sync_status()
+
+
+def test_slopes_of_large_values(rcd, ctx):
+    """Far from zero the slopes are 0 and 1, whatever the squares on the way to them."""
+    import torch
+    z = torch.tensor([[-1e30, -1e20, -200.0, 200.0, 1e20, 1e30]], device="cuda", dtype=torch.bfloat16)
+    one = torch.ones_like(z)
+    for act in ACTS[1:]:
+        _, _, db = ctx.rcd_linear_backward(one, torch.ones(1, 8, device="cuda", dtype=torch.bfloat16), torch.ones(6, 8, device="cuda", dtype=torch.bfloat16),
+                                           preact=z, activation=code(rcd, act))
+        assert db.tolist() == [0, 0, 0, 1, 1, 1], act
+    ctx.sync_status()
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """An output of 2.3 billion elements: its last rows, and x's last rows behind a stride that alone passes 32 bits."""
+    import torch
+    g = seeded("far")
+    m, n, k = 70000, 33000, 32
+    x, w = whole(g, m, k, torch.bfloat16), whole(g, n, k, torch.bfloat16)
+    y, _ = ctx.rcd_linear(x, w)
+    at = torch.tensor([0, 1, m // 2, m - 130, m - 1], device="cuda")
+    assert torch.equal(y[at], rounded(x[at].double() @ w.double().t(), torch.bfloat16))
+    del y
+    far = torch.zeros(5, 1 << 29, device="cuda", dtype=torch.bfloat16)[:, :k]
+    far.copy_(x[:5])
+    y, _ = ctx.rcd_linear(far, w)
+    assert torch.equal(y, rounded(x[:5].double() @ w.double().t(), torch.bfloat16))
+    far2, _ = ctx.rcd_linear(x[:400], w[:64], out=torch.empty(400, 1 << 23, device="cuda", dtype=torch.bfloat16)[:, :64])
+    assert torch.equal(far2, rounded(x[:400].double() @ w[:64].double().t(), torch.bfloat16))
+    ctx.sync_status()

@@ -359,3 +359,20 @@ def test_refusals(rcd, ctx):
     assert rcd.lib.rcd_rms_norm_backward(ctx._h, C.byref(b), C.c_void_p(ws.data_ptr() + 8), (1 << 20) - 8, None) == 1
     assert rcd.lib.rcd_rms_norm(None, C.byref(a), None) == 1
     ctx.sync_status()
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """2.3 billion elements: the last rows, forward and backward."""
+    import torch
+    n, d = 140000, 16384
+    x = torch.ones(n, d, device="cuda", dtype=torch.bfloat16)
+    tail = rows(seeded("far"), 300, d, torch.bfloat16)
+    x[-300:] = tail
+    q, s, _ = ctx.rcd_rms_norm(x, out_dtype=torch.int8)
+    want, _ = steps_of(tail, None, None, 1e-6)
+    assert torch.equal(q[-300:], want) and bool((q[:5] == 127).all())
+    dx, _ = ctx.rcd_rms_norm_backward(x, x)
+    few, _ = ctx.rcd_rms_norm_backward(tail, tail)
+    parts = tail.double().abs() * 2 / tail.double().square().mean(1, keepdim=True).sqrt()
+    check(dx[-300:], few.double(), torch.bfloat16, slack=parts * (STEPS + half_step(torch.bfloat16)))
+    ctx.sync_status()
