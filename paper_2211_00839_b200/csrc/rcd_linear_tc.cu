@@ -84,7 +84,8 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, const void 
                  :: "l"(map), "r"(smem_addr(src)), "r"(c0), "r"(c1) : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" :: "n"(kLeft) : "memory"); }
 __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -354,7 +355,11 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         // a piece's place in shared memory is free, and the residual lies there
         auto begin_piece = [&](int u, int k, const Piece &o) {
             yPiece = mine + (alternate ? (turn & 1) * kPiece : 0);
-            if (lane == 0) bulk_wait_read();                          // (what was stored from it has been read out of it)
+            // (what was stored from it has been read out of it; a residual that comes next needs the other place too)
+            if (lane == 0) {
+                if (alternate && !p.tmaR) bulk_wait_read<1>();
+                else bulk_wait_read<0>();
+            }
             __syncwarp();
             if (p.tmaR) {
                 if (alternate && lane == 0) fetch(u, k + 2, (turn & 1) ^ 1);
@@ -434,7 +439,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             if (lane == 0) bulk_commit();
             __syncwarp();
             if (p.tmaR && !alternate && lane == 0) {
-                bulk_wait_read();
+                bulk_wait_read<0>();
                 fetch(u, k + 2, 0);
             }
             ++turn;

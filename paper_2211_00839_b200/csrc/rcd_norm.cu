@@ -316,7 +316,7 @@ rcd_status norm_rows(rcd_ctx *ctx, const rcd_norm_args &a, bool normalize, cudaS
                          rows_aligned(p.y, p.ldy, yb, std::min<int64_t>(16, vec * yb)) &&
                          rows_aligned(p.w, 0, 1, p.w ? std::min<int64_t>(16, vec * elem_bytes(a.weight_type)) : 1);
     const Ring ring = vectors ? ring_shape(a.d, xb, a.residual_dev_or_null ? 2 : 1, false) : Ring{};
-    if (vectors && ring_pays(ctx, a.rows, ring)) {
+    if (vectors && ring_pays(a.rows, a.d, false)) {
         RCD_TRY(launch_norm_ring(ctx, p, a.x_type, ring, st));
     }
     else if (a.x_type == RCD_ELEM_BF16) launch_norm_type<__nv_bfloat16>(p, vectors, ctx->smCount, st);
@@ -339,7 +339,7 @@ BackShape back_shape(const rcd_ctx *ctx, const rcd_norm_back_args &a)
     if (b.vectors) {
         b.ring = ring_shape(a.d, eb, a.dsum_dev_or_null ? 3 : 2, true);
         // (weights of the rows' type or fp32)
-        b.useRing = ring_pays(ctx, a.rows, b.ring) && (!a.weight_dev_or_null || a.weight_type == a.type || a.weight_type == RCD_ELEM_F32);
+        b.useRing = ring_pays(a.rows, a.d, true) && (!a.weight_dev_or_null || a.weight_type == a.type || a.weight_type == RCD_ELEM_F32);
         if (b.useRing) {
             b.partialRows = ring_ctas(ctx, a.rows, b.ring);
             return b;

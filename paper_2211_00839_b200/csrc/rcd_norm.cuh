@@ -147,8 +147,12 @@ inline Ring ring_shape(int64_t d, int64_t eb, int streams, bool sums)
     g.stages = std::max(1, std::min(kRingStages, slots()));
     return g;
 }
-// The ring pays from some rows per group on (16384 x 4096 ...)
-inline bool ring_pays(const rcd_ctx *ctx, int64_t rows, const Ring &g) { return rows >= 2LL * ctx->smCount * g.groups; }
+// Whether the ring is the faster form.  It takes 3.5 us more to set out than a row per CTA.  bf16, us, ring : row per CTA, rows of
+//   512   forward with residual 9600 rows 9.8 : 7.0, 50 000 43.7 : 47   backward 600 9.3 : 8.5, 1200 9.8 : 10.8
+//   2048  1200 6.8 : 6.1, 2400 8.8 : 9.8, 9600 24.5 : 40.7              600 11.4 : 11.9, 9600 35.3 : 41.6
+//   4096  600 6.1 : 6.9, 1200 8.4 : 9.9                                 148 10.9 : 8.5, 296 11.1 : 11.9
+//   16384 148 5.5 : 6.4, 600 17.2 : 23.2                                148 15.4 : 22.2
+inline bool ring_pays(int64_t rows, int64_t d, bool back) { return rows * d >= (back ? 1LL << 20 : d >= 1024 ? 4LL << 20 : 12LL << 20); }
 
 template <typename Kernel, typename Params>
 rcd_status launch_ring(rcd_ctx *ctx, Kernel *kernel, const Params &p, const Ring &g, int ctas, size_t bytes, cudaStream_t st)

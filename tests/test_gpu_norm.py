@@ -76,7 +76,7 @@ def reference(x, r, w, eps):
 
 SIZES = [(1, 1), (2, 7), (5, 32), (3, 100), (1, 2048), (33, 512), (1300, 64), (7, 1001), (9, 4096), (2, 4100), (3, 9000), (2, 16384), (3, 16383), (1500, 640)]
 # enough rows for the ring in shared memory: one to sixteen warps per row, rows that leave lanes without elements, a last turn not all groups have
-MANY = [(7200, 64), (7105, 72), (8001, 512), (7111, 1000), (3700, 2048), (3600, 2056), (1900, 4096), (1000, 8192), (700, 16384), (650, 9000)]
+MANY = [(7200, 64), (7105, 72), (8001, 512), (7111, 1000), (3700, 2048), (3600, 2056), (1900, 4096), (1000, 8192), (700, 16384), (650, 9000), (25000, 520), (190000, 72)]
 
 
 @pytest.mark.parametrize("n,d", SIZES + MANY)
@@ -136,7 +136,7 @@ def test_int8(ctx, n, d, dtype, pad, residual, weight):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("d,rows_behind", [(1, 0), (48, 0), (513, 0), (2048, 0), (48, 8000), (2048, 8000)])
+@pytest.mark.parametrize("d,rows_behind", [(1, 0), (48, 0), (513, 0), (2048, 0), (48, 300000), (2048, 8000)])
 def test_rows_of_zeros_and_special_values(ctx, dtype, d, rows_behind):
     import torch
     t = kind(dtype)
