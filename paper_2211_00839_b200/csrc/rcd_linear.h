@@ -33,7 +33,7 @@ struct Product {
 size_t product_workspace(rcd_ctx *ctx, const Product &p);
 rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaStream_t st);
 
-// The product of at most 32 rows (rcd_linear_few.cu), and whether it takes one: no workspace.
+// The product of few rows (rcd_linear_few.cu; no workspace), and whether it takes one.
 bool few_rows(const Product &p);
 rcd_status launch_few_rows(rcd_ctx *ctx, const Product &p, cudaStream_t st);
 

@@ -142,10 +142,19 @@ void launch_typed(const FewParams &p, int threads, cudaStream_t st)
 
 }  // namespace
 
+// Up to 8 rows always, up to 16 where the weights are at most 64 MB, up to 32 at most 24 MB: x comes from L1 once per 16 weight rows, and
+// beyond that its way is longer than the weights'.  us here : with the tiles of rcd_linear_tc.cu, weights of
+//   2 MB (512 x 2048 bf16)   1 row 3.2 : 8.5     16 rows 3.7 : 8.6     32 rows 5.0 : 9.0
+//   8 MB (2048 x 2048 bf16)        3.7 : 10.4            4.5 : 10.5            5.7 : 9.9
+//   16 MB (4096 x 4096 int8)       4.3 : 12.8            7.1 : 11.7            9.7 : 14.6
+//   32 MB (4096 x 4096 bf16)       10.6 : 19.1           14.1 : 17.4           18.4 : 17.3
+//   64 MB (4096 x 8192 bf16)       17.2 : 23.3           23.2 : 23.0           30.6 : 23.1
+//   128 MB (8192 x 8192 bf16)      30.6 : 35.6           40.7 : 35.8           50.7 : 33.9
 bool few_rows(const Product &p)
 {
-    const int64_t eb = elem_bytes(p.type);
-    return p.M <= kFewRows && !p.a.across && !p.b.across && p.K * eb % 16 == 0 && p.K * eb < (1LL << 30) && rows_aligned(p.a.p, p.a.ld, eb, 16) && rows_aligned(p.b.p, p.b.ld, eb, 16);
+    const int64_t eb = elem_bytes(p.type), weights = p.N * p.K * eb;
+    return p.M <= kFewRows && (p.M <= 8 || weights <= (p.M <= 16 ? 64LL << 20 : 24LL << 20)) && !p.a.across && !p.b.across && p.K * eb % 16 == 0 &&
+           p.K * eb < (1LL << 30) && rows_aligned(p.a.p, p.a.ld, eb, 16) && rows_aligned(p.b.p, p.b.ld, eb, 16);
 }
 
 rcd_status launch_few_rows(rcd_ctx *ctx, const Product &p, cudaStream_t st)

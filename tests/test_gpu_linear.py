@@ -62,7 +62,7 @@ def rounded(z, dtype):
 SIZES = [(1, 1, 1), (1, 2048, 2048), (1, 16, 8), (1, 333, 77), (2, 64, 64), (3, 130, 72), (5, 1000, 520), (8, 512, 1024), (9, 256, 64), (16, 48, 4096), (17, 512, 200),
          (31, 129, 65), (32, 1024, 512), (64, 320, 640), (65, 256, 128), (100, 8, 16), (127, 127, 127), (128, 128, 64), (129, 257, 65), (200, 64, 64),
          (256, 512, 256), (300, 1, 33), (333, 777, 1001), (500, 520, 2048), (1300, 333, 777), (700, 2048, 512), (2100, 1300, 192), (5000, 64, 512),
-         (20000, 512, 256), (12000, 1288, 72)]
+         (20000, 512, 256), (12000, 1288, 72), (32, 8200, 2048), (16, 8256, 4096)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
