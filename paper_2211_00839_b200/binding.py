@@ -185,9 +185,15 @@ def rcd_batch_sizes(B: int, capacities: Sequence[float], rule: int = RCD_BATCH_P
     return out
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t) -> int:
@@ -258,6 +264,7 @@ class Context:
         cfg.incremental = incremental
         cfg.incremental_max = incremental_max
         self.similarity_kind = similarity_kind
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._h = C.c_void_p()
         st = lib.rcd_create(C.byref(self._h), self.device, C.byref(cfg))
         if st != 0:
@@ -288,7 +295,7 @@ class Context:
 
     def _stream(self):
         # (the raw handle where this torch gives it: a Stream object is a tenth of a small call's time)
-        raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)
+        raw = self._raw_stream
         return C.c_void_p(raw(self.device) if raw is not None else _torch().cuda.current_stream(self.torch_device).cuda_stream)
 
     def workspace(self, nbytes: int):
@@ -529,7 +536,7 @@ class Context:
         a.eps = eps
         kind = (x.dtype if out_dtype is None else out_dtype) if out is None else out.dtype
         a.y_type = _elem(kind, "out_dtype")
-        y = torch.empty(x.shape, dtype=kind, device=self.torch_device) if out is None else out
+        y = (x.new_empty(x.shape) if kind == x.dtype else x.new_empty(x.shape, dtype=kind)) if out is None else out
         a.ldy = d if out is None else self._out(out, "out", x.shape, kind if out_dtype is None else out_dtype)
         a.y = y.data_ptr()
         scales = total = None
@@ -541,7 +548,7 @@ class Context:
             scales = torch.empty(rows, dtype=torch.float32, device=self.torch_device)
             a.scales = scales.data_ptr()
         if want_sum or sum_out is not None:
-            total = torch.empty(x.shape, dtype=x.dtype, device=self.torch_device) if sum_out is None else sum_out
+            total = x.new_empty(x.shape) if sum_out is None else sum_out
             a.ld_sum = d if sum_out is None else self._out(sum_out, "sum_out", x.shape, x.dtype)
             a.sum = total.data_ptr()
         self._check(lib.rcd_rms_norm(self._h, C.byref(a), self._stream()))
@@ -607,7 +614,7 @@ class Context:
             kind = out_dtype if out_dtype is not None else torch.bfloat16 if x.dtype == torch.int8 else x.dtype
         a.y_type = _elem(kind, "out_dtype")
         shape = (*x.shape[:-1], n)
-        y = torch.empty(shape, dtype=kind, device=self.torch_device) if out is None else out
+        y = (x.new_empty(shape) if kind == x.dtype else x.new_empty(shape, dtype=kind)) if out is None else out
         a.ldy = n if out is None else self._out(out, "out", shape, kind if out_dtype is None else out_dtype)
         a.y = y.data_ptr()
         if bias is not None:
