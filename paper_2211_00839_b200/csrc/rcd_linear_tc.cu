@@ -423,7 +423,8 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             put_row(yPiece, lane, h / 8, z, e.type);
         };
         auto end_piece = [&](int u, int k, const Piece &o, int rowBase) {
-            if (p.tmaY || p.tmaZ) proxy_fence();
+            // (for the stores that leave from here by TMA, and for the next residual that TMA writes here: either comes after these ordinary writes)
+            if (p.tmaY || p.tmaZ || p.tmaR) proxy_fence();
             __syncwarp();
             auto send = [&](bool byTma, const CUtensorMap *map, unsigned char *piece, void *to, int64_t ld, int base) {
                 if (byTma) {
