@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kRowThreads) rms_norm_back_kernel(const __grid
         if (!mine) continue;
         const float v = s.x / (float)p.d + p.eps;
         const float rstd = v > 0.0f ? 1.0f / sqrtf(v) : v == 0.0f ? 0.0f : v;
-        const float back = rstd * rstd * (s.y / (float)p.d);
+        const float back = rstd * (rstd * (s.y / (float)p.d));       // (rstd^2 alone leaves fp32 where rstd does not)
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const int col = (c * G + tid) * VEC;

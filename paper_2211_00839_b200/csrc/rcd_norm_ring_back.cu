@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_back_ring_kernel(
         }
         const float v = s.x / (float)p.d + p.eps;
         const float rstd = v > 0.0f ? 1.0f / sqrtf(v) : v == 0.0f ? 0.0f : v;
-        const float back = rstd * rstd * (s.y / (float)p.d);
+        const float back = rstd * (rstd * (s.y / (float)p.d));       // (rstd^2 alone leaves fp32 where rstd does not)
         const Two r2 = two(rstd, rstd), b2 = two(-back, -back);
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
