@@ -184,14 +184,16 @@ RCD_API void rcd_destroy(rcd_ctx *ctx);
 RCD_API const char *rcd_last_error(const rcd_ctx *ctx);
 RCD_API const char *rcd_version(void);
 
-/* Waits for `cuda_stream` and returns the device-side status of the last call on the context. */
+/* Waits for `cuda_stream` and returns the device-side status of the last call on the context.  Norms and products
+ * (rcd_rms_norm, rcd_quantize_rows, rcd_linear and their gradients) are used in chains and before a partition: what they
+ * record is kept, whatever calls follow and however often a captured graph of them is replayed, until this call returns it (once). */
 RCD_API rcd_status rcd_sync_status(rcd_ctx *ctx, void *cuda_stream);
 /* Self-test of the bounded waits the kernels use.  First the greedy loops that write their outputs last get a class whose
  * quotas end before its samples: they have to record that and to write no outputs (RCD_ERR_INTERNAL otherwise; waits for
  * the stream).  Then it enqueues a one-CTA kernel that arrives at a grid barrier expecting two
- * arrivals, and one whose threads wait for copies that nobody makes (the loop in rounds: all have to leave at the same
- * step).  The waits give up after a few thousand polls and record the timeout in the context's status word, so the next
- * rcd_sync_status returns RCD_ERR_TIMEOUT (RCD_ERR_INTERNAL if the threads did not leave together) and the context
+ * arrivals, one whose threads wait for copies that nobody makes (the loop in rounds: all have to leave at the same
+ * step), and one that waits so as the norms and products do.  The waits give up after a few thousand polls and record the
+ * timeout in the context's status words, so the next rcd_sync_status returns RCD_ERR_TIMEOUT (RCD_ERR_INTERNAL if the threads did not leave together) and the context
  * stays usable.  Nothing faults or hangs. */
 RCD_API rcd_status rcd_selftest_bounded_wait(rcd_ctx *ctx, void *cuda_stream);
 /* Waits for the events of the last profiled call and fills `out`. */

@@ -311,6 +311,7 @@ class Context:
         self._check(lib.rcd_selftest_bounded_wait(self._h, self._stream()))
 
     def sync_status(self):
+        """Waits for the current stream and raises what the last call recorded on the device, or any norm or product since it was last asked."""
         self._check(lib.rcd_sync_status(self._h, self._stream()))
 
     def profile(self) -> Dict[str, float]:

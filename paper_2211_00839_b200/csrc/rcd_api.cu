@@ -526,13 +526,23 @@ void rcd_destroy(rcd_ctx *ctx)
     delete ctx;
 }
 
+// (another stream's kernel may be adding to the word meanwhile)
+static __global__ void clear_status_kernel(int32_t *word, int32_t bits) { atomicAnd(word, ~bits); }
+
 rcd_status rcd_sync_status(rcd_ctx *ctx, void *cuda_stream)
 {
     if (!ctx) return RCD_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     RCD_CUDA(ctx, cudaStreamSynchronize(st));
-    int32_t word = 0;
-    RCD_CUDA(ctx, cudaMemcpy(&word, ctx->statusOwn, sizeof word, cudaMemcpyDeviceToHost));
+    int32_t words[kOperatorStatus + 1] = {};
+    RCD_CUDA(ctx, cudaMemcpy(words, ctx->statusOwn, sizeof words, cudaMemcpyDeviceToHost));
+    // the last call's word, if it was one of those that begin by clearing it, and what norms and products have collected
+    const int32_t collected = words[kOperatorStatus], word = collected | (ctx->statusDev == ctx->statusOwn + kOperatorStatus ? 0 : words[0]);
+    if (collected) {
+        clear_status_kernel<<<1, 1, 0, st>>>(ctx->statusOwn + kOperatorStatus, collected);
+        RCD_CUDA(ctx, cudaGetLastError());
+        RCD_CUDA(ctx, cudaStreamSynchronize(st));
+    }
     if (word == 0) return RCD_OK;
     if (word & kDevBadLabel) return fail(ctx, RCD_ERR_INVALID_ARG, "device status %d: label out of range", word);
     if (word & kDevTimeout) return fail(ctx, RCD_ERR_TIMEOUT, "device status %d: a bounded wait inside a kernel ran out", word);
@@ -550,7 +560,8 @@ rcd_status rcd_selftest_bounded_wait(rcd_ctx *ctx, void *cuda_stream)
     if (rs == RCD_OK) rs = selftest_stopped(ctx, false, st);
     if (rs != RCD_OK) return rs;
     rs = launch_bounded_wait_selftest(ctx, (unsigned *)(ctx->statusOwn + 8), ctx->statusOwn, st);
-    return rs == RCD_OK ? launch_step_wait_selftest(ctx, ctx->statusOwn, st) : rs;
+    if (rs == RCD_OK) rs = launch_step_wait_selftest(ctx, ctx->statusOwn, st);
+    return rs == RCD_OK ? launch_operator_wait_selftest(ctx, ctx->statusOwn + kOperatorStatus, st) : rs;
 }
 
 rcd_status rcd_get_profile(rcd_ctx *ctx, rcd_profile *out)

@@ -144,6 +144,7 @@ struct Workspace {
 // Words of rcd_ctx::statusOwn, and where the similarity kernel's tile tickets (zero between launches) begin.
 constexpr int kStatusWords = 1024;
 constexpr int kHistTicket = 32;            // label_hist_few_kernel's (zero between launches)
+constexpr int kOperatorStatus = 48;        // what the norms and products report to: added to by their kernels, cleared by rcd_sync_status alone
 constexpr int kFirstTicket = 64;
 // The staging buffer holds as many class sizes as a call may have, behind them the status words that come along, and last two words
 // that the device writes: a class was left in floating point; the number of the last histogram whose sizes have arrived.
@@ -386,6 +387,7 @@ rcd_status launch_greedy_small(rcd_ctx *ctx, SmallPlan &plan, const Sizes &sz, c
 
 rcd_status launch_bounded_wait_selftest(rcd_ctx *ctx, unsigned *counter, int32_t *status, cudaStream_t st);
 rcd_status launch_step_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st);
+rcd_status launch_operator_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st);
 
 // graph-cut objective: the whole greedy loop, and f from an assignment (selftest: in step, on two CTAs, whatever the plan says)
 rcd_status launch_cut_stopped_selftest(rcd_ctx *ctx, const Sizes &sz, const Workspace &ws, int32_t *assignment, int32_t *order, cudaStream_t st);

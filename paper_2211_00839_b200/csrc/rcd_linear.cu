@@ -199,7 +199,6 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_linear_back_args &a, unsigned char *b
     b.dw.a = {dzRows.p, dzRows.ld, true};
     b.dw.b = {a.x_dev, a.ldx, true};
     b.dw.out.y = a.dw_dev_or_null; b.dw.out.ldy = a.ld_dw; b.dw.out.type = a.dw_type;
-    b.dw.later = a.dx_dev_or_null != nullptr;
     b.dxWork = b.dwWork = work;            // (one product after the other: the same memory)
     size_t most = 0;
     if (a.dx_dev_or_null) most = std::max(most, product_workspace(ctx, b.dx));
@@ -245,6 +244,7 @@ extern "C" rcd_status rcd_linear(rcd_ctx *ctx, const rcd_linear_args *args, void
     size_t need = 0;
     RCD_TRY(rcd_linear_workspace_bytes(ctx, args, &need));
     const rcd_linear_args &a = *args;
+    begin_operator(ctx);
     if (a.rows == 0 || a.n == 0) return RCD_OK;
     RCD_TRY(check_workspace(ctx, workspace_dev, workspace_bytes, need));
     const int64_t eb = elem_bytes(a.type), yb = elem_bytes(a.y_type);
@@ -253,9 +253,6 @@ extern "C" rcd_status rcd_linear(rcd_ctx *ctx, const rcd_linear_args *args, void
                        {a.bias_dev_or_null, 1, a.n, a.n, 4}, {a.x_scales_dev_or_null, 1, a.rows, a.rows, 4}, {a.w_scales_dev_or_null, 1, a.n, a.n, 4}};
     RCD_TRY(check_apart(ctx, out, 3, in, 6));
     RCD_CUDA(ctx, cudaSetDevice(ctx->device));
-    ctx->kernelLaunches = 0;
-    ctx->tcLaunches = 0;
-    ctx->statusDev = ctx->statusOwn;
     return launch_product(ctx, linear_product(a), workspace_dev, (cudaStream_t)cuda_stream);
 }
 
@@ -283,9 +280,7 @@ extern "C" rcd_status rcd_linear_backward(rcd_ctx *ctx, const rcd_linear_back_ar
     RCD_TRY(check_apart(ctx, out, 4, in, 4));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     RCD_CUDA(ctx, cudaSetDevice(ctx->device));
-    ctx->kernelLaunches = 0;
-    ctx->tcLaunches = 0;
-    ctx->statusDev = ctx->statusOwn;
+    begin_operator(ctx);
     if (a.rows == 0 || a.n == 0) {         // sums over nothing
         if (a.n > 0 && a.dw_dev_or_null) RCD_CUDA(ctx, cudaMemset2DAsync(a.dw_dev_or_null, (size_t)(a.ld_dw * wb), 0, (size_t)(a.k * wb), (size_t)a.n, st));
         if (a.n > 0 && a.dbias_dev_or_null) RCD_CUDA(ctx, cudaMemsetAsync(a.dbias_dev_or_null, 0, (size_t)a.n * 4, st));
@@ -294,7 +289,6 @@ extern "C" rcd_status rcd_linear_backward(rcd_ctx *ctx, const rcd_linear_back_ar
     }
     unsigned char *ws = (unsigned char *)workspace_dev;
     const BackPlan b = back_plan(ctx, a, ws);
-    if (!a.dx_dev_or_null && !a.dw_dev_or_null) RCD_CUDA(ctx, cudaMemsetAsync(ctx->statusOwn, 0, sizeof(int32_t), st));     // (no product does)
     if (b.slope || b.sums) {
         float *partial = b.sums ? (float *)(ws + b.partial) : nullptr;
         const int64_t per = rows_aligned(a.dy_dev, a.ld_dy, eb, 16) && rows_aligned(a.preact_dev_or_null, a.ld_preact, eb, 16) && a.n % 8 == 0 ? 256 : 32;

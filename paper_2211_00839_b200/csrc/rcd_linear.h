@@ -27,7 +27,6 @@ struct Product {
     int64_t M, N, K;
     Operand a, b;
     Epilogue out;
-    bool later;                            // a launch before it in the same call has reported to the status word
 };
 
 size_t product_workspace(rcd_ctx *ctx, const Product &p);
@@ -39,6 +38,14 @@ rcd_status launch_few_rows(rcd_ctx *ctx, const Product &p, cudaStream_t st);
 
 // out[c] = sum over the rows of partial[rows][d], in a fixed order
 rcd_status launch_column_sums(rcd_ctx *ctx, const float *partial, int64_t rows, int64_t d, float *out, cudaStream_t st);
+
+// Counters of a call's launches, and the word that rcd_sync_status asks for.
+inline void begin_operator(rcd_ctx *ctx)
+{
+    ctx->kernelLaunches = 0;
+    ctx->tcLaunches = 0;
+    ctx->statusDev = ctx->statusOwn + kOperatorStatus;
+}
 
 rcd_status check_rows(rcd_ctx *ctx, const char *name, const void *p, int64_t rows, int64_t ld, int64_t len, rcd_elem type);
 

@@ -21,7 +21,6 @@ struct FewParams {
     int64_t ldx, ldw;
     int32_t M, N, kBytes;
     Epilogue e;
-    int32_t *status;
 };
 
 template <typename T, bool kInt8>
@@ -51,7 +50,6 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const __grid_constant__ F
     extern __shared__ float sums[];                     // [warps][kBlocks * 8][kTileW]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, g = lane >> 2, t = lane & 3;
     const int n0 = blockIdx.x * kTileW;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)p.status = 0;
     const unsigned char *const wA = (const unsigned char *)p.w + (int64_t)min(n0 + g, p.N - 1) * p.ldw * (int64_t)sizeof(T);
     const unsigned char *const wB = (const unsigned char *)p.w + (int64_t)min(n0 + g + 8, p.N - 1) * p.ldw * (int64_t)sizeof(T);
     const unsigned char *x[kBlocks];
@@ -165,7 +163,6 @@ rcd_status launch_few_rows(rcd_ctx *ctx, const Product &p, cudaStream_t st)
     q.M = (int32_t)p.M; q.N = (int32_t)p.N;
     q.kBytes = (int32_t)(p.K * elem_bytes(p.type));
     q.e = p.out;
-    q.status = ctx->statusOwn;
     // (twice the warps where there are at most two CTAs per SM and every warp still has a piece)
     const int threads = (p.N + kTileW - 1) / kTileW <= 2 * ctx->smCount && q.kBytes >= 1024 ? 512 : 256;
     if (p.type == RCD_ELEM_I8) launch_typed<int8_t>(q, threads, st);

@@ -15,6 +15,7 @@
 // Every wait is bounded, as in the similarity kernel: on expiry the CTA records kDevTimeout and leaves.
 #include "rcd_act.cuh"
 #include "rcd_linear.h"
+#include "rcd_norm.cuh"
 #include "rcd_tc.cuh"
 
 namespace rcd {
@@ -50,14 +51,14 @@ struct TcParams {
     uint32_t idesc;
     Epilogue e;
     bool raw;                                           // accumulators as they are, into e.y: [split][rowsPart][ldy]
-    bool tmaY, tmaZ, tmaR, clearStatus;
+    bool tmaY, tmaZ, tmaR;
     int32_t *status;
 };
 
 // (Suspended by the hardware up to 20 us at a time: polls with pauses cost the ring half a slab's time at every turn.)
-__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Shared *sh)
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Shared *sh, uint32_t turns = kWaitTurns)
 {
-    for (uint32_t turn = 0; turn < kWaitTurns; ++turn) {
+    for (uint32_t turn = 0; turn < turns; ++turn) {
         uint32_t ok;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity), "r"(20000) : "memory");
@@ -74,9 +75,9 @@ __device__ __forceinline__ bool elect_one()
     return mine != 0;
 }
 // wait_for a whole warp, which goes on together or gives up together.
-__device__ __forceinline__ bool warp_wait_for(uint64_t *bar, uint32_t parity, Shared *sh)
+__device__ __forceinline__ bool warp_wait_for(uint64_t *bar, uint32_t parity, Shared *sh, uint32_t turns = kWaitTurns)
 {
-    return __all_sync(0xffffffffu, wait_for(bar, parity, sh));
+    return __all_sync(0xffffffffu, wait_for(bar, parity, sh, turns));
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, const void *src, int c0, int c1)
 {
@@ -205,7 +206,6 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
     const int first = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, step = kPair ? (int)(gridDim.x >> 1) : (int)gridDim.x;
-    if (p.clearStatus && blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)p.status = 0;      // (no wait runs out for a second)
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMostStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
@@ -618,6 +618,28 @@ __global__ void __launch_bounds__(256) pack_kernel(const T *__restrict__ src, in
     }
 }
 
+// The waits of the product and of the norm's ring for copies that nobody makes: either one has to run out for every thread, and the one
+// behind it at once; all of it in the status word, or that it went otherwise.
+__global__ void __launch_bounds__(64) operator_wait_selftest_kernel(int32_t *status)
+{
+    __shared__ Shared sh;
+    __shared__ RingShared ring;
+    if (threadIdx.x == 0) {
+        for (int k = 0; k < 2; ++k) {
+            mbar_init(&sh.full[k], 1);
+            mbar_init(&ring.bar[0][k], 1);
+        }
+        sh.abort = 0;
+        ring.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    const bool came = warp_wait_for(&sh.full[0], 0, &sh, 1u << 5) || ring_wait(&ring.bar[0][0], 0, &ring, 1u << 12);
+    const bool then = warp_wait_for(&sh.full[1], 0, &sh) || ring_wait(&ring.bar[0][1], 0, &ring);
+    const bool wrong = __syncthreads_or(came || then);
+    if (threadIdx.x == 0) atomicOr(status, wrong || !sh.abort || !ring.abort ? kDevBadState : kDevTimeout);
+}
+
 // ---- host side ----
 
 struct Plan {
@@ -741,6 +763,14 @@ rcd_status run_product(rcd_ctx *ctx, Kernel *kernel, int bit, int grid, size_t s
 
 }  // namespace
 
+rcd_status launch_operator_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st)
+{
+    operator_wait_selftest_kernel<<<1, 64, 0, st>>>(status);
+    ctx->kernelLaunches++;
+    RCD_CUDA(ctx, cudaGetLastError());
+    return RCD_OK;
+}
+
 size_t product_workspace(rcd_ctx *ctx, const Product &p) { return few_rows(p) ? 0 : plan_product(ctx, p).bytes; }
 
 rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaStream_t st)
@@ -791,8 +821,7 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
         q.e.ldy = plan.ldPart;
         q.rowsPart = (int32_t)plan.rowsPart;
     }
-    q.status = ctx->statusOwn;
-    q.clearStatus = !p.later;
+    q.status = ctx->statusOwn + kOperatorStatus;
     const int64_t yb = elem_bytes(q.e.type);
     auto output = [&](const void *base, int64_t ld, int64_t rows, bool *use, CUtensorMap *map) {
         *use = base && rows_aligned(base, ld, yb, 16) && ld * yb < (1LL << 40);

@@ -88,7 +88,6 @@ __global__ void __launch_bounds__(kRowThreads) rms_norm_kernel(const __grid_cons
     __shared__ float shMax[32];
     const int G = p.group, tid = threadIdx.x & (G - 1), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t row = (int64_t)blockIdx.x * (blockDim.x / G) + threadIdx.x / G;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)p.status = 0;
     const bool mine = row < p.rows;
     float h[NV][VEC];
 #pragma unroll
@@ -129,7 +128,6 @@ __global__ void __launch_bounds__(kRowThreads) rms_norm_back_kernel(const __grid
     __shared__ float2 sh[2][32];
     const int G = p.group, tid = threadIdx.x & (G - 1), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int perCta = blockDim.x / G, group = threadIdx.x / G;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)p.status = 0;
     float dw[NV][VEC], w[NV][VEC];
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
@@ -295,11 +293,10 @@ rcd_status norm_rows(rcd_ctx *ctx, const rcd_norm_args &a, bool normalize, cudaS
         ranges_meet(a.y_dev, a.rows, a.ldy, a.d, yb, a.scales_dev_or_null, 1, a.rows, a.rows, 4) ||
         ranges_meet(a.sum_dev_or_null, a.rows, a.ld_sum, a.d, xb, a.scales_dev_or_null, 1, a.rows, a.rows, 4))
         return fail(ctx, RCD_ERR_INVALID_ARG, "an output overlaps another argument");
+    begin_operator(ctx);
     if (a.rows == 0) return RCD_OK;
 
     RCD_CUDA(ctx, cudaSetDevice(ctx->device));
-    ctx->kernelLaunches = 0;
-    ctx->statusDev = ctx->statusOwn;
     NormParams p{};
     p.rows = a.rows;
     p.d = (int32_t)a.d;
@@ -310,7 +307,7 @@ rcd_status norm_rows(rcd_ctx *ctx, const rcd_norm_args &a, bool normalize, cudaS
     p.invScale = i8 && a.scale > 0.0f ? 1.0f / a.scale : 0.0f;
     p.normalize = normalize;
     p.sum = a.sum_dev_or_null; p.y = a.y_dev; p.scales = a.scales_dev_or_null;
-    p.status = ctx->statusOwn;
+    p.status = ctx->statusOwn + kOperatorStatus;
     const int64_t vec = 16 / xb;
     const bool vectors = a.d % vec == 0 && rows_aligned(p.x, p.ldx, xb, 16) && rows_aligned(p.r, p.ldr, xb, 16) && rows_aligned(p.sum, p.lds, xb, 16) &&
                          rows_aligned(p.y, p.ldy, yb, std::min<int64_t>(16, vec * yb)) &&
@@ -441,8 +438,7 @@ extern "C" rcd_status rcd_rms_norm_backward(rcd_ctx *ctx, const rcd_norm_back_ar
     }
     cudaStream_t st = (cudaStream_t)cuda_stream;
     RCD_CUDA(ctx, cudaSetDevice(ctx->device));
-    ctx->kernelLaunches = 0;
-    ctx->statusDev = ctx->statusOwn;
+    begin_operator(ctx);
     if (a.rows == 0) {
         if (a.dweight_dev_or_null) RCD_CUDA(ctx, cudaMemsetAsync(a.dweight_dev_or_null, 0, (size_t)a.d * sizeof(float), st));
         return RCD_OK;
@@ -456,7 +452,7 @@ extern "C" rcd_status rcd_rms_norm_backward(rcd_ctx *ctx, const rcd_norm_back_ar
     p.eps = a.eps;
     p.dx = a.dx_dev;
     p.partial = a.dweight_dev_or_null ? (float *)workspace_dev : nullptr;
-    p.status = ctx->statusOwn;
+    p.status = ctx->statusOwn + kOperatorStatus;
     if (b.useRing) {
         RCD_TRY(launch_norm_back_ring(ctx, p, a.type, b.ring, st));
     }

@@ -93,16 +93,17 @@ struct RingShared {
 };
 
 // Bounded.  When it runs out the CTA goes on with what is there and says so in the status word: its groups stay in step.
-__device__ __forceinline__ void ring_wait(uint64_t *bar, uint32_t parity, RingShared *sh)
+__device__ __forceinline__ bool ring_wait(uint64_t *bar, uint32_t parity, RingShared *sh, uint32_t limit = kSpinLimit)
 {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
-        if (mbar_test(bar, parity)) return;
+    for (uint32_t spin = 0; spin < limit; ++spin) {
+        if (mbar_test(bar, parity)) return true;
         if (spin > 64) {
-            if (*(volatile int32_t *)&sh->abort) return;
+            if (*(volatile int32_t *)&sh->abort) return false;
             __nanosleep(64);
         }
     }
     atomicExch(&sh->abort, 1);
+    return false;
 }
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
 {
@@ -111,9 +112,8 @@ __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t b
 }
 __device__ __forceinline__ void group_barrier(int group, int threads) { asm volatile("bar.sync %0, %1;" :: "r"(1 + group), "r"(threads) : "memory"); }
 
-__device__ __forceinline__ void ring_begin(RingShared *sh, const Ring &ring, int32_t *status)
+__device__ __forceinline__ void ring_begin(RingShared *sh, const Ring &ring)
 {
-    if (blockIdx.x == 0 && threadIdx.x == 0) *(volatile int32_t *)status = 0;        // (no wait runs out for a quarter of a second)
     if (threadIdx.x == 0) {
         for (int g = 0; g < ring.groups; ++g)
             for (int k = 0; k < ring.stages; ++k) mbar_init(&sh->bar[g][k], 1);

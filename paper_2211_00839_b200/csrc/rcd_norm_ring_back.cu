@@ -14,7 +14,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_back_ring_kernel(
     [[maybe_unused]] const W *const weights = (const W *)p.w;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ RingShared sh;
-    ring_begin(&sh, ring, p.status);
+    ring_begin(&sh, ring);
     const int lane = threadIdx.x & 31, gw = ring.warpsPerRow, G = 32 * gw;
     const int group = (threadIdx.x >> 5) / gw, inGroup = (threadIdx.x >> 5) % gw, tid = inGroup * 32 + lane;
     const int64_t first = (int64_t)group * gridDim.x + blockIdx.x, step = (int64_t)gridDim.x * ring.groups;
