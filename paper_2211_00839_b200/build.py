@@ -20,6 +20,7 @@ SOURCES = ["rcd_api.cu", "rcd_group.cu", "rcd_similarity.cu", "rcd_similarity_tc
            "rcd_objective.cu", "rcd_objective_static.cu", "rcd_gaussian.cu", "rcd_cut.cu", "rcd_yardstick.cu", "rcd_norm.cu", "rcd_norm_ring.cu", "rcd_norm_ring_back.cu", "rcd_linear.cu", "rcd_linear_tc.cu", "rcd_linear_few.cu"]
 HEADERS = [os.path.join(CSRC, "rcd_internal.h"), os.path.join(CSRC, "rcd_exact.cuh"), os.path.join(CSRC, "rcd_cut_plan.h"),
            os.path.join(CSRC, "rcd_elem.cuh"), os.path.join(CSRC, "rcd_act.cuh"), os.path.join(CSRC, "rcd_linear.h"), os.path.join(CSRC, "rcd_tc.cuh"), os.path.join(CSRC, "rcd_norm.cuh"),
+           os.path.join(CSRC, "rcd_ring.h"),
            os.path.join(ROOT, "include", "rcd.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

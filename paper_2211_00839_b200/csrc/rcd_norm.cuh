@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "rcd_linear.h"
+#include "rcd_ring.h"
 #include "rcd_tc.cuh"
 
 namespace rcd {
@@ -92,7 +93,8 @@ struct RingShared {
     int32_t abort;
 };
 
-// Bounded.  When it runs out the CTA goes on with what is there and says so in the status word: its groups stay in step.
+// Bounded.  When it runs out the CTA goes on with what is there and says so in the status word: its groups stay in step (RingTurn: and
+// order nothing more).
 __device__ __forceinline__ bool ring_wait(uint64_t *bar, uint32_t parity, RingShared *sh, uint32_t limit = kSpinLimit)
 {
     for (uint32_t spin = 0; spin < limit; ++spin) {

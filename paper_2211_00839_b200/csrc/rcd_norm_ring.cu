@@ -58,12 +58,11 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_ring_kernel(const
     };
     if (tid == 0)
         for (int k = 0; k < ring.stages; ++k) order(first + k * step, k);
-    int slot = 0;
-    uint32_t parity = 0;
+    RingTurn at;
     int turn = 0;
     for (int64_t row = first; row < p.rows; row += step, turn ^= 1) {
-        ring_wait(&sh.bar[group][slot], parity, &sh);
-        const T *const x = reinterpret_cast<const T *>(slots + slot * ring.slotBytes);
+        at.waited(ring_wait(&sh.bar[group][at.slot], at.parity, &sh));
+        const T *const x = reinterpret_cast<const T *>(slots + at.slot * ring.slotBytes);
         Two h[NV][P];
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
@@ -89,7 +88,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_ring_kernel(const
         }
         if (gw == 1) {
             __syncwarp();
-            if (tid == 0) order(row + ring.stages * step, slot);
+            if (tid == 0 && at.may_order()) order(row + ring.stages * step, at.slot);
         }
         if (p.sum) {
 #pragma unroll
@@ -141,7 +140,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_ring_kernel(const
                 else sh.part[turn][threadIdx.x >> 5] = make_float4(sum, a, 0.0f, 0.0f);
             }
             group_barrier(group, G);
-            if (tid == 0) order(row + ring.stages * step, slot);
+            if (tid == 0 && at.may_order()) order(row + ring.stages * step, at.slot);
             sum = a = 0.0f;
             sum64 = 0.0;
             for (int k = 0; k < gw; ++k) {
@@ -182,7 +181,7 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_ring_kernel(const
                 }
             }
         }
-        if (++slot == ring.stages) { slot = 0; parity ^= 1; }
+        at.next(ring.stages);
     }
     ring_end(&sh, p.status);
 }

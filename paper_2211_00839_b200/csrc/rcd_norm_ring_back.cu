@@ -35,12 +35,11 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_back_ring_kernel(
     for (int c = 0; c < NV; ++c)
 #pragma unroll
         for (int i = 0; i < P; ++i) dw[c][i] = two(0.0f, 0.0f);
-    int slot = 0;
-    uint32_t parity = 0;
+    RingTurn at;
     int turn = 0;
     for (int64_t row = first; row < p.rows; row += step, turn ^= 1) {
-        ring_wait(&sh.bar[group][slot], parity, &sh);
-        const T *const dyRow = reinterpret_cast<const T *>(slots + slot * ring.slotBytes), *const hRow = dyRow + p.d, *const sumRow = hRow + p.d;
+        at.waited(ring_wait(&sh.bar[group][at.slot], at.parity, &sh));
+        const T *const dyRow = reinterpret_cast<const T *>(slots + at.slot * ring.slotBytes), *const hRow = dyRow + p.d, *const sumRow = hRow + p.d;
         Two hh = two(0.0f, 0.0f), gh = hh;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
@@ -106,8 +105,8 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_back_ring_kernel(
         }
         if (gw == 1) __syncwarp();
         else group_barrier(group, G);
-        if (tid == 0) order(row + ring.stages * step, slot);
-        if (++slot == ring.stages) { slot = 0; parity ^= 1; }
+        if (tid == 0 && at.may_order()) order(row + ring.stages * step, at.slot);
+        at.next(ring.stages);
     }
     ring_end(&sh, p.status);
     if (p.partial) {                                        // (every copy has landed and been read)
