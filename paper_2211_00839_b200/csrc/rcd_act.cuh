@@ -6,7 +6,7 @@
 namespace rcd {
 
 #ifdef __CUDACC__
-constexpr float kRootHalf = 0.70710678118654752f, kRootInv2Pi = 0.39894228040143268f, kTanhScale = 0.79788456080286536f, kTanhCube = 0.044715f;
+constexpr float kRootInv2Pi = 0.39894228040143268f, kTanhScale = 0.79788456080286536f, kTanhCube = 0.044715f;
 
 // One instruction each, results below the normal range as 0: 2^x within 2 units of fp32, 1 / x within one; 1 / infinity is 0.
 __device__ __forceinline__ float exp2_fast(float x)
@@ -22,24 +22,43 @@ __device__ __forceinline__ float inverse_fast(float x)
     return r;
 }
 constexpr float kLog2e = 1.44269504088896341f;
-// erf by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions (absolute error at most 1.5e-7, three units of
-// fp32 next to 1), without branches: many of them side by side in a kernel's epilogue are short.
-__device__ __forceinline__ float erf_as(float x)
+// The normal distribution from -|z| on, and exp(-z^2 / 2): phi = t P(t) exp(-z^2 / 2) with t = 1 / (1 + |z| / sqrt(8)), the form of formula 7.1.26 of
+// Abramowitz and Stegun, Handbook of Mathematical Functions.  P is of degree 8, fitted to the relative error up to |z| = 14 (4.3e-8): what
+// is left below zero is never a difference of near numbers.  In fp32: some 6 units next to 0, and z^2 units from the exponential's
+// argument.  Without branches and two values at a time (each rounded as alone): 301 us for 50 000 x 2048 x 2048 with z kept, 321 one at a time.
+__device__ __forceinline__ float2 normal_tails(float2 z, float2 *density)
 {
-    const float a = fabsf(x), t = inverse_fast(fmaf(0.3275911f, a, 1.0f));
-    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    return copysignf(fmaf(-poly, exp2_fast(-kLog2e * a * a), 1.0f), x);
+    const Two t = two(inverse_fast(fmaf(0.35355339f, fabsf(z.x), 1.0f)), inverse_fast(fmaf(0.35355339f, fabsf(z.y), 1.0f)));
+    auto both = [](float c) { return two(c, c); };
+    Two p = fma2(t, both(-0.0295355041f), both(0.142291993f));
+    p = fma2(t, p, both(-0.243608341f));
+    p = fma2(t, p, both(0.139042139f));
+    p = fma2(t, p, both(-0.0133180469f));
+    p = fma2(t, p, both(0.101345368f));
+    p = fma2(t, p, both(0.121551454f));
+    p = fma2(t, p, both(0.141187713f));
+    p = fma2(t, p, both(0.141043201f));
+    const Two zz = two(z.x, z.y);
+    const float2 u = parts(mul2(both(-0.5f * kLog2e), mul2(zz, zz)));
+    *density = make_float2(exp2_fast(u.x), exp2_fast(u.y));
+    return parts(mul2(mul2(p, t), two(density->x, density->y)));
 }
-// tanh(u) = 1 - 2 / (1 + exp(2 u)); an infinite exponential makes the quotient 0.
-__device__ __forceinline__ float tanh_exp(float u) { return fmaf(-2.0f, inverse_fast(1.0f + exp2_fast(2.0f * kLog2e * u)), 1.0f); }
 __device__ __forceinline__ float logistic(float z) { return inverse_fast(1.0f + exp2_fast(-kLog2e * z)); }
+// The logistic function and its derivative, either of them as small as it is on both sides.
+__device__ __forceinline__ float logistic_slope(float z, float *slope)
+{
+    const float e = exp2_fast(-kLog2e * fabsf(z)), p = inverse_fast(1.0f + e), q = e * p;
+    *slope = q * p;
+    return z < 0.0f ? q : p;
+}
+// 0.5 (1 + tanh(u)) is the logistic function of 2 u, which does not end in a difference: this is 2 u.
+__device__ __forceinline__ float tanh_argument(float z) { return 2.0f * kTanhScale * (z * fmaf(kTanhCube, z * z, 1.0f)); }
 
 template <int kAct>
 __device__ __forceinline__ float activate_as(float z)
 {
     if constexpr (kAct == RCD_ACT_RELU) return z > 0.0f ? z : z == z ? 0.0f : z;      // (a NaN stays one)
-    if constexpr (kAct == RCD_ACT_GELU) return 0.5f * z * (1.0f + erf_as(z * kRootHalf));
-    if constexpr (kAct == RCD_ACT_GELU_TANH) return 0.5f * z * (1.0f + tanh_exp(kTanhScale * (z + kTanhCube * z * z * z)));
+    if constexpr (kAct == RCD_ACT_GELU_TANH) return z * logistic(tanh_argument(z));
     if constexpr (kAct == RCD_ACT_SILU) return z * logistic(z);
     return z;
 }
@@ -47,14 +66,15 @@ template <int kAct>
 __device__ __forceinline__ float slope_as(float z)
 {
     if constexpr (kAct == RCD_ACT_RELU) return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
-    if constexpr (kAct == RCD_ACT_GELU) return 0.5f * (1.0f + erf_as(z * kRootHalf)) + z * exp2_fast(-0.5f * kLog2e * z * z) * kRootInv2Pi;
     if constexpr (kAct == RCD_ACT_GELU_TANH) {
-        const float t = tanh_exp(kTanhScale * (z + kTanhCube * z * z * z));
-        return 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * kTanhScale * (1.0f + 3.0f * kTanhCube * fminf(z * z, 1e30f));     // (0 times that, not times infinity)
+        float slope;
+        const float s = logistic_slope(tanh_argument(z), &slope);
+        return fmaf(z * slope, 2.0f * kTanhScale * fmaf(3.0f * kTanhCube, fminf(z * z, 1e30f), 1.0f), s);     // (0 times that, not times infinity)
     }
     if constexpr (kAct == RCD_ACT_SILU) {
-        const float s = logistic(z);
-        return s * (1.0f + z * (1.0f - s));
+        float slope;
+        const float s = logistic_slope(z, &slope);
+        return fmaf(z, slope, s);
     }
     return 1.0f;
 }
@@ -62,8 +82,19 @@ __device__ __forceinline__ float slope_as(float z)
 template <int N, int kAct>
 __device__ __forceinline__ void activate_all(float (&z)[N])
 {
+    if constexpr (kAct == RCD_ACT_GELU) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) z[j] = activate_as<kAct>(z[j]);
+        for (int j = 0; j < N; j += 2) {
+            const float2 x = make_float2(z[j], z[j + 1 < N ? j + 1 : j]);
+            float2 density;
+            const float2 tail = normal_tails(x, &density);
+            z[j] = x.x * (x.x < 0.0f ? tail.x : 1.0f - tail.x);
+            if (j + 1 < N) z[j + 1] = x.y * (x.y < 0.0f ? tail.y : 1.0f - tail.y);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) z[j] = activate_as<kAct>(z[j]);
+    }
 }
 template <int N>
 __device__ __forceinline__ void activate(float (&z)[N], int act)
@@ -79,8 +110,19 @@ __device__ __forceinline__ void activate(float (&z)[N], int act)
 template <int N, int kAct>
 __device__ __forceinline__ void slopes_all(float (&d)[N], const float (&z)[N])
 {
+    if constexpr (kAct == RCD_ACT_GELU) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) d[j] *= slope_as<kAct>(z[j]);
+        for (int j = 0; j < N; j += 2) {
+            const float2 x = make_float2(z[j], z[j + 1 < N ? j + 1 : j]);
+            float2 density;
+            const float2 tail = normal_tails(x, &density);
+            d[j] *= fmaf(x.x * density.x, kRootInv2Pi, x.x < 0.0f ? tail.x : 1.0f - tail.x);
+            if (j + 1 < N) d[j + 1] *= fmaf(x.y * density.y, kRootInv2Pi, x.y < 0.0f ? tail.y : 1.0f - tail.y);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) d[j] *= slope_as<kAct>(z[j]);
+    }
 }
 template <int N>
 __device__ __forceinline__ void slopes(float (&d)[N], const float (&z)[N], int act)
