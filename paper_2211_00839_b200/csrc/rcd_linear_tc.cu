@@ -29,7 +29,11 @@ constexpr int kBox = 64 * kSlab;                        // 8 KB: 64 k rows of 64
 constexpr int kABytes = kRows * kSlab;
 constexpr int kMostStages = 8;
 constexpr int kEpiWarps = 8;
-constexpr int kChunkSlabs = 8;                          // 512 k of 16 bits
+// The tensor cores cut an fp32 sum off where they cannot hold it, towards zero: products of fp16 and of one sign lose 6.5e-9 of the result
+// each, 3.2e-4 over 50 000 (two thirds of the type's half step).  So sums are taken in chunks that are added up outside with rounding.  fp32
+// outputs: 512 k (2.4e-6 within a chunk, bf16 2.3e-7, and half a unit of fp32 at most for each of them).  16-bit outputs: 2048 k (1.3e-5) where a piece has more than 4096, up to
+// which the loss is a twentieth of fp16's half step.
+constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kPiece = 32 * 128;                        // an epilogue warp's piece of the output: 32 rows of 128 bytes
 constexpr int kStaging = kEpiWarps * 2 * kPiece;
@@ -194,7 +198,8 @@ __device__ __forceinline__ Unit unit_of(const TcParams &p, int u)
     return t;
 }
 
-template <bool kInt8, bool kAcrossA, bool kAcrossB, bool kChunks, bool kPair>
+// kChunks: 0, or the columns of a piece of the output, whose sums are taken in chunks.
+template <bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks, bool kPair>
 __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUtensorMap &mapB, const CUtensorMap &mapY, const CUtensorMap &mapZ, const CUtensorMap &mapR, const TcParams &p)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -325,7 +330,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         unsigned char *const mine = staging + ew * 2 * kPiece;
         float *const biases = columns + ew * 64, *const scales = biases + 32;
         const Epilogue &e = p.e;
-        const int wide = e.type == RCD_ELEM_F32 ? 32 : 64;            // columns of a piece
+        const int wide = kChunks ? kChunks : e.type == RCD_ELEM_F32 ? 32 : 64;        // columns of a piece
         const int pieces = p.tn / wide;
         // a piece's coordinates; false where nothing of it lies inside the output
         struct Piece { int row, col; };
@@ -461,10 +466,8 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             const float sx = kInt8 && e.xs && row < p.M ? e.xs[row] : 1.0f;
             const uint32_t lanes = (uint32_t)(q * 32) << 16;
             ask_columns(t);
-            if constexpr (kChunks) {
-                // The tensor cores cut an fp32 sum off where they cannot hold it, towards zero: 1e-9 of the result per product, 9e-6 after
-                // 8192.  fp32 outputs therefore take their sums in chunks of 512, added up here with rounding (below 6e-7 whatever k is).
-                // The sums are a lane's 128 registers; the next chunk is computed meanwhile.
+            if constexpr (kChunks != 0) {
+                // Sums of chunks (see kChunkSlabs) in a lane's 128 registers, four times 32 columns; the next chunk is computed meanwhile.
                 float sum[4][32];
                 const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
                 for (int begin = t.split * p.slabsPerSplit; begin < end && ok; begin += p.chunk, ++nt) {
@@ -474,10 +477,10 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                     const bool fresh = begin == t.split * p.slabsPerSplit;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int k = half + 2 * i;
-                        if (k < pieces) {
+                        const int col = wide == 64 ? (half + 2 * (i >> 1)) * 64 + (i & 1) * 32 : (half + 2 * i) * 32;
+                        if (col < p.tn) {
                             uint32_t v[32];
-                            tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)(k * 32), v);
+                            tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)col, v);
                             tmem_load_wait();
 #pragma unroll
                             for (int j = 0; j < 32; ++j) sum[i][j] = fresh ? __uint_as_float(v[j]) : sum[i][j] + __uint_as_float(v[j]);
@@ -487,14 +490,14 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int k = half + 2 * i;
+                    const int k = wide == 64 ? half + 2 * (i >> 1) : half + 2 * i, h = wide == 64 ? (i & 1) * 32 : 0;
                     Piece o;
                     if (ok && k < pieces && piece_of(u, k, &o)) {
-                        ok = begin_piece(u, k, o);
+                        if (h == 0) ok = begin_piece(u, k, o);
                         if (ok) {
                             columns_of(i);
-                            finish(sum[i], sx, 0);
-                            end_piece(u, k, o, rowBase);
+                            finish(sum[i], sx, h);
+                            if (h + 32 == wide) end_piece(u, k, o, rowBase);
                         }
                     }
                 }
@@ -539,12 +542,12 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
 
 #define RCD_PRODUCT_ARGS const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapY, \
                          const __grid_constant__ CUtensorMap mapZ, const __grid_constant__ CUtensorMap mapR, const __grid_constant__ TcParams p
-template <bool kInt8, bool kAcrossA, bool kAcrossB, bool kChunks = false>
+template <bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks = 0>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(RCD_PRODUCT_ARGS)
 {
     product_body<kInt8, kAcrossA, kAcrossB, kChunks, false>(mapA, mapB, mapY, mapZ, mapR, p);
 }
-template <bool kInt8, bool kAcrossA, bool kAcrossB, bool kChunks = false>
+template <bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks = 0>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_pair_kernel(RCD_PRODUCT_ARGS)
 {
     product_body<kInt8, kAcrossA, kAcrossB, kChunks, true>(mapA, mapB, mapY, mapZ, mapR, p);
@@ -805,8 +808,9 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     q.slabs = (int32_t)plan.slabs;
     q.slabsPerSplit = plan.slabsPerSplit;
     q.tn = plan.tn;
-    const bool chunks = !i8 && p.out.type == RCD_ELEM_F32 && plan.slabsPerSplit > kChunkSlabs;
-    q.chunk = chunks ? kChunkSlabs : q.slabs;
+    const int chunk = p.out.type == RCD_ELEM_F32 ? kChunkSlabs : kChunkSlabs16;
+    const bool chunks = !i8 && plan.slabsPerSplit > (p.out.type == RCD_ELEM_F32 ? chunk : 2 * chunk);
+    q.chunk = chunks ? chunk : q.slabs;
     q.stageBytes = kABytes + (plan.pair ? plan.tn / 2 : plan.tn) * kSlab;
     q.stages = std::min(kMostStages, (kMostShared - kFixedShared) / q.stageBytes);
     q.idesc = (i8 ? (2u << 4) | (1u << 7) | (1u << 10)                                     // S8 x S8 -> S32
@@ -836,12 +840,19 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     const int order = i8 ? 0 : !p.a.across && !p.b.across ? 1 : !p.a.across ? 2 : 3;
     if (p.a.across && !p.b.across) return fail(ctx, RCD_ERR_INTERNAL, "no product takes these orders");
     auto run = [&](auto *single, auto *pair, int bit) { return plan.pair ? run_product(ctx, pair, bit, grid, smem, maps, q, st) : run_product(ctx, single, bit + 1, grid, smem, maps, q, st); };
-    const rcd_status rs = order == 0              ? run(product_kernel<true, false, false>, product_pair_kernel<true, false, false>, 0)
-                          : order == 1 && chunks  ? run(product_kernel<false, false, false, true>, product_pair_kernel<false, false, false, true>, 2)
-                          : order == 1            ? run(product_kernel<false, false, false>, product_pair_kernel<false, false, false>, 4)
-                          : order == 2            ? run(product_kernel<false, false, true>, product_pair_kernel<false, false, true>, 6)
-                          : chunks                ? run(product_kernel<false, true, true, true>, product_pair_kernel<false, true, true, true>, 8)
-                                                  : run(product_kernel<false, true, true>, product_pair_kernel<false, true, true>, 10);
+    const int wide = !chunks ? 0 : q.e.type == RCD_ELEM_F32 ? 32 : 64;
+    auto run_order = [&](auto acrossA, auto acrossB, int bit) {
+        constexpr bool kA = decltype(acrossA)::value, kB = decltype(acrossB)::value;
+        return wide == 0    ? run(product_kernel<false, kA, kB>, product_pair_kernel<false, kA, kB>, bit)
+               : wide == 32 ? run(product_kernel<false, kA, kB, 32>, product_pair_kernel<false, kA, kB, 32>, bit + 2)
+                            : run(product_kernel<false, kA, kB, 64>, product_pair_kernel<false, kA, kB, 64>, bit + 4);
+    };
+    const std::false_type along;
+    const std::true_type across;
+    const rcd_status rs = order == 0   ? run(product_kernel<true, false, false>, product_pair_kernel<true, false, false>, 0)
+                          : order == 1 ? run_order(along, along, 2)
+                          : order == 2 ? run_order(along, across, 8)
+                                       : run_order(across, across, 14);
     if (rs != RCD_OK || !q.raw) return rs;
     const int64_t threads = p.M * ((p.N + 3) / 4);
     if (i8) join_kernel<true><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(ws + plan.partAt, plan.splits, (int32_t)p.M, plan.rowsPart, (int32_t)p.N, plan.ldPart, p.out);
