@@ -352,7 +352,8 @@ RCD_API rcd_status rcd_objective_class_static(rcd_ctx *ctx, const void *S_dev, r
  *   - rows lie `ld...` ELEMENTS apart (at least the row's length); rows that start on 16 bytes are fastest, any start that
  *     suits the type is taken;
  *   - a call with no rows writes nothing but gradients summed over the rows, as zeros;
- *   - an output overlaps no other argument, but for the one exception stated;
+ *   - an output shares no byte with another argument, but for the one exception stated (it may be a column slice of the same buffer,
+ *     whose rows then lie equally far apart);
  *   - everything is only enqueued, captured calls included; no call keeps anything for the next. */
 typedef enum { RCD_ELEM_I8 = 0, RCD_ELEM_BF16 = 1, RCD_ELEM_F16 = 2, RCD_ELEM_F32 = 3 } rcd_elem;
 

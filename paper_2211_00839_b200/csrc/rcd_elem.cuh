@@ -11,14 +11,21 @@ namespace rcd {
 inline int64_t elem_bytes(rcd_elem t) { return t == RCD_ELEM_I8 ? 1 : t == RCD_ELEM_F32 ? 4 : 2; }
 inline bool elem_is_float(rcd_elem t) { return t == RCD_ELEM_BF16 || t == RCD_ELEM_F16 || t == RCD_ELEM_F32; }
 
-// The last byte of `rows` rows and whether two such ranges share one (an output may not overlap an input).
+// Whether two matrices (rows, elements from row to row, elements of a row, bytes of an element) share a byte; an output may not share one with
+// another argument.  Matrices whose rows lie equally far apart, as column slices of one buffer do, are told apart by their columns;
+// others by their first and last byte.
 inline bool ranges_meet(const void *a, int64_t aRows, int64_t aLd, int64_t aLen, int64_t aBytes,
                         const void *b, int64_t bRows, int64_t bLd, int64_t bLen, int64_t bBytes)
 {
     if (!a || !b || aRows <= 0 || bRows <= 0 || aLen <= 0 || bLen <= 0) return false;
-    const uintptr_t a0 = (uintptr_t)a, a1 = a0 + (uintptr_t)(((aRows - 1) * aLd + aLen) * aBytes);
-    const uintptr_t b0 = (uintptr_t)b, b1 = b0 + (uintptr_t)(((bRows - 1) * bLd + bLen) * bBytes);
-    return a0 < b1 && b0 < a1;
+    const int64_t la = aLen * aBytes, lb = bLen * bBytes;
+    const uintptr_t a0 = (uintptr_t)a, a1 = a0 + (uintptr_t)((aRows - 1) * aLd * aBytes + la);
+    const uintptr_t b0 = (uintptr_t)b, b1 = b0 + (uintptr_t)((bRows - 1) * bLd * bBytes + lb);
+    if (a1 <= b0 || b1 <= a0) return false;
+    const int64_t pitch = aRows > 1 ? aLd * aBytes : bLd * bBytes;          // (a single row lies as far from the next as one likes)
+    if ((bRows > 1 && bLd * bBytes != pitch) || pitch < la || pitch < lb) return true;
+    const int64_t column = a0 <= b0 ? (int64_t)(b0 - a0) % pitch : (pitch - (int64_t)(a0 - b0) % pitch) % pitch;     // of b's rows, from a's
+    return column < la || column + lb > pitch;
 }
 // Whether every row of a matrix starts on `align` bytes (null: nothing to load).
 inline bool rows_aligned(const void *p, int64_t ld, int64_t bytes, int64_t align)

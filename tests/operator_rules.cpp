@@ -3,6 +3,7 @@
 #include <string>
 #include <vector>
 
+#include "rcd_elem.cuh"
 #include "rcd_ring.h"
 
 // A barrier that expects one arrival with the bytes of a copy: its phase ends when both are there.
@@ -55,6 +56,11 @@ int main()
             bool twice = false;
             for (const Barrier &b : bars) twice = twice || b.twice;
             std::cout << twice << " " << inTime << "\n";
+        } else if (what == "meet") {                       // twice: address, rows, elements between rows, elements, bytes of one
+            int64_t a[5], b[5];
+            for (int64_t &x : a) std::cin >> x;
+            for (int64_t &x : b) std::cin >> x;
+            std::cout << rcd::ranges_meet((const void *)a[0], a[1], a[2], a[3], a[4], (const void *)b[0], b[1], b[2], b[3], b[4]) << "\n";
         } else {
             return 1;
         }
