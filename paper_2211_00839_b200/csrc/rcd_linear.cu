@@ -160,13 +160,11 @@ rcd_status check_back(rcd_ctx *ctx, const rcd_linear_back_args &a)
     if (a.dw_dev_or_null && a.dw_type != a.type && a.dw_type != RCD_ELEM_F32) return fail(ctx, RCD_ERR_INVALID_ARG, "dw must have the type of x or be fp32, got type %d", (int)a.dw_type);
     RCD_TRY(check_floats(ctx, "dbias", a.dbias_dev_or_null));
     if (a.dw_dev_or_null) RCD_TRY(check_rows(ctx, "dw", a.dw_dev_or_null, a.n, a.ld_dw, a.k, a.dw_type));
+    if (a.dx_dev_or_null && a.rows > 0) RCD_TRY(check_rows(ctx, "dx", a.dx_dev_or_null, a.rows, a.ld_dx, a.k, a.type));
     if (a.rows == 0 || a.n == 0) return RCD_OK;
     RCD_TRY(check_rows(ctx, "dy", a.dy_dev, a.rows, a.ld_dy, a.n, a.type));
     if (a.dw_dev_or_null) RCD_TRY(check_rows(ctx, "x", a.x_dev, a.rows, a.ldx, a.k, a.type));
-    if (a.dx_dev_or_null) {
-        RCD_TRY(check_rows(ctx, "w", a.w_dev, a.n, a.ldw, a.k, a.type));
-        RCD_TRY(check_rows(ctx, "dx", a.dx_dev_or_null, a.rows, a.ld_dx, a.k, a.type));
-    }
+    if (a.dx_dev_or_null) RCD_TRY(check_rows(ctx, "w", a.w_dev, a.n, a.ldw, a.k, a.type));
     if (a.activation != RCD_ACT_NONE) RCD_TRY(check_rows(ctx, "preact", a.preact_dev_or_null, a.rows, a.ld_preact, a.n, a.type));
     else if (a.preact_dev_or_null) return fail(ctx, RCD_ERR_INVALID_ARG, "preact is given, but there is no activation");
     return RCD_OK;
