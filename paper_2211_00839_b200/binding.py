@@ -13,6 +13,7 @@ The functions keep the names of the C entry points (``rcd_similarity``,
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Dict, Optional, Sequence, Tuple
 
@@ -476,7 +477,7 @@ class Context:
         if t.dim() != 2:
             if t.dim() == 0:
                 raise ValueError("%s has no dimension" % name)
-            t = t.reshape(-1, t.shape[-1]) if t.shape[-1] else t.reshape(0, 0)
+            t = t.reshape(math.prod(t.shape[:-1]), t.shape[-1])
         r, n = t.shape
         if (d is not None and n != d) or (rows is not None and r != rows):
             raise ValueError("%s has shape %s, expected %s rows of %s" % (name, tuple(t.shape), r if rows is None else rows, n if d is None else d))

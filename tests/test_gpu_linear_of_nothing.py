@@ -8,6 +8,16 @@ from test_gpu_norm import ctx, rcd  # noqa: F401  (fixtures)
 pytestmark = pytest.mark.gpu
 
 
+def test_no_columns_of_any_rank(ctx):
+    import torch
+    x, w = torch.ones(2, 3, 64, device="cuda", dtype=torch.bfloat16), torch.empty(0, 64, device="cuda", dtype=torch.bfloat16)
+    y, z = ctx.rcd_linear(x, w, want_preact=True)
+    assert y.shape == (2, 3, 0) and z.shape == (2, 3, 0)
+    dx, dw, db = ctx.rcd_linear_backward(y, x, w)
+    ctx.sync_status()
+    assert dx.shape == (2, 3, 64) and not dx.any() and dw.shape == (0, 64) and db.shape == (0,)
+
+
 def args_of(rcd, rows, n, k):
     a = rcd.RcdLinearBackArgs()
     a.rows, a.n, a.k, a.type, a.dw_type = rows, n, k, rcd.RCD_ELEM_BF16, rcd.RCD_ELEM_F32
