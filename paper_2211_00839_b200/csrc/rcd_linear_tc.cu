@@ -9,7 +9,8 @@
 // memory, so that eight warps finish a tile while the next one is computed: 32 columns at a time from tensor memory, times the scales,
 // plus bias, activation, plus residual, rounded into 32 rows x 128 bytes of shared memory, and out by TMA.  The residual's piece
 // comes in by TMA into the same place one piece ahead.  Rows that a tensor map cannot describe (they do not start on 16 bytes)
-// are first copied (operands), or moved between that place and memory by the warp itself (outputs, residual).
+// are first copied (operands), or moved between that place and memory by the warp itself (outputs, residual); so are the ends of output
+// rows that do not end on 16 bytes: a TMA store writes the last 16 bytes that an element of the row lies in whole.
 //
 // Warp roles: 0 = TMA producer, 1 = TMEM allocation + MMA issue, 2..9 = epilogue, two per quarter of the TMEM lanes.
 // Every wait is bounded, as in the similarity kernel: on expiry the CTA records kDevTimeout and leaves.
@@ -55,7 +56,7 @@ struct TcParams {
     uint32_t idesc;
     Epilogue e;
     bool raw;                                           // accumulators as they are, into e.y: [split][rowsPart][ldy]
-    bool tmaY, tmaZ, tmaR;
+    bool tmaY, tmaZ, tmaR, edgeByHand;                  // edgeByHand: a piece that holds the rows' ends, since TMA stores 16 bytes at a time
     int32_t *status;
 };
 
@@ -432,7 +433,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             if (p.tmaY || p.tmaZ || p.tmaR) proxy_fence();
             __syncwarp();
             auto send = [&](bool byTma, const CUtensorMap *map, unsigned char *piece, void *to, int64_t ld, int base) {
-                if (byTma) {
+                if (byTma && !(p.edgeByHand && o.col + wide > p.N)) {
                     if (lane == 0) tma_store_2d(map, piece, o.col, base + o.row);
                 } else if (e.type == RCD_ELEM_F32) {
                     move_piece<false>(piece, (float *)to + ((int64_t)base + o.row) * ld + o.col, ld, p.M - o.row, p.N - o.col);
@@ -834,6 +835,7 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     RCD_TRY(output(q.e.y, q.e.ldy, q.raw ? plan.splits * plan.rowsPart : p.M, &q.tmaY, &maps[2]));
     RCD_TRY(output(q.e.z, q.e.ldz, p.M, &q.tmaZ, &maps[3]));
     RCD_TRY(output(q.e.residual, q.e.ldr, p.M, &q.tmaR, &maps[4]));
+    q.edgeByHand = !q.raw && p.N * yb % 16 != 0;           // (a piece of the k axis has rows of whole 128 bytes)
     const size_t smem = (size_t)q.stages * q.stageBytes + kFixedShared;
     const int slots = plan.pair ? ctx->smCount / 2 : ctx->smCount;
     const int grid = std::min(slots, q.units) * (plan.pair ? 2 : 1);
