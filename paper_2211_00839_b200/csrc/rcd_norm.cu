@@ -63,7 +63,14 @@ __device__ __forceinline__ void finish_row(const NormParams &p, float (&h)[NV][V
     float rstd;
     if (p.invScale > 0.0f) rstd = rstd_of(sum, p);
     else rstd = rstd_of((float)sum, p);
-    const float inv = rowScale ? row_scale(a, rstd, tid == 0 ? p.scales + row : nullptr) : p.invScale;
+    bool raised = false;
+    const float inv = rowScale ? row_scale(a, rstd, tid == 0 ? p.scales + row : nullptr, &raised) : p.invScale;
+    if (raised) {
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) h[c][i] *= kRaise;
+    }
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
         const int col = (c * G + tid) * VEC;

@@ -60,12 +60,14 @@ __device__ __forceinline__ float rstd_of(double sum, const NormParams &p)
     const double v = sum / (double)p.d + (double)p.eps;
     return v > 0.0 ? (float)(1.0 / sqrt(v)) : v == 0.0 ? 0.0f : (float)v;
 }
-// 127 / a, and the row's scale.
-__device__ __forceinline__ float row_scale(float a, float rstd, float *scale)
+// 127 / a, and the row's scale.  Where 127 / a would leave fp32 (a below 4e-37) it is that of the row times 2^64: the row is to be `raised` first.
+constexpr float kRaise = 18446744073709551616.0f;
+__device__ __forceinline__ float row_scale(float a, float rstd, float *scale, bool *raised)
 {
     const bool fine = a < INFINITY;                            // (not so for a NaN)
     if (scale) *scale = fine ? rstd * a / 127.0f : NAN;
-    return fine && a > 0.0f ? fminf(127.0f / a, 3.402823466e38f) : 0.0f;
+    *raised = a > 0.0f && a < 7.8886091e-31f;                  // 2^-100
+    return fine && a > 0.0f ? 127.0f / (*raised ? a * kRaise : a) : 0.0f;
 }
 // To the nearest integer, halves to even; a NaN is 0.  (With a scale per row nothing is above 127.)
 template <bool kCut>

@@ -161,7 +161,14 @@ __global__ void __launch_bounds__(32 * kRingWarps, 1) rms_norm_ring_kernel(const
         } else {
             float inv = p.invScale;
             if constexpr (kOut == kOutRowScale) {
-                inv = row_scale(a, rstd, tid == 0 ? p.scales + row : nullptr);
+                bool raised;
+                inv = row_scale(a, rstd, tid == 0 ? p.scales + row : nullptr, &raised);
+                if (raised) {
+#pragma unroll
+                    for (int c = 0; c < NV; ++c)
+#pragma unroll
+                        for (int i = 0; i < P; ++i) h[c][i] = mul2(h[c][i], two(kRaise, kRaise));
+                }
             }
             const Two by = kOut == kOutRowScale ? two(inv, inv) : two(rstd, rstd), then = two(inv, inv);
 #pragma unroll
