@@ -467,7 +467,8 @@ class Context:
                                       C.c_void_p(ws.data_ptr()), ws.numel(), self._stream()))
         return values, total
 
-    # -- from hidden states to features
+    # -- from hidden states to features.  (None of these calls is recorded by autograd, also where an argument requires a gradient: the
+    # gradients are the calls' own _backward, which a torch.autograd.Function of the program's can call.)
     def _rows(self, t, name: str, d: Optional[int] = None, rows: Optional[int] = None, dtype=None):
         """A tensor [..., d] on this context's device as (tensor to keep alive, rows, d, elements between rows)."""
         if t.device != self.torch_device:
@@ -521,7 +522,7 @@ class Context:
 
         ``out_dtype`` (default: x's) may be int8: with a scale per row, or all rows on the one ``scale``.  Returns
         (y, scales [rows] | None, h rounded to x's type | None).  ``out`` and ``sum_out`` take y and h in place of new tensors;
-        ``sum_out`` may be ``x`` or ``residual`` itself."""
+        ``sum_out`` may be ``x`` or ``residual`` itself.  Autograd does not record the call: ``rcd_rms_norm_backward`` is its gradient."""
         torch = _torch()
         a = RcdNormArgs()
         kept, rows, d, a.ldx = self._rows(x, "x")
@@ -601,7 +602,8 @@ class Context:
         """act(x w^T + bias) + residual for x [..., k] and w [n, k] in bfloat16, float16 or int8 (x_scales [rows], w_scales [n]).
 
         bias: float32 [n]; residual: [..., n] in the output's type; ``out_dtype``: default x's type, bfloat16 for int8.
-        Returns (y [..., n], the values before the activation | None)."""
+        Returns (y [..., n], the values before the activation | None).  Autograd does not record the call: ``rcd_linear_backward`` is its
+        gradient (bfloat16 and float16)."""
         torch = _torch()
         a = RcdLinearArgs()
         xk, rows, k, a.ldx = self._rows(x, "x")
