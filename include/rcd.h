@@ -356,7 +356,7 @@ RCD_API rcd_status rcd_objective_class_static(rcd_ctx *ctx, const void *S_dev, r
  *     whose rows then lie equally far apart);
  *   - everything is only enqueued, captured calls included (a captured graph may be replayed as long as the context lives: its
  *     kernels report to it);
- *   - no call keeps any of its data for the next; the context remembers how it went about the last eight sizes of products. */
+ *   - no call keeps any of its data for the next; the context remembers how it went about the last sixteen sizes of products. */
 typedef enum { RCD_ELEM_I8 = 0, RCD_ELEM_BF16 = 1, RCD_ELEM_F16 = 2, RCD_ELEM_F32 = 3 } rcd_elem;
 
 /* Root-mean-square norm of every row, in fp32:
@@ -471,6 +471,77 @@ typedef struct {
 RCD_API rcd_status rcd_linear_backward_workspace_bytes(rcd_ctx *ctx, const rcd_linear_back_args *args, size_t *bytes_out);
 RCD_API rcd_status rcd_linear_backward(rcd_ctx *ctx, const rcd_linear_back_args *args, void *workspace_dev, size_t workspace_bytes,
                                        void *cuda_stream);
+
+/* ---- training a head or a projection (no counterpart in the paper: its training is decentralized SGD) ------------------- */
+
+/* Softmax cross entropy of a linear head on the samples' labels, without its logits in memory:  z = x w^T + bias,
+ *   lse = log(sum over the classes of exp(z)),  loss = lse - z[label];  a row with a negative label is passed over (loss 0, lse as any other).
+ * A label of n or more: loss NaN, and rcd_sync_status returns RCD_ERR_INVALID_ARG.  Classes are closed by a bias of -infinity: they add nothing, and
+ * a label among them has an infinite loss; where none is open lse is -infinity and loss NaN.  Products as rcd_linear's for an fp32 y; sums of
+ * exponentials in fp32. */
+typedef struct {
+    int64_t rows, n, k;                 /* n classes (from 1); each at most 2^30, and 2^28 tiles of 128 x 64 logits */
+    rcd_elem type;                      /* BF16 or F16: of x and w */
+    const void *x_dev;                  /* [rows][k] */
+    int64_t ldx;
+    const void *w_dev;                  /* [n][k] */
+    int64_t ldw;
+    const float *bias_dev_or_null;      /* [n] */
+    const int32_t *labels_dev;          /* [rows] */
+    float *loss_dev;                    /* out [rows] */
+    float *lse_dev_or_null;             /* out [rows]: what the backward pass reads */
+} rcd_cross_entropy_args;
+RCD_API rcd_status rcd_linear_cross_entropy_workspace_bytes(rcd_ctx *ctx, const rcd_cross_entropy_args *args, size_t *bytes_out);
+RCD_API rcd_status rcd_linear_cross_entropy(rcd_ctx *ctx, const rcd_cross_entropy_args *args, void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
+
+/* Its gradients, from those of loss and lse; the logits are made again, a piece of the classes at a time:
+ *   p = exp(z - lse),  dz = (dloss + dlse) p, less dloss in the label's column;  dx = dz w,  dw = dz^T x,  dbias = sum over the rows of dz.
+ * dloss counts as 0 where the label is negative (or n or more: RCD_ERR_INVALID_ARG from rcd_sync_status); p is 0 where lse is -infinity, and dz where dloss
+ * and dlse are 0.  (x of such rows has to be finite all the same: dw multiplies it by 0.)  dz is rounded to `type` for the products, as a
+ * tensor-core operand has to be (fp16: times a power of two by the largest dloss + dlse, so that 2^-38 of that is still held); dbias takes it unrounded.
+ * Workspace: dz of a piece, and where there are several dx in fp32. */
+typedef struct {
+    int64_t rows, n, k;
+    rcd_elem type;                      /* BF16 or F16: of x, w and dx */
+    const void *x_dev;                  /* [rows][k] */
+    int64_t ldx;
+    const void *w_dev;                  /* [n][k] */
+    int64_t ldw;
+    const float *bias_dev_or_null;      /* [n] */
+    const int32_t *labels_dev;          /* [rows] */
+    const float *lse_dev;               /* [rows], as rcd_linear_cross_entropy wrote it */
+    const float *dloss_dev_or_null;     /* [rows]; null: ones */
+    const float *dlse_dev_or_null;      /* [rows]; null: zeros */
+    int64_t piece;                      /* classes in a piece (rounded down to a multiple of 64); 0: as many as take 512 MB of dz */
+    void *dx_dev_or_null;               /* out [rows][k] */
+    int64_t ld_dx;
+    rcd_elem dw_type;                   /* `type`, or F32 */
+    void *dw_dev_or_null;               /* out [n][k] */
+    int64_t ld_dw;
+    float *dbias_dev_or_null;           /* out [n] */
+} rcd_cross_entropy_back_args;
+RCD_API rcd_status rcd_linear_cross_entropy_backward_workspace_bytes(rcd_ctx *ctx, const rcd_cross_entropy_back_args *args, size_t *bytes_out);
+RCD_API rcd_status rcd_linear_cross_entropy_backward(rcd_ctx *ctx, const rcd_cross_entropy_back_args *args, void *workspace_dev, size_t workspace_bytes,
+                                                     void *cuda_stream);
+
+/* A weight's gradient (dw of rcd_linear_backward) on its way to the update, its singular values brought near one by Newton-Schulz products:
+ *   X = G / (|G| + eps), |G| the Frobenius norm;  for every step, with its coefficients a, b, c:  A = X X^T,  X = a X + (b A + c A A) X.
+ * (3.4445, -4.7750, 2.0315, five times, bring singular values from 0.005 of |G| on to between 0.65 and 1.25.)  Of a batch every matrix is taken by
+ * itself.  X, A and b A + c A A stand between the products as fp16 times 2^10: the result is within 1e-3 to 5e-3 of its norm (small singular values
+ * carry more of the roundings), and coefficients that bring an entry of them to 63 lose it to infinity.  A G of zeros stays one; one with an infinity or a NaN becomes NaN. */
+typedef struct {
+    int64_t batch, rows, cols;          /* up to 65535 matrices of up to 65536 x 65536 */
+    rcd_elem type;                      /* BF16, F16 or F32: of g */
+    const void *g_dev;                  /* [batch][rows][cols] */
+    int64_t ld_g, step_g;               /* elements from row to row and from matrix to matrix */
+    int32_t steps;                      /* from 1 to 64 */
+    const float *coefficients_host;     /* [steps][3], read during the call */
+    float eps;                          /* >= 0 */
+    void *o_dev;                        /* out [batch][rows][cols], bf16 */
+    int64_t ld_o, step_o;
+} rcd_orthogonalize_args;
+RCD_API rcd_status rcd_orthogonalize_workspace_bytes(rcd_ctx *ctx, const rcd_orthogonalize_args *args, size_t *bytes_out);
+RCD_API rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_args *args, void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
 
 /* ---- yardsticks (measurement only; no counterpart in the paper) ------------------------------ */
 

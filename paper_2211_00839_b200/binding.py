@@ -7,7 +7,8 @@ fallback of any kind.
 
 The functions keep the names of the C entry points (``rcd_similarity``,
 ``rcd_partition``, ``rcd_partition_host``, ``rcd_objective``, ``rcd_quotas``,
-``rcd_rms_norm``, ``rcd_linear`` and their ``_backward``, ...);
+``rcd_rms_norm``, ``rcd_linear``, ``rcd_linear_cross_entropy`` and their ``_backward``,
+``rcd_orthogonalize``, ...);
 ``Context`` wraps ``rcd_create`` / ``rcd_destroy``.
 """
 from __future__ import annotations
@@ -34,6 +35,8 @@ RCD_ELEM_I8, RCD_ELEM_BF16, RCD_ELEM_F16, RCD_ELEM_F32 = range(4)
 RCD_ACT_NONE, RCD_ACT_RELU, RCD_ACT_GELU, RCD_ACT_GELU_TANH, RCD_ACT_SILU = range(5)
 # int8 features made by `normalize`: rows of root mean square 1 on a scale that cuts them off at four times that
 RCD_FEATURE_SCALE = 4.0 / 127.0
+# a, b, c of a Newton-Schulz step that brings small singular values up fast and leaves them between 0.65 and 1.25
+RCD_QUINTIC = (3.4445, -4.7750, 2.0315)
 
 STATUS_NAMES = {0: "RCD_OK", 1: "RCD_ERR_INVALID_ARG", 2: "RCD_ERR_UNSUPPORTED", 3: "RCD_ERR_WORKSPACE_TOO_SMALL",
                 4: "RCD_ERR_CUDA", 5: "RCD_ERR_TIMEOUT", 6: "RCD_ERR_INTERNAL"}
@@ -47,6 +50,8 @@ EXPORTS = ["rcd_create", "rcd_destroy", "rcd_last_error", "rcd_version", "rcd_sy
            "rcd_worker_lists_workspace_bytes", "rcd_worker_lists", "rcd_batch_sizes", "rcd_batch_sizes_rule",
            "rcd_rms_norm", "rcd_quantize_rows", "rcd_rms_norm_backward_workspace_bytes", "rcd_rms_norm_backward",
            "rcd_linear_workspace_bytes", "rcd_linear", "rcd_linear_backward_workspace_bytes", "rcd_linear_backward",
+           "rcd_linear_cross_entropy_workspace_bytes", "rcd_linear_cross_entropy", "rcd_linear_cross_entropy_backward_workspace_bytes",
+           "rcd_linear_cross_entropy_backward", "rcd_orthogonalize_workspace_bytes", "rcd_orthogonalize",
            "rcd_yardstick_read", "rcd_yardstick_mma"]
 
 
@@ -103,6 +108,24 @@ class RcdLinearBackArgs(C.Structure):
                 ("dw", C.c_void_p), ("ld_dw", C.c_int64), ("dbias", C.c_void_p)]
 
 
+class RcdCrossEntropyArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("type", C.c_int), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("w", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p), ("labels", C.c_void_p), ("loss", C.c_void_p), ("lse", C.c_void_p)]
+
+
+class RcdCrossEntropyBackArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("type", C.c_int), ("x", C.c_void_p), ("ldx", C.c_int64),
+                ("w", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p), ("labels", C.c_void_p), ("lse", C.c_void_p), ("dloss", C.c_void_p),
+                ("dlse", C.c_void_p), ("piece", C.c_int64), ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dw_type", C.c_int), ("dw", C.c_void_p),
+                ("ld_dw", C.c_int64), ("dbias", C.c_void_p)]
+
+
+class RcdOrthogonalizeArgs(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64), ("type", C.c_int), ("g", C.c_void_p), ("ld_g", C.c_int64),
+                ("step_g", C.c_int64), ("steps", C.c_int32), ("coefficients_host", C.c_void_p), ("eps", C.c_float), ("o", C.c_void_p),
+                ("ld_o", C.c_int64), ("step_o", C.c_int64)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError("%s is missing: build it with `python -m paper_2211_00839_b200.build` "
@@ -142,6 +165,12 @@ def _load() -> C.CDLL:
     lib.rcd_linear.argtypes = [vp, C.POINTER(RcdLinearArgs), vp, sz, vp]
     lib.rcd_linear_backward_workspace_bytes.argtypes = [vp, C.POINTER(RcdLinearBackArgs), C.POINTER(sz)]
     lib.rcd_linear_backward.argtypes = [vp, C.POINTER(RcdLinearBackArgs), vp, sz, vp]
+    lib.rcd_linear_cross_entropy_workspace_bytes.argtypes = [vp, C.POINTER(RcdCrossEntropyArgs), C.POINTER(sz)]
+    lib.rcd_linear_cross_entropy.argtypes = [vp, C.POINTER(RcdCrossEntropyArgs), vp, sz, vp]
+    lib.rcd_linear_cross_entropy_backward_workspace_bytes.argtypes = [vp, C.POINTER(RcdCrossEntropyBackArgs), C.POINTER(sz)]
+    lib.rcd_linear_cross_entropy_backward.argtypes = [vp, C.POINTER(RcdCrossEntropyBackArgs), vp, sz, vp]
+    lib.rcd_orthogonalize_workspace_bytes.argtypes = [vp, C.POINTER(RcdOrthogonalizeArgs), C.POINTER(sz)]
+    lib.rcd_orthogonalize.argtypes = [vp, C.POINTER(RcdOrthogonalizeArgs), vp, sz, vp]
     lib.rcd_yardstick_read.argtypes = [vp, vp, sz, i32, vp]
     lib.rcd_yardstick_mma.argtypes = [vp, C.c_int, i32, C.POINTER(C.c_double), vp]
     for name in EXPORTS:
@@ -684,6 +713,140 @@ class Context:
         return dx, dw, db
 
 
+    # -- training a head or a projection.  (Not recorded by autograd either.)
+    def _per_row(self, t, name: str, shape, dtype):
+        """One value for every row of x: a tensor of x's leading dimensions, dense."""
+        if t.device != self.torch_device:
+            raise ValueError("%s is on %s, the context on %s" % (name, t.device, self.torch_device))
+        if t.dtype != dtype:
+            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+        return t.contiguous()
+
+    def rcd_linear_cross_entropy(self, x, w, labels, bias=None):
+        """Softmax cross entropy of the head x w^T + bias on the samples' labels, without its logits in memory: (loss, lse), float32 of the rows' shape.
+
+        x [..., k] and w [n, k] in bfloat16 or float16, labels [...] int32 (a negative one: the row is passed over), bias [n] float32 (-inf closes
+        a class).  lse is the log of the sum of exponentials, which ``rcd_linear_cross_entropy_backward`` reads.  Autograd does not record the call."""
+        torch = _torch()
+        a = RcdCrossEntropyArgs()
+        xk, rows, k, a.ldx = self._rows(x, "x")
+        if w.dim() != 2:
+            raise ValueError("w must be [n, k]")
+        wk, n, _, a.ldw = self._rows(w, "w", k, None, x.dtype)
+        a.rows, a.n, a.k, a.type, a.x, a.w = rows, n, k, _elem(x.dtype, "x"), xk.data_ptr(), wk.data_ptr()
+        shape = x.shape[:-1]
+        lk = self._per_row(labels, "labels", shape, torch.int32)
+        a.labels = lk.data_ptr()
+        keep = [xk, wk, lk]
+        if bias is not None:
+            b = self._vector(bias, "bias", n, torch.float32)
+            a.bias = b.data_ptr()
+            keep.append(b)
+        loss = torch.empty(shape, dtype=torch.float32, device=self.torch_device)
+        lse = torch.empty(shape, dtype=torch.float32, device=self.torch_device)
+        a.loss, a.lse = loss.data_ptr(), lse.data_ptr()
+        need = C.c_size_t()
+        self._check(lib.rcd_linear_cross_entropy_workspace_bytes(self._h, C.byref(a), C.byref(need)))
+        ws = self._scratch(need.value)
+        self._check(lib.rcd_linear_cross_entropy(self._h, C.byref(a), ws.data_ptr() if ws is not None else None, need.value, self._stream()))
+        return loss, lse
+
+    def rcd_linear_cross_entropy_backward(self, x, w, labels, lse, bias=None, dloss=None, dlse=None, dw_dtype=None, want_dx: bool = True,
+                                          want_dw: bool = True, want_dbias: bool = True, piece: int = 0):
+        """Gradients of ``rcd_linear_cross_entropy`` from those of loss and lse ([...] float32; None: ones, zeros): (dx [..., k], dw [n, k],
+        dbias [n] float32), None where not wanted.  lse: what the forward call returned for the same x, w and bias.
+
+        The logits are made again, ``piece`` classes at a time (0: as many as take 512 MB of workspace).  ``dw_dtype``: default x's type, or float32."""
+        torch = _torch()
+        a = RcdCrossEntropyBackArgs()
+        xk, rows, k, a.ldx = self._rows(x, "x")
+        if w.dim() != 2:
+            raise ValueError("w must be [n, k]")
+        wk, n, _, a.ldw = self._rows(w, "w", k, None, x.dtype)
+        a.rows, a.n, a.k, a.type, a.x, a.w, a.piece = rows, n, k, _elem(x.dtype, "x"), xk.data_ptr(), wk.data_ptr(), piece
+        shape = x.shape[:-1]
+        lk, sk = self._per_row(labels, "labels", shape, torch.int32), self._per_row(lse, "lse", shape, torch.float32)
+        a.labels, a.lse = lk.data_ptr(), sk.data_ptr()
+        keep = [xk, wk, lk, sk]
+        if bias is not None:
+            b = self._vector(bias, "bias", n, torch.float32)
+            a.bias = b.data_ptr()
+            keep.append(b)
+        if dloss is not None:
+            b = self._per_row(dloss, "dloss", shape, torch.float32)
+            a.dloss = b.data_ptr()
+            keep.append(b)
+        if dlse is not None:
+            b = self._per_row(dlse, "dlse", shape, torch.float32)
+            a.dlse = b.data_ptr()
+            keep.append(b)
+        dx = dw = db = None
+        if want_dx:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=self.torch_device)
+            a.dx, a.ld_dx = dx.data_ptr(), k
+        kind = x.dtype if dw_dtype is None else dw_dtype
+        a.dw_type = _elem(kind, "dw_dtype")
+        if want_dw:
+            dw = torch.empty((n, k), dtype=kind, device=self.torch_device)
+            a.dw, a.ld_dw = dw.data_ptr(), k
+        if want_dbias:
+            db = torch.empty(n, dtype=torch.float32, device=self.torch_device)
+            a.dbias = db.data_ptr()
+        need = C.c_size_t()
+        self._check(lib.rcd_linear_cross_entropy_backward_workspace_bytes(self._h, C.byref(a), C.byref(need)))
+        ws = self._scratch(need.value)
+        self._check(lib.rcd_linear_cross_entropy_backward(self._h, C.byref(a), ws.data_ptr() if ws is not None else None, need.value, self._stream()))
+        return dx, dw, db
+
+    def rcd_orthogonalize(self, g, steps: int = 5, coefficients=RCD_QUINTIC, eps: float = 1e-7, out=None):
+        """A weight gradient with its singular values brought near one, bfloat16 of g's shape: g / |g|, then Newton-Schulz steps.
+
+        g [..., rows, cols] in bfloat16, float16 or float32, every matrix by itself (``rcd_linear_backward``'s dw, or several stacked).
+        ``coefficients``: (a, b, c) of every step, or a sequence of ``steps`` such.  ``out`` takes the result in place of a new tensor."""
+        torch = _torch()
+        if g.device != self.torch_device:
+            raise ValueError("g is on %s, the context on %s" % (g.device, self.torch_device))
+        if g.dim() < 2:
+            raise ValueError("g must be [..., rows, cols], got shape %s" % (tuple(g.shape),))
+        c = np.ascontiguousarray(coefficients, dtype=np.float32)
+        if c.shape == (3,):
+            c = np.ascontiguousarray(np.broadcast_to(c, (max(int(steps), 0), 3)))
+        if c.shape != (max(int(steps), 0), 3):
+            raise ValueError("coefficients must be (a, b, c), or %d of them" % steps)
+
+        def matrices(t):
+            """[batch, rows, cols] of it with dense rows, as it lies."""
+            v = t if t.dim() == 3 else t.unsqueeze(0) if t.dim() == 2 else t.flatten(0, -3)
+            s0, s1, s2 = v.stride()
+            rows, cols = v.shape[1:]
+            dense = (cols <= 1 or s2 == 1) and (rows <= 1 or s1 >= cols) and (v.shape[0] <= 1 or s0 >= max(rows - 1, 0) * max(s1, cols) + cols)
+            ld = max(s1, cols) if rows > 1 else cols
+            return v, dense, ld, s0 if v.shape[0] > 1 else rows * ld
+
+        a = RcdOrthogonalizeArgs()
+        v, dense, ld, step = matrices(g)
+        if not dense:
+            v, _, ld, step = matrices(v.contiguous())
+        a.batch, a.rows, a.cols = v.shape
+        a.type, a.g, a.ld_g, a.step_g, a.eps, a.steps = _elem(g.dtype, "g"), v.data_ptr(), ld, step, eps, steps
+        a.coefficients_host = c.ctypes.data
+        if out is None:
+            out = torch.empty(g.shape, dtype=torch.bfloat16, device=self.torch_device)
+        elif out.device != self.torch_device or out.dtype != torch.bfloat16 or out.shape != g.shape:
+            raise ValueError("out must be bfloat16 of shape %s on %s" % (tuple(g.shape), self.torch_device))
+        o, dense, a.ld_o, a.step_o = matrices(out)
+        if not dense or (out.numel() and o.data_ptr() != out.data_ptr()):
+            raise ValueError("out: the elements of a row must lie next to each other, and its matrices equally far apart")
+        a.o = o.data_ptr()
+        need = C.c_size_t()
+        self._check(lib.rcd_orthogonalize_workspace_bytes(self._h, C.byref(a), C.byref(need)))
+        ws = self._scratch(need.value)
+        self._check(lib.rcd_orthogonalize(self._h, C.byref(a), ws.data_ptr() if ws is not None else None, need.value, self._stream()))
+        return out
+
+
 def rcd_worker_lists(ctx: Context, assignment, W: int):
     """assignment [N] int32 on the device -> (offsets [W+1] int64, indices [N] int32): worker j's samples are
     indices[offsets[j]:offsets[j+1]], ascending."""
@@ -763,3 +926,15 @@ def rcd_linear(ctx: Context, x, w, **kw):
 
 def rcd_linear_backward(ctx: Context, dy, x, w, **kw):
     return ctx.rcd_linear_backward(dy, x, w, **kw)
+
+
+def rcd_linear_cross_entropy(ctx: Context, x, w, labels, **kw):
+    return ctx.rcd_linear_cross_entropy(x, w, labels, **kw)
+
+
+def rcd_linear_cross_entropy_backward(ctx: Context, x, w, labels, lse, **kw):
+    return ctx.rcd_linear_cross_entropy_backward(x, w, labels, lse, **kw)
+
+
+def rcd_orthogonalize(ctx: Context, g, **kw):
+    return ctx.rcd_orthogonalize(g, **kw)

@@ -267,8 +267,8 @@ struct rcd_ctx {
     int32_t *statusOwn = nullptr;       // device status word for calls that take no workspace; from kFirstTicket on, tile tickets
     int32_t histTurn = 0;               // histograms of few numbers so far
     unsigned simReady = 0;              // tensor-core similarity kernels whose shared memory has been asked for, a bit each
-    unsigned productReady = 0;          // the same of rcd_linear's kernels
-    alignas(16) unsigned char productPlans[2048] = {};   // how rcd_linear goes about the last few sizes
+    uint64_t productReady = 0;          // the same of rcd_linear's kernels
+    alignas(16) unsigned char productPlans[4096] = {};   // how rcd_linear goes about the last few sizes
     unsigned simTurn = 0;               // similarity launches so far: each takes the next ticket
     size_t hostStageInts = 0;
     unsigned char *hostBlob = nullptr;  // pinned, what a call's host side hands to its kernels

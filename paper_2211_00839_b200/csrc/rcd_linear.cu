@@ -83,42 +83,9 @@ __global__ void __launch_bounds__(1024) column_sums_kernel(const float *__restri
     if (lane == 0 && (int64_t)blockIdx.x * 32 + warp < d) out[(int64_t)blockIdx.x * 32 + warp] = s;
 }
 
-rcd_status check_sizes(rcd_ctx *ctx, int64_t rows, int64_t n, int64_t k)
-{
-    constexpr int64_t most = 1LL << 30;
-    if (rows < 0 || rows > most || n < 0 || n > most) return fail(ctx, RCD_ERR_INVALID_ARG, "rows=%lld or n=%lld out of range", (long long)rows, (long long)n);
-    if (k <= 0 || k > most) return fail(ctx, RCD_ERR_INVALID_ARG, "k=%lld must be from 1 to 2^30", (long long)k);
-    return RCD_OK;
-}
 rcd_status check_act(rcd_ctx *ctx, rcd_activation act)
 {
     if (act < RCD_ACT_NONE || act > RCD_ACT_SILU) return fail(ctx, RCD_ERR_INVALID_ARG, "unknown activation %d", (int)act);
-    return RCD_OK;
-}
-rcd_status check_floats(rcd_ctx *ctx, const char *name, const float *p)
-{
-    if (((uintptr_t)p) % 4) return fail(ctx, RCD_ERR_INVALID_ARG, "%s is not aligned to its type", name);
-    return RCD_OK;
-}
-
-// A rectangle of memory that a call reads or writes.
-struct Area { const void *p; int64_t rows, ld, len, bytes; };
-bool meet(const Area &a, const Area &b) { return ranges_meet(a.p, a.rows, a.ld, a.len, a.bytes, b.p, b.rows, b.ld, b.len, b.bytes); }
-rcd_status check_apart(rcd_ctx *ctx, const Area *out, int outs, const Area *in, int ins)
-{
-    for (int i = 0; i < outs; ++i) {
-        for (int j = 0; j < ins; ++j)
-            if (meet(out[i], in[j])) return fail(ctx, RCD_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
-        for (int j = 0; j < i; ++j)
-            if (meet(out[i], out[j])) return fail(ctx, RCD_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
-    }
-    return RCD_OK;
-}
-rcd_status check_workspace(rcd_ctx *ctx, const void *ws, size_t have, size_t need)
-{
-    if (need == 0) return RCD_OK;
-    if (!ws || have < need) return fail(ctx, RCD_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws ? have : 0, need);
-    if (((uintptr_t)ws) % kAlign) return fail(ctx, RCD_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     return RCD_OK;
 }
 
@@ -206,6 +173,38 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_linear_back_args &a, unsigned char *b
 }
 
 }  // namespace
+
+rcd_status check_sizes(rcd_ctx *ctx, int64_t rows, int64_t n, int64_t k)
+{
+    constexpr int64_t most = 1LL << 30;
+    if (rows < 0 || rows > most || n < 0 || n > most) return fail(ctx, RCD_ERR_INVALID_ARG, "rows=%lld or n=%lld out of range", (long long)rows, (long long)n);
+    if (k <= 0 || k > most) return fail(ctx, RCD_ERR_INVALID_ARG, "k=%lld must be from 1 to 2^30", (long long)k);
+    return RCD_OK;
+}
+rcd_status check_floats(rcd_ctx *ctx, const char *name, const float *p)
+{
+    if (((uintptr_t)p) % 4) return fail(ctx, RCD_ERR_INVALID_ARG, "%s is not aligned to its type", name);
+    return RCD_OK;
+}
+
+static bool meet(const Area &a, const Area &b) { return ranges_meet(a.p, a.rows, a.ld, a.len, a.bytes, b.p, b.rows, b.ld, b.len, b.bytes); }
+rcd_status check_apart(rcd_ctx *ctx, const Area *out, int outs, const Area *in, int ins)
+{
+    for (int i = 0; i < outs; ++i) {
+        for (int j = 0; j < ins; ++j)
+            if (meet(out[i], in[j])) return fail(ctx, RCD_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
+        for (int j = 0; j < i; ++j)
+            if (meet(out[i], out[j])) return fail(ctx, RCD_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
+    }
+    return RCD_OK;
+}
+rcd_status check_workspace(rcd_ctx *ctx, const void *ws, size_t have, size_t need)
+{
+    if (need == 0) return RCD_OK;
+    if (!ws || have < need) return fail(ctx, RCD_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws ? have : 0, need);
+    if (((uintptr_t)ws) % kAlign) return fail(ctx, RCD_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    return RCD_OK;
+}
 
 rcd_status check_rows(rcd_ctx *ctx, const char *name, const void *p, int64_t rows, int64_t ld, int64_t len, rcd_elem type)
 {

@@ -9,6 +9,11 @@ namespace rcd {
 
 #define RCD_TRY(call) do { const rcd_status rs__ = (call); if (rs__ != RCD_OK) return rs__; } while (0)
 
+// How a product ends.  kPlain: rcd_linear's epilogue, or partial sums as they are.  kLoss: every row's logits of a tile to a
+// reference and a sum of exponentials; nothing else leaves the SM.  kLogitGrads: logits to their gradients.  kScaled: alpha times the product
+// plus beta times the residual, symmetric ones from their lower half; a batch of matrices.
+enum Form { kPlain, kLoss, kLogitGrads, kScaled };
+
 // What is done with an accumulator on its way out: z = acc [* xs[m] * ws[n]] + bias[n], y = act(z) + residual.
 struct Epilogue {
     const float *xs, *ws, *bias;
@@ -19,6 +24,24 @@ struct Epilogue {
     int32_t act;
 };
 
+// The head whose logits a product makes (rcd_head.cu).
+struct Head {
+    const int32_t *labels;                 // [rows]
+    int32_t classes, firstClass;           // of all pieces; the class that column 0 is
+    float2 *parts;                         // out [2 tile columns][rows]: reference and sum of exponentials of half a tile's columns
+    float *picked;                         // out [rows]: the label's logit
+    const float *lse, *dloss, *dlse;       // [rows]; null: ones, zeros
+    const float *up;                       // a power of two that the gradients are multiplied by; null: 1
+    float *sums;                           // out [32-row groups][n], or null: columns of the gradients, not multiplied by it
+};
+// alpha * factor^alphaPower times the product plus beta * factor^betaPower times the residual; powers from 0 to 2.
+struct Scaling {
+    float alpha, beta;
+    const float *factor;                   // one for every matrix of the batch, or null: 1
+    int32_t alphaPower, betaPower;
+    rcd_elem residualType;
+};
+
 // C[m][n] = sum over k of A(m, k) B(n, k).  An operand has its k elements next to each other (rows lie `ld` apart), or, with
 // `across`, its m or n elements (and steps of k are `ld` apart).
 struct Operand { const void *p; int64_t ld; bool across; };
@@ -27,9 +50,20 @@ struct Product {
     int64_t M, N, K;
     Operand a, b;
     Epilogue out;
+    Form form;                             // kPlain where nothing is said
+    Head head;
+    Scaling scaling;
+    bool symmetric;                        // kScaled: the output is, and M is N; both halves of it are written
+    int64_t batch;                         // kScaled: matrices (0: one), whose rows lie below one another, in every argument this many apart:
+    int64_t aStep, bStep, yStep, rStep;
 };
+struct KernelChoice { const void *kernel; int bit; };          // bit: of rcd_ctx::productReady
+KernelChoice head_kernel(Form form, int wide, bool pair);
+KernelChoice scaled_kernel(int order, int wide, bool pair);
+constexpr int kPlainKernels = 20, kHeadKernels = 8;            // (and 18 scaled ones)
 
 size_t product_workspace(rcd_ctx *ctx, const Product &p);
+int64_t product_tile_columns(rcd_ctx *ctx, const Product &p);          // kLoss: of what parts holds
 rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaStream_t st);
 
 // The product of few rows (rcd_linear_few.cu; no workspace), and whether it takes one.
@@ -47,6 +81,12 @@ inline void begin_operator(rcd_ctx *ctx)
     ctx->statusDev = ctx->statusOwn + kOperatorStatus;
 }
 
+// Checks of arguments.  An area: a rectangle of memory that a call reads or writes.
+struct Area { const void *p; int64_t rows, ld, len, bytes; };
+rcd_status check_apart(rcd_ctx *ctx, const Area *out, int outs, const Area *in, int ins);
+rcd_status check_sizes(rcd_ctx *ctx, int64_t rows, int64_t n, int64_t k);
+rcd_status check_floats(rcd_ctx *ctx, const char *name, const float *p);
+rcd_status check_workspace(rcd_ctx *ctx, const void *ws, size_t have, size_t need);
 rcd_status check_rows(rcd_ctx *ctx, const char *name, const void *p, int64_t rows, int64_t ld, int64_t len, rcd_elem type);
 
 }  // namespace rcd

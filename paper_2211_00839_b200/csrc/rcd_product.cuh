@@ -1,0 +1,752 @@
+// The product on the tensor cores that rcd_linear, the loss of a head and the orthogonalised update share:  C = A B^T, finished in one of four
+// forms (see Form).
+//
+// Persistent CTAs (one per SM), or pairs of CTAs on one tile (cta_group::2: each holds half of A's rows and half of B's, so an
+// operand row comes in once for 256 rows of the other).  Operand tiles come by TMA in slabs of 128 bytes of k (64 elements of
+// 16 bits, 128 of 8) with the 128-byte swizzle into a ring; an operand whose m or n elements lie next to each other instead of its k
+// elements (`across`: the gradients' transposed factors) comes in boxes of 64 such elements by 64 k and is multiplied as it lies
+// (the instruction takes either order).  One thread issues tcgen05.mma into one of two 256-column accumulators in tensor
+// memory, so that eight warps finish a tile while the next one is computed: 32 columns at a time from tensor memory, times the scales,
+// plus bias, activation, plus residual, rounded into 32 rows x 128 bytes of shared memory, and out by TMA.  The residual's piece
+// comes in by TMA into the same place one piece ahead.  Rows that a tensor map cannot describe (they do not start on 16 bytes)
+// are first copied (operands), or moved between that place and memory by the warp itself (outputs, residual); so are the ends of output
+// rows that do not end on 16 bytes: a TMA store writes the last 16 bytes that an element of the row lies in whole.
+//
+// Warp roles: 0 = TMA producer, 1 = TMEM allocation + MMA issue, 2..9 = epilogue, two per quarter of the TMEM lanes.
+// Every wait is bounded, as in the similarity kernel: on expiry the CTA records kDevTimeout and leaves.
+#pragma once
+
+#include "rcd_act.cuh"
+#include "rcd_linear.h"
+#include "rcd_tc.cuh"
+#include "rcd_walk.h"
+
+namespace rcd {
+
+constexpr int kRows = 128;                              // rows of A per CTA
+constexpr int kSlab = 128;                              // bytes of k per operand row and stage
+constexpr int kSlabRows16 = 64;                         // k elements of 16 bits per slab
+constexpr int kBox = 64 * kSlab;                        // 8 KB: 64 k rows of 64 elements
+constexpr int kABytes = kRows * kSlab;
+constexpr int kMostStages = 8;
+constexpr int kEpiWarps = 8;
+// The tensor cores cut an fp32 sum off where they cannot hold it, towards zero: products of fp16 and of one sign lose 6.5e-9 of the result
+// each, 3.2e-4 over 50 000 (two thirds of the type's half step).  So sums are taken in chunks that are added up outside with rounding.
+// fp32 outputs: 512 k (2.4e-6 within a chunk, bf16 2.3e-7, and half a unit of fp32 at most for each of them).  16-bit outputs: 2048 k (1.3e-5)
+// where a piece has more than 4096, up to which the loss is a twentieth of fp16's half step.  (Gradients of 2048 x 2048 weights over 600 000
+// rows: 3.56 ms in chunks, 3.45 in one sum.)
+constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kPiece = 32 * 128;                        // an epilogue warp's piece of the output: 32 rows of 128 bytes
+constexpr int kStaging = kEpiWarps * 2 * kPiece;
+constexpr int kColumnBytes = kEpiWarps * 2 * 32 * 4;    // 32 biases and 32 scales per warp
+constexpr uint32_t kWaitTurns = 1u << 16;               // of at most 20 us: a second or so
+constexpr int kMostShared = 227 * 1024;
+
+struct __align__(8) ProductShared {
+    uint64_t full[kMostStages], empty[kMostStages];     // full: CTA 0's of a pair
+    uint64_t accFull[2], accEmpty[2];                   // accEmpty: CTA 0's of a pair
+    uint64_t residual[kEpiWarps][2];
+    uint32_t tmemBase;
+    int32_t abort;
+};
+constexpr int kFixedShared = kStaging + kColumnBytes + (int)sizeof(ProductShared);
+
+struct TcParams {
+    int32_t M, N, units, slabs, slabsPerSplit, chunk, tn, stages, stageBytes, rowsPart;
+    uint32_t idesc;
+    Walk walk;
+    int32_t aStep, bStep, yStep, rStep;                        // rows from one matrix of a batch to the next (rows of k, where an operand is across)
+    Epilogue e;
+    Head head;
+    Scaling s;
+    bool raw;                                           // accumulators as they are, into e.y: [split][rowsPart][ldy]
+    bool tmaY, tmaZ, tmaR, edgeByHand;                  // edgeByHand: a piece that holds the rows' ends, since TMA stores 16 bytes at a time
+    int32_t *status;
+};
+
+// (Suspended by the hardware up to 20 us at a time: polls with pauses cost the ring half a slab's time at every turn.)
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, ProductShared *sh, uint32_t turns = kWaitTurns)
+{
+    for (uint32_t turn = 0; turn < turns; ++turn) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity), "r"(20000) : "memory");
+        if (ok) return true;
+        if (*(volatile int32_t *)&sh->abort) return false;
+    }
+    atomicExch(&sh->abort, 1);
+    return false;
+}
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t mine;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(mine));
+    return mine != 0;
+}
+// wait_for a whole warp, which goes on together or gives up together.
+__device__ __forceinline__ bool warp_wait_for(uint64_t *bar, uint32_t parity, ProductShared *sh, uint32_t turns = kWaitTurns)
+{
+    return __all_sync(0xffffffffu, wait_for(bar, parity, sh, turns));
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, const void *src, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                 :: "l"(map), "r"(smem_addr(src)), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" :: "n"(kLeft) : "memory"); }
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Descriptor of an operand whose m (n) elements lie next to each other: boxes of 64 of them (128 bytes) by 64 k, 8 KB apart; groups of 8 k
+// are 1024 bytes apart.
+__device__ __forceinline__ uint64_t across_desc(uint32_t addr)
+{
+    uint64_t d = make_smem_desc(addr) & ~((uint64_t)0x3fff << 16);
+    return d | (uint64_t)(kBox >> 4) << 16;
+}
+
+// Byte of (row, 16-byte chunk) in a piece, as the 128-byte swizzle places it.
+__device__ __forceinline__ int piece_at(int row, int chunk) { return row * 128 + ((chunk ^ (row & 7)) << 4); }
+
+// A piece between its place in shared memory and rows that TMA cannot reach: element by element, neighbours by neighbouring lanes.
+template <bool kLoad, typename T>
+__device__ __forceinline__ void move_piece(unsigned char *piece, T *at, int64_t ld, int rows, int cols)
+{
+    constexpr int kCols = 128 / sizeof(T);
+    const int lane = threadIdx.x & 31;
+    rows = min(rows, 32);
+    // (eight rows' accesses under way at once)
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        T v[8][kCols / 32];
+        auto each = [&](auto go) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    const int row = r0 + r, col = c * 32 + lane;
+                    if (row < rows && col < cols) go(v[r][c], *reinterpret_cast<T *>(piece + piece_at(row, col * (int)sizeof(T) / 16) + col * (int)sizeof(T) % 16), at[(int64_t)row * ld + col]);
+                }
+        };
+        if constexpr (kLoad) {
+            each([](T &x, T &, T &there) { x = there; });
+            each([](T &x, T &here, T &) { here = x; });
+        } else {
+            each([](T &x, T &here, T &) { x = here; });
+            each([](T &x, T &, T &there) { there = x; });
+        }
+    }
+}
+
+// 32 fp32 values to one row's 64 or 128 bytes of a piece, from 16-byte chunk `chunk` on.
+__device__ __forceinline__ uint32_t pack2(float a, float b, rcd_elem type)
+{
+    if (type == RCD_ELEM_BF16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float2 unpack2(uint32_t x, rcd_elem type)
+{
+    if (type == RCD_ELEM_BF16) return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2 *>(&x));
+}
+__device__ __forceinline__ void put_row(unsigned char *piece, int row, int chunk, const float (&v)[32], rcd_elem type)
+{
+    if (type == RCD_ELEM_F32) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+            *reinterpret_cast<float4 *>(piece + piece_at(row, c)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint4 *>(piece + piece_at(row, chunk + c)) =
+                make_uint4(pack2(v[8 * c], v[8 * c + 1], type), pack2(v[8 * c + 2], v[8 * c + 3], type), pack2(v[8 * c + 4], v[8 * c + 5], type),
+                           pack2(v[8 * c + 6], v[8 * c + 7], type));
+    }
+}
+// v += factor * row (factor 1: the sum itself, rounded once)
+__device__ __forceinline__ void add_row(const unsigned char *piece, int row, int chunk, float (&v)[32], rcd_elem type, float factor)
+{
+    if (type == RCD_ELEM_F32) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const float4 x = *reinterpret_cast<const float4 *>(piece + piece_at(row, c));
+            v[4 * c] = fmaf(factor, x.x, v[4 * c]);
+            v[4 * c + 1] = fmaf(factor, x.y, v[4 * c + 1]);
+            v[4 * c + 2] = fmaf(factor, x.z, v[4 * c + 2]);
+            v[4 * c + 3] = fmaf(factor, x.w, v[4 * c + 3]);
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(piece + piece_at(row, chunk + c));
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = unpack2(w[i], type);
+                v[8 * c + 2 * i] = fmaf(factor, f.x, v[8 * c + 2 * i]);
+                v[8 * c + 2 * i + 1] = fmaf(factor, f.y, v[8 * c + 2 * i + 1]);
+            }
+        }
+    }
+}
+// The log of a sum of exponentials in pieces: a finite reference `top` and the sum of exp(z - top).  Values of -infinity add nothing and NaN
+// stays; +infinity leaves the largest finite number as the reference and an infinite sum.
+struct SumOfExp { float top, sum; };
+constexpr float kLargest = 3.402823466e38f;
+__device__ __forceinline__ SumOfExp no_terms() { return {-kLargest, 0.0f}; }
+__device__ __forceinline__ void add_terms(SumOfExp &s, const float (&z)[32])
+{
+    float m[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m[j] = fmaxf(fmaxf(z[j], z[j + 8]), fmaxf(z[j + 16], z[j + 24]));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = fmaxf(m[j], m[j + 4]);
+    const float top = fminf(fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), s.top), kLargest);
+    // (the difference first: digits of z that exp(z - top) depends on are still there at large z)
+    const Two less = two(-top, -top), log2e = two(kLog2e, kLog2e);
+    Two sum[4];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const float2 a = parts(mul2(add2(two(z[2 * j], z[2 * j + 1]), less), log2e));
+        const Two e = two(exp2_fast(a.x), exp2_fast(a.y));
+        sum[j & 3] = j < 4 ? e : add2(sum[j & 3], e);
+    }
+    const float2 both = parts(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+    s.sum = fmaf(s.sum, exp2_fast((s.top - top) * kLog2e), both.x + both.y);
+    s.top = top;
+}
+__device__ __forceinline__ void join_terms(SumOfExp &s, const SumOfExp &o)
+{
+    const float top = fmaxf(s.top, o.top);
+    s.sum = s.sum * exp2_fast((s.top - top) * kLog2e) + o.sum * exp2_fast((o.top - top) * kLog2e);
+    s.top = top;
+}
+
+// Sums of 32 columns over the warp's 32 rows, a lane's row in v: lane j ends with column j's.  A lane passes on half of what it holds at
+// every step: 31 exchanges.
+__device__ __forceinline__ float column_sum(float (&v)[32])
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (i < o) {
+                const float mine = upper ? v[i + o] : v[i], other = upper ? v[i] : v[i + o];
+                v[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
+            }
+    }
+    return v[0];
+}
+
+// kChunks: 0, or the columns of a piece of the output, whose sums are taken in chunks.
+template <Form kForm, bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks, bool kPair>
+__device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUtensorMap &mapB, const CUtensorMap &mapY, const CUtensorMap &mapZ, const CUtensorMap &mapR, const TcParams &p)
+{
+    extern __shared__ __align__(1024) unsigned char smem[];
+    unsigned char *const tiles = smem;
+    unsigned char *const staging = smem + (size_t)p.stages * p.stageBytes;
+    float *const columns = reinterpret_cast<float *>(staging + kStaging);
+    ProductShared &sh = *reinterpret_cast<ProductShared *>(staging + kStaging + kColumnBytes);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
+    const int first = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, step = kPair ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kMostStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&sh.accFull[b], 1); mbar_init(&sh.accEmpty[b], (kPair ? 2 : 1) * kEpiWarps); }
+        for (int w = 0; w < kEpiWarps; ++w) { mbar_init(&sh.residual[w][0], 1); mbar_init(&sh.residual[w][1], 1); }
+        sh.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if constexpr (kPair) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_addr(&sh.tmemBase)), "r"(512) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_addr(&sh.tmemBase)), "r"(512) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (kPair) cluster_barrier();              // the other CTA's barriers exist
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmemBase = sh.tmemBase;
+    const int rowsPerTile = kPair ? 2 * kRows : kRows;
+    const int nMine = kPair ? p.tn / 2 : p.tn;           // B's rows that this CTA brings in
+
+    if (warp == 0) {
+        // ---------------- TMA producer ----------------
+        // (The whole warp goes through the loop, one lane issues: addresses stay in uniform registers, which is where these instructions
+        // want them.  With the loop inside one lane's branch a slab took the issuer 600 cycles whatever its size.)
+        const bool leader = elect_one();
+        int s = 0;
+        uint32_t phase = 1;
+        bool ok = true;
+        const int slabElems = kInt8 ? kSlab : kSlab / 2;
+        const uint32_t bytes = (uint32_t)(kPair ? 2 : 1) * (uint32_t)(kABytes + nMine * kSlab);
+        for (int u = first; u < p.units && ok; u += step) {
+            const Unit t = unit_of(p.walk, u);
+            const int m0 = t.m * rowsPerTile + rank * kRows, n0 = t.n * p.tn + rank * nMine;
+            const int aRow = kForm == kScaled ? t.batch * p.aStep : 0, bRow = kForm == kScaled ? t.batch * p.bStep : 0;
+            const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
+            for (int kb = t.split * p.slabsPerSplit; kb < end; ++kb) {
+                if (!warp_wait_for(&sh.empty[s], phase, &sh)) { ok = false; break; }
+                unsigned char *a = tiles + s * p.stageBytes, *b = a + kABytes;
+                if (leader) {
+                    if (rank == 0) mbar_expect_tx(&sh.full[s], bytes);
+                    uint32_t bar = smem_addr(&sh.full[s]);
+                    if constexpr (kPair) bar = leader_addr(&sh.full[s]);
+                    auto load = [&](void *dst, const CUtensorMap *map, int c0, int c1) {
+                        if constexpr (kPair) pair_load_2d(dst, map, c0, c1, bar);
+                        else tma_load_2d(dst, map, c0, c1, &sh.full[s]);
+                    };
+                    if constexpr (kAcrossA) {
+#pragma unroll
+                        for (int j = 0; j < kRows / 64; ++j) load(a + j * kBox, &mapA, m0 + 64 * j, aRow + kb * kSlabRows16);
+                    } else {
+                        load(a, &mapA, kb * slabElems, aRow + m0);
+                    }
+                    if constexpr (kAcrossB) {
+                        for (int j = 0; j < nMine / 64; ++j) load(b + j * kBox, &mapB, n0 + 64 * j, bRow + kb * kSlabRows16);
+                    } else {
+                        load(b, &mapB, kb * slabElems, bRow + n0);
+                    }
+                }
+                __syncwarp();
+                if (++s == p.stages) { s = 0; phase ^= 1; }
+            }
+        }
+        // after an abort: let the copies already issued land (a pair's report to CTA 0, so by time)
+        if (*(volatile int32_t *)&sh.abort) let_copies_land();
+    } else if (warp == 1) {
+        // ---------------- MMA issuer (a pair's first CTA, for both) ----------------
+        if (rank == 0) {
+            const bool leader = elect_one();
+            int s = 0;
+            uint32_t phase = 0, nt = 0;
+            bool ok = true;
+            const uint32_t tile0 = smem_addr(tiles);
+            for (int u = first; u < p.units && ok; u += step) {
+                const Unit t = unit_of(p.walk, u);
+                const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
+                for (int begin = t.split * p.slabsPerSplit; begin < end && ok; begin += p.chunk, ++nt) {
+                    const uint32_t buf = nt & 1;
+                    if (!warp_wait_for(&sh.accEmpty[buf], ((nt >> 1) & 1) ^ 1, &sh)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t tmemD = tmemBase + buf * 256;
+                    const int stop = min(end, begin + p.chunk);
+                    for (int kb = begin; kb < stop; ++kb) {
+                        if (!warp_wait_for(&sh.full[s], phase, &sh)) { ok = false; break; }
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint32_t aAddr = tile0 + (uint32_t)(s * p.stageBytes), bAddr = aAddr + kABytes;
+                        const uint64_t descA = kAcrossA ? across_desc(aAddr) : make_smem_desc(aAddr);
+                        const uint64_t descB = kAcrossB ? across_desc(bAddr) : make_smem_desc(bAddr);
+                        // one MMA takes 32 bytes of k per row, or 16 rows of k of 128 bytes each
+                        constexpr uint64_t kStepA = kAcrossA ? 128 : 2, kStepB = kAcrossB ? 128 : 2;
+                        if (leader) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                if constexpr (kPair) pair_mma<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
+                                else mma_issue<kInt8>(tmemD, descA + kStepA * k, descB + kStepB * k, p.idesc, (kb > begin || k > 0) ? 1u : 0u);
+                            }
+                            if constexpr (kPair) pair_commit(&sh.empty[s]);
+                            else mma_commit(&sh.empty[s]);
+                        }
+                        __syncwarp();
+                        if (++s == p.stages) { s = 0; phase ^= 1; }
+                    }
+                    if (leader) {
+                        if constexpr (kPair) pair_commit(&sh.accFull[buf]);
+                        else mma_commit(&sh.accFull[buf]);
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+    } else {
+        // ---------------- epilogue: this CTA's 128 rows ----------------
+        const int q = warp & 3, ew = warp - 2, half = ew >> 2;       // TMEM lanes 32 q ..; pieces half, half + 2, ...
+        unsigned char *const mine = staging + ew * 2 * kPiece;
+        float *const biases = columns + ew * 64, *const scales = biases + 32;
+        const Epilogue &e = p.e;
+        const int wide = kChunks ? kChunks : e.type == RCD_ELEM_F32 ? 32 : 64;        // columns of a piece
+        const int pieces = p.tn / wide;
+        // a piece's coordinates; false where nothing of it lies inside the output
+        struct Piece { int row, col, base, from; };        // base, from: rows of the output and of the residual before this matrix
+        auto piece_of = [&](int u, int k, Piece *o) {
+            const Unit t = unit_of(p.walk, u);
+            o->row = t.m * rowsPerTile + rank * kRows + q * 32;
+            o->col = t.n * p.tn + k * wide;
+            o->base = kForm == kScaled ? t.batch * p.yStep : 0;
+            o->from = kForm == kScaled ? t.batch * p.rStep : 0;
+            return o->row < p.M && o->col < p.N;
+        };
+        // the residual of the next piece that has one, from (u, k) on, is on its way into buffer `to`
+        auto fetch = [&](int u, int k, int to) {
+            Piece o;
+            for (; u < p.units; u += step, k = half)
+                for (; k < pieces; k += 2)
+                    if (piece_of(u, k, &o)) {
+                        mbar_expect_tx(&sh.residual[ew][to], kPiece);
+                        tma_load_2d(mine + to * kPiece, &mapR, o.col, o.from + o.row, &sh.residual[ew][to]);
+                        return;
+                    }
+        };
+        const bool mirrors = kForm == kScaled && p.walk.subM != 0;
+        const bool alternate = e.z == nullptr && !mirrors;            // two buffers in turn, or one for y and one for z or the transpose
+        uint32_t nt = 0, turn = 0;
+        if (p.tmaR && lane == 0) fetch(first, half, 0);
+        bool ok = true;
+        unsigned char *yPiece = mine;
+        unsigned char *const zPiece = mine + kPiece;
+        // a piece's place in shared memory is free, and the residual lies there
+        auto begin_piece = [&](int u, int k, const Piece &o) {
+            yPiece = mine + (alternate ? (turn & 1) * kPiece : 0);
+            // (what was stored from it has been read out of it; a residual that comes next needs the other place too)
+            if (lane == 0) {
+                if (alternate && !p.tmaR) bulk_wait_read<1>();
+                else bulk_wait_read<0>();
+            }
+            __syncwarp();
+            if (p.tmaR) {
+                if (alternate && lane == 0) fetch(u, k + 2, (turn & 1) ^ 1);
+                // (with z in the other buffer the residual is fetched when the last piece has left)
+                return warp_wait_for(&sh.residual[ew][alternate ? turn & 1 : 0], alternate ? (turn >> 1) & 1 : turn & 1, &sh);
+            }
+            if (e.residual) {
+                const int64_t at = ((int64_t)o.from + o.row) * e.ldr + o.col;
+                if (e.type == RCD_ELEM_F32) move_piece<true>(yPiece, (float *)e.residual + at, e.ldr, p.M - o.row, p.N - o.col);
+                else move_piece<true>(yPiece, (uint16_t *)e.residual + at, e.ldr, p.M - o.row, p.N - o.col);
+                __syncwarp();
+            }
+            return true;
+        };
+        // The biases and scales of the warp's columns of a tile, 32 at a time (up to four times): asked for before the tile is ready, since
+        // memory takes longer to answer than 32 columns take to finish; and those of one time to all lanes.
+        const bool anyColumns = !p.raw && (e.bias || e.ws);
+        float bias4[4], scale4[4];
+        auto ask_columns = [&](const Unit &t) {
+            if (!anyColumns) return;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int col = t.n * p.tn + (wide == 64 ? (half + 2 * (c >> 1)) * 64 + (c & 1) * 32 : (half + 2 * c) * 32) + lane;
+                bias4[c] = e.bias && col < p.N ? e.bias[col] : 0.0f;
+                scale4[c] = e.ws && col < p.N ? e.ws[col] : 1.0f;
+            }
+        };
+        auto columns_of = [&](int c) {
+            if (!anyColumns) return;
+            __syncwarp();
+            biases[lane] = c == 0 ? bias4[0] : c == 1 ? bias4[1] : c == 2 ? bias4[2] : bias4[3];
+            scales[lane] = c == 0 ? scale4[0] : c == 1 ? scale4[1] : c == 2 ? scale4[2] : scale4[3];
+            __syncwarp();
+        };
+        // what the lane's row brings along: asked for before the tile is ready
+        struct Row {
+            float sx;                                                  // int8: its scale
+            int label;                                                 // its class's column in this output
+            float lse, weight, atLabel;                                // kLogitGrads: dz = weight * p, less atLabel in the label's column
+            float alpha, beta;                                         // kScaled
+            bool mirror;
+        };
+        auto ask_row = [&](const Unit &t, int row) {
+            Row r{};
+            r.sx = kInt8 && e.xs && row < p.M ? e.xs[row] : 1.0f;
+            if constexpr (kForm == kLoss || kForm == kLogitGrads) {
+                const Head &hd = p.head;
+                const int label = row < p.M ? hd.labels[row] : -1;
+                const bool valid = label >= 0 && label < hd.classes;
+                r.label = valid ? label - hd.firstClass : -1;          // (another piece's: outside 0..N-1)
+                if constexpr (kForm == kLogitGrads) {
+                    if (label >= hd.classes && t.n == 0) atomicOr(p.status, kDevBadLabel);
+                    const float up = hd.up ? *hd.up : 1.0f;
+                    float lse = 0.0f, g = 0.0f, gl = 0.0f;
+                    if (row < p.M) {
+                        lse = hd.lse[row];
+                        if (valid) g = hd.dloss ? hd.dloss[row] : 1.0f;
+                        if (hd.dlse) gl = hd.dlse[row];
+                    }
+                    r.lse = lse == -INFINITY ? INFINITY : lse;         // (a row without a class that is open: p is 0)
+                    r.weight = (g + gl) * up;
+                    r.atLabel = g * up;
+                }
+            }
+            if constexpr (kForm == kScaled) {
+                const Scaling &sc = p.s;
+                const float f = sc.factor ? sc.factor[t.batch] : 1.0f;
+                auto power = [&](int n) { return n == 0 ? 1.0f : n == 1 ? f : f * f; };
+                r.alpha = sc.alpha * power(sc.alphaPower);
+                r.beta = sc.beta * power(sc.betaPower);
+                r.mirror = t.mirror;
+            }
+            return r;
+        };
+        // 32 columns of the lane's row, from column h of the piece on
+        auto finish = [&](float (&z)[32], const Row &r, int h, const Piece &o) {
+            if (p.raw) {
+                // (as they are)
+            } else if constexpr (kForm == kScaled) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) z[j] *= r.alpha;
+                if (e.residual) add_row(yPiece, lane, h / 8, z, p.s.residualType, r.beta);
+                if (r.mirror) {                                        // (rows of 64 bytes: a lane's row is a column there)
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        const uint32_t two = pack2(z[j], z[j + 1], e.type);
+                        *reinterpret_cast<uint16_t *>(zPiece + (h + j) * 64 + lane * 2) = (uint16_t)two;
+                        *reinterpret_cast<uint16_t *>(zPiece + (h + j + 1) * 64 + lane * 2) = (uint16_t)(two >> 16);
+                    }
+                }
+            } else if constexpr (kForm == kLogitGrads) {
+                if (e.bias) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 b = reinterpret_cast<const float4 *>(biases)[j / 4];
+                        z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
+                    }
+                }
+                const Two less = two(-r.lse, -r.lse), log2e = two(kLog2e, kLog2e), weight = two(r.weight, r.weight);
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                    const float2 a = parts(mul2(add2(two(z[j], z[j + 1]), less), log2e));
+                    const float2 dz = parts(mul2(two(exp2_fast(a.x), exp2_fast(a.y)), weight));
+                    z[j] = dz.x;
+                    z[j + 1] = dz.y;
+                }
+                const int at = r.label - (o.col + h);
+                if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[j] -= at == j ? r.atLabel : 0.0f;
+                }
+                if (r.weight == 0.0f && r.atLabel == 0.0f) {           // (whatever p is: a row that is passed over may hold anything)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[j] = 0.0f;
+                }
+                if (p.head.sums) {
+                    float v[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = z[j];
+                    const float sum = column_sum(v);
+                    if (o.col + h + lane < p.N) p.head.sums[(int64_t)(o.row / 32) * p.N + o.col + h + lane] = p.head.up ? sum / *p.head.up : sum;
+                }
+            } else {
+                if constexpr (kInt8) {
+                    if (e.xs) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] *= r.sx;
+                    }
+                    if (e.ws) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 w = reinterpret_cast<const float4 *>(scales)[j / 4];
+                            z[j] *= w.x; z[j + 1] *= w.y; z[j + 2] *= w.z; z[j + 3] *= w.w;
+                        }
+                    }
+                }
+                if (e.bias) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 b = reinterpret_cast<const float4 *>(biases)[j / 4];
+                        z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
+                    }
+                }
+                if (e.z) put_row(zPiece, lane, h / 8, z, e.type);
+                activate(z, e.act);
+                if (e.residual) add_row(yPiece, lane, h / 8, z, e.type, 1.0f);
+            }
+            put_row(yPiece, lane, h / 8, z, e.type);
+        };
+        auto end_piece = [&](int u, int k, const Piece &o, int rowBase, bool mirror) {
+            // (for the stores that leave from here by TMA, and for the next residual that TMA writes here: either comes after these ordinary writes)
+            if (p.tmaY || p.tmaZ || p.tmaR) proxy_fence();
+            __syncwarp();
+            auto send = [&](bool byTma, const CUtensorMap *map, unsigned char *piece, void *to, int64_t ld, int base) {
+                if (byTma && !(p.edgeByHand && o.col + wide > p.N)) {
+                    if (lane == 0) tma_store_2d(map, piece, o.col, base + o.row);
+                } else if (e.type == RCD_ELEM_F32) {
+                    move_piece<false>(piece, (float *)to + ((int64_t)base + o.row) * ld + o.col, ld, p.M - o.row, p.N - o.col);
+                } else {
+                    move_piece<false>(piece, (uint16_t *)to + ((int64_t)base + o.row) * ld + o.col, ld, p.M - o.row, p.N - o.col);
+                }
+            };
+            send(p.tmaY, &mapY, yPiece, e.y, e.ldy, rowBase + o.base);
+            if (kForm == kScaled) {
+                if (mirror && lane == 0) tma_store_2d(&mapZ, zPiece, o.row, o.base + o.col);
+            } else if (e.z) {
+                send(p.tmaZ, &mapZ, zPiece, e.z, e.ldz, 0);
+            }
+            if (lane == 0) bulk_commit();
+            __syncwarp();
+            if (p.tmaR && !alternate && lane == 0) {
+                bulk_wait_read<0>();
+                fetch(u, k + 2, 0);
+            }
+            ++turn;
+        };
+        // hands an accumulator back
+        auto release = [&](uint32_t buf) {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (kPair) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(leader_addr(&sh.accEmpty[buf])) : "memory");
+                else mbar_arrive(&sh.accEmpty[buf]);
+            }
+        };
+        for (int u = first; u < p.units && ok; u += step) {
+            const Unit t = unit_of(p.walk, u);
+            const int rowBase = p.raw ? t.split * p.rowsPart : 0;
+            const int row = t.m * rowsPerTile + rank * kRows + q * 32 + lane;
+            const Row mineRow = ask_row(t, row);
+            [[maybe_unused]] SumOfExp terms = no_terms();
+            // kLoss: 32 columns join the row's sum, and its label's logit is noted
+            [[maybe_unused]] auto take = [&](float (&z)[32], const Piece &o) {
+                if (e.bias) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 b = reinterpret_cast<const float4 *>(biases)[j / 4];
+                        z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
+                    }
+                }
+                if (o.col + 32 > p.N) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[j] = o.col + j < p.N ? z[j] : -INFINITY;
+                }
+                const int at = mineRow.label - o.col;
+                if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+                    float picked = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) picked = at == j ? z[j] : picked;
+                    if (at >= 0 && at < 32) p.head.picked[row] = picked;
+                }
+                add_terms(terms, z);
+            };
+            const uint32_t lanes = (uint32_t)(q * 32) << 16;
+            ask_columns(t);
+            if constexpr (kChunks != 0) {
+                // Sums of chunks (see kChunkSlabs) in a lane's 128 registers, four times 32 columns; the next chunk is computed meanwhile.
+                float sum[4][32];
+                const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
+                for (int begin = t.split * p.slabsPerSplit; begin < end && ok; begin += p.chunk, ++nt) {
+                    const uint32_t buf = nt & 1;
+                    if (!warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const bool fresh = begin == t.split * p.slabsPerSplit;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int col = wide == 64 ? (half + 2 * (i >> 1)) * 64 + (i & 1) * 32 : (half + 2 * i) * 32;
+                        if (col < p.tn) {
+                            uint32_t v[32];
+                            tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)col, v);
+                            tmem_load_wait();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sum[i][j] = fresh ? __uint_as_float(v[j]) : sum[i][j] + __uint_as_float(v[j]);
+                        }
+                    }
+                    release(buf);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int k = wide == 64 ? half + 2 * (i >> 1) : half + 2 * i, h = wide == 64 ? (i & 1) * 32 : 0;
+                    Piece o;
+                    if (ok && k < pieces && piece_of(u, k, &o)) {
+                        if constexpr (kForm == kLoss) {
+                            columns_of(i);
+                            take(sum[i], o);
+                            continue;
+                        }
+                        if (h == 0) ok = begin_piece(u, k, o);
+                        if (ok) {
+                            columns_of(i);
+                            finish(sum[i], mineRow, h, o);
+                            if (h + 32 == wide) end_piece(u, k, o, rowBase, t.mirror);
+                        }
+                    }
+                }
+            } else {
+                const uint32_t buf = nt & 1;
+                if (!warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int k = half; k < pieces; k += 2) {
+                    Piece o;
+                    if (!piece_of(u, k, &o)) continue;
+                    if constexpr (kForm != kLoss) {
+                        if (!begin_piece(u, k, o)) { ok = false; break; }
+                    }
+                    for (int h = 0; h < wide; h += 32) {
+                        uint32_t v[32];
+                        tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)(k * wide + h), v);
+                        columns_of(wide == 64 ? (k - half) + h / 32 : (k - half) / 2);
+                        tmem_load_wait();
+                        float z[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] = kInt8 && !p.raw ? (float)(int32_t)v[j] : __uint_as_float(v[j]);      // (raw integers stay what they are)
+                        if constexpr (kForm == kLoss) take(z, o);
+                        else finish(z, mineRow, h, o);
+                    }
+                    if constexpr (kForm != kLoss) end_piece(u, k, o, rowBase, t.mirror);
+                }
+                release(buf);
+                ++nt;
+            }
+            if constexpr (kForm == kLoss) {
+                if (row < p.M) p.head.parts[((int64_t)t.n * 2 + half) * p.M + row] = make_float2(terms.top, terms.sum);
+            }
+        }
+        if (lane == 0) bulk_wait();
+        if (!ok || *(volatile int32_t *)&sh.abort)                    // a residual may be on its way
+            let_copies_land();
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (kPair) cluster_barrier();              // nothing of the other CTA is on its way here any more
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if constexpr (kPair) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmemBase), "r"(512) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmemBase), "r"(512) : "memory");
+    }
+    if (threadIdx.x == 0 && sh.abort) atomicOr(p.status, kDevTimeout);
+}
+
+#define RCD_PRODUCT_ARGS const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapY, \
+                         const __grid_constant__ CUtensorMap mapZ, const __grid_constant__ CUtensorMap mapR, const __grid_constant__ TcParams p
+template <Form kForm, bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks>
+__global__ void __launch_bounds__(kThreads, 1) product_kernel(RCD_PRODUCT_ARGS)
+{
+    product_body<kForm, kInt8, kAcrossA, kAcrossB, kChunks, false>(mapA, mapB, mapY, mapZ, mapR, p);
+}
+template <Form kForm, bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_pair_kernel(RCD_PRODUCT_ARGS)
+{
+    product_body<kForm, kInt8, kAcrossA, kAcrossB, kChunks, true>(mapA, mapB, mapY, mapZ, mapR, p);
+}
+template <Form kForm, bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks>
+KernelChoice product_choice(bool pair, int bit)
+{
+    return pair ? KernelChoice{(const void *)product_pair_kernel<kForm, kInt8, kAcrossA, kAcrossB, kChunks>, bit}
+                : KernelChoice{(const void *)product_kernel<kForm, kInt8, kAcrossA, kAcrossB, kChunks>, bit + 1};
+}
+// By the operands' orders (0: neither across, 1: B, 2: both) and the columns of a piece whose sums are taken in chunks: six kernels each order.
+template <Form kForm>
+KernelChoice product_choice_by_order(int order, int wide, bool pair, int bit)
+{
+    auto by_width = [&](auto acrossA, auto acrossB, int at) {
+        constexpr bool kA = decltype(acrossA)::value, kB = decltype(acrossB)::value;
+        return wide == 0 ? product_choice<kForm, false, kA, kB, 0>(pair, at)
+               : wide == 32 ? product_choice<kForm, false, kA, kB, 32>(pair, at + 2) : product_choice<kForm, false, kA, kB, 64>(pair, at + 4);
+    };
+    const std::false_type along;
+    const std::true_type across;
+    return order == 0 ? by_width(along, along, bit) : order == 1 ? by_width(along, across, bit + 6) : by_width(across, across, bit + 12);
+}
+
+}  // namespace rcd
