@@ -236,13 +236,28 @@ KernelChoice plain_kernel(bool i8, int order, int wide, bool pair)
 rcd_status run_product(rcd_ctx *ctx, const KernelChoice &c, int grid, size_t smem, CUtensorMap (&maps)[5], TcParams &q, cudaStream_t st)
 {
     if (!(ctx->productReady >> c.bit & 1)) {            // (shared memory beyond 48 KB is asked for once per context and kernel)
+        cudaFuncAttributes at;
+        RCD_CUDA(ctx, cudaFuncGetAttributes(&at, c.kernel));
+        if (at.numRegs < kLaunchRegs) return fail(ctx, RCD_ERR_INTERNAL, "a product's kernel has %d registers a thread, too few for its warpgroups' split", at.numRegs);
         RCD_CUDA(ctx, cudaFuncSetAttribute(c.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared));
         ctx->productReady |= 1ull << c.bit;
     }
     void *args[6] = {&maps[0], &maps[1], &maps[2], &maps[3], &maps[4], &q};
+    // The launch may overtake the end of the kernel before it: barriers, tensor memory and maps are ready by then, and griddepcontrol.wait comes before the first
+    // access to memory.
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3((unsigned)grid);
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = smem;
+    config.stream = st;
+    config.attrs = &early;
+    config.numAttrs = 1;
     ctx->kernelLaunches++;
     ctx->tcLaunches++;
-    RCD_CUDA(ctx, cudaLaunchKernel(c.kernel, dim3((unsigned)grid), dim3(kThreads), args, smem, st));
+    RCD_CUDA(ctx, cudaLaunchKernelExC(&config, c.kernel, args));
     return RCD_OK;
 }
 
@@ -296,8 +311,8 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     q.slabs = (int32_t)plan.slabs;
     q.slabsPerSplit = plan.slabsPerSplit;
     q.tn = plan.tn;
-    const int chunk = p.out.type == RCD_ELEM_F32 ? kChunkSlabs : kChunkSlabs16;
-    const bool chunks = !i8 && plan.slabsPerSplit > (p.out.type == RCD_ELEM_F32 ? chunk : 2 * chunk);
+    const int chunk = p.head.sums ? kChunkSlabsSums : p.out.type == RCD_ELEM_F32 ? kChunkSlabs : kChunkSlabs16;
+    const bool chunks = !i8 && plan.slabsPerSplit > (p.head.sums || p.out.type == RCD_ELEM_F32 ? chunk : 2 * chunk);
     q.chunk = chunks ? chunk : q.slabs;
     q.stageBytes = kABytes + (plan.pair ? plan.tn / 2 : plan.tn) * kSlab;
     q.stages = std::min(kMostStages, (kMostShared - kFixedShared) / q.stageBytes);

@@ -12,7 +12,7 @@
 // are first copied (operands), or moved between that place and memory by the warp itself (outputs, residual); so are the ends of output
 // rows that do not end on 16 bytes: a TMA store writes the last 16 bytes that an element of the row lies in whole.
 //
-// Warp roles: 0 = TMA producer, 1 = TMEM allocation + MMA issue, 2..9 = epilogue, two per quarter of the TMEM lanes.
+// Warp roles: 0 = TMA producer, 1 = TMEM allocation + MMA issue, 4..11 = epilogue, two per quarter of the TMEM lanes.
 // Every wait is bounded, as in the similarity kernel: on expiry the CTA records kDevTimeout and leaves.
 #pragma once
 
@@ -35,8 +35,16 @@ constexpr int kEpiWarps = 8;
 // fp32 outputs: 512 k (2.4e-6 within a chunk, bf16 2.3e-7, and half a unit of fp32 at most for each of them).  16-bit outputs: 2048 k (1.3e-5)
 // where a piece has more than 4096, up to which the loss is a twentieth of fp16's half step.  (Gradients of 2048 x 2048 weights over 600 000
 // rows: 3.56 ms in chunks, 3.45 in one sum.)
-constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32;
-constexpr int kThreads = 64 + 32 * kEpiWarps;
+#ifndef CS
+#define CS 4
+#endif
+constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32, kChunkSlabsSums = CS;
+constexpr int kFirstEpiWarp = 4;                        // (a warpgroup for the two that issue: registers are handed over by warpgroups)
+constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
+// Registers per thread at launch (65536 over 12 warps in whole eights), and how the warpgroups split them: 128 x 40 + 256 x 232 = 384 x 168.  (168 for
+// all left a third of the sums of chunks in local memory, whose way is the one that operands come by: DESCRIBE.)
+constexpr int kLaunchRegs = 168, kIssueRegs = 40, kEpiRegs = 232;
+static_assert(128 * kIssueRegs + 32 * kEpiWarps * kEpiRegs <= kThreads * kLaunchRegs, "what one warpgroup gets the other has to have given");
 constexpr int kPiece = 32 * 128;                        // an epilogue warp's piece of the output: 32 rows of 128 bytes
 constexpr int kStaging = kEpiWarps * 2 * kPiece;
 constexpr int kColumnBytes = kEpiWarps * 2 * 32 * 4;    // 32 biases and 32 scales per warp
@@ -70,7 +78,7 @@ __device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Product
 {
     for (uint32_t turn = 0; turn < turns; ++turn) {
         uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity), "r"(20000) : "memory");
         if (ok) return true;
         if (*(volatile int32_t *)&sh->abort) return false;
@@ -260,6 +268,9 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
     const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
     const int first = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, step = kPair ? (int)(gridDim.x >> 1) : (int)gridDim.x;
 
+    if (warp == 2 && elect_one()) {
+        for (const CUtensorMap *map : {&mapA, &mapB, &mapY, &mapR}) asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMostStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&sh.accFull[b], 1); mbar_init(&sh.accEmpty[b], (kPair ? 2 : 1) * kEpiWarps); }
@@ -280,10 +291,15 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
     __syncthreads();
     if constexpr (kPair) cluster_barrier();              // the other CTA's barriers exist
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    // Up to here the kernel before this one may still be running (see run_product), from here on it has ended; and the next one may come up.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tmemBase = sh.tmemBase;
     const int rowsPerTile = kPair ? 2 * kRows : kRows;
     const int nMine = kPair ? p.tn / 2 : p.tn;           // B's rows that this CTA brings in
 
+    if (warp < kFirstEpiWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kIssueRegs));
     if (warp == 0) {
         // ---------------- TMA producer ----------------
         // (The whole warp goes through the loop, one lane issues: addresses stay in uniform registers, which is where these instructions
@@ -373,9 +389,11 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 }
             }
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kEpiRegs));
         // ---------------- epilogue: this CTA's 128 rows ----------------
-        const int q = warp & 3, ew = warp - 2, half = ew >> 2;       // TMEM lanes 32 q ..; pieces half, half + 2, ...
+        const int q = warp & 3, ew = warp - kFirstEpiWarp, half = ew >> 2;       // TMEM lanes 32 q ..; pieces half, half + 2, ...
         unsigned char *const mine = staging + ew * 2 * kPiece;
         float *const biases = columns + ew * 64, *const scales = biases + 32;
         const Epilogue &e = p.e;
@@ -383,34 +401,37 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         const int pieces = p.tn / wide;
         // a piece's coordinates; false where nothing of it lies inside the output
         struct Piece { int row, col, base, from; };        // base, from: rows of the output and of the residual before this matrix
-        auto piece_of = [&](int u, int k, Piece *o) {
-            const Unit t = unit_of(p.walk, u);
+        auto piece_of = [&](const Unit &t, int k, Piece *o) {
             o->row = t.m * rowsPerTile + rank * kRows + q * 32;
             o->col = t.n * p.tn + k * wide;
             o->base = kForm == kScaled ? t.batch * p.yStep : 0;
             o->from = kForm == kScaled ? t.batch * p.rStep : 0;
             return o->row < p.M && o->col < p.N;
         };
-        // the residual of the next piece that has one, from (u, k) on, is on its way into buffer `to`
-        auto fetch = [&](int u, int k, int to) {
+        // the residual of the next piece that has one, from piece k of t, which is unit u, on, is on its way into buffer `to`
+        auto fetch = [&](Unit t, int u, int k, int to) {
             Piece o;
-            for (; u < p.units; u += step, k = half)
+            while (true) {
                 for (; k < pieces; k += 2)
-                    if (piece_of(u, k, &o)) {
+                    if (piece_of(t, k, &o)) {
                         mbar_expect_tx(&sh.residual[ew][to], kPiece);
                         tma_load_2d(mine + to * kPiece, &mapR, o.col, o.from + o.row, &sh.residual[ew][to]);
                         return;
                     }
+                if ((u += step) >= p.units) return;
+                t = unit_of(p.walk, u);
+                k = half;
+            }
         };
         const bool mirrors = kForm == kScaled && p.walk.subM != 0;
         const bool alternate = e.z == nullptr && !mirrors;            // two buffers in turn, or one for y and one for z or the transpose
         uint32_t nt = 0, turn = 0;
-        if (p.tmaR && lane == 0) fetch(first, half, 0);
+        if (p.tmaR && lane == 0 && first < p.units) fetch(unit_of(p.walk, first), first, half, 0);
         bool ok = true;
         unsigned char *yPiece = mine;
         unsigned char *const zPiece = mine + kPiece;
         // a piece's place in shared memory is free, and the residual lies there
-        auto begin_piece = [&](int u, int k, const Piece &o) {
+        auto begin_piece = [&](const Unit &t, int u, int k, const Piece &o) {
             yPiece = mine + (alternate ? (turn & 1) * kPiece : 0);
             // (what was stored from it has been read out of it; a residual that comes next needs the other place too)
             if (lane == 0) {
@@ -419,7 +440,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             }
             __syncwarp();
             if (p.tmaR) {
-                if (alternate && lane == 0) fetch(u, k + 2, (turn & 1) ^ 1);
+                if (alternate && lane == 0) fetch(t, u, k + 2, (turn & 1) ^ 1);
                 // (with z in the other buffer the residual is fetched when the last piece has left)
                 return warp_wait_for(&sh.residual[ew][alternate ? turn & 1 : 0], alternate ? (turn >> 1) & 1 : turn & 1, &sh);
             }
@@ -451,7 +472,24 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             scales[lane] = c == 0 ? scale4[0] : c == 1 ? scale4[1] : c == 2 ? scale4[2] : scale4[3];
             __syncwarp();
         };
-        // what the lane's row brings along: asked for before the tile is ready
+        // What the lane's row brings along: asked for a tile ahead (memory answers in a tenth of what a small tile takes), worked out when its tile comes.
+        struct Asked { int label; float sx, lse, dloss, dlse; };
+        auto ask_row = [&](const Unit &t) {
+            Asked r{-1, 1.0f, 0.0f, 0.0f, 0.0f};
+            const int row = t.m * rowsPerTile + rank * kRows + q * 32 + lane;
+            if (row < p.M) {
+                if constexpr (kInt8) {
+                    if (e.xs) r.sx = e.xs[row];
+                }
+                if constexpr (kForm == kLoss || kForm == kLogitGrads) r.label = p.head.labels[row];
+                if constexpr (kForm == kLogitGrads) {
+                    r.lse = p.head.lse[row];
+                    r.dloss = p.head.dloss ? p.head.dloss[row] : 1.0f;
+                    if (p.head.dlse) r.dlse = p.head.dlse[row];
+                }
+            }
+            return r;
+        };
         struct Row {
             float sx;                                                  // int8: its scale
             int label;                                                 // its class's column in this output
@@ -459,25 +497,18 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             float alpha, beta;                                         // kScaled
             bool mirror;
         };
-        auto ask_row = [&](const Unit &t, int row) {
+        [[maybe_unused]] const float up = kForm == kLogitGrads && p.head.up ? *p.head.up : 1.0f;
+        auto row_of = [&](const Unit &t, const Asked &asked) {
             Row r{};
-            r.sx = kInt8 && e.xs && row < p.M ? e.xs[row] : 1.0f;
+            r.sx = asked.sx;
             if constexpr (kForm == kLoss || kForm == kLogitGrads) {
-                const Head &hd = p.head;
-                const int label = row < p.M ? hd.labels[row] : -1;
-                const bool valid = label >= 0 && label < hd.classes;
-                r.label = valid ? label - hd.firstClass : -1;          // (another piece's: outside 0..N-1)
+                const bool valid = asked.label >= 0 && asked.label < p.head.classes;
+                r.label = valid ? asked.label - p.head.firstClass : -1;          // (another piece's: outside 0..N-1)
                 if constexpr (kForm == kLogitGrads) {
-                    if (label >= hd.classes && t.n == 0) atomicOr(p.status, kDevBadLabel);
-                    const float up = hd.up ? *hd.up : 1.0f;
-                    float lse = 0.0f, g = 0.0f, gl = 0.0f;
-                    if (row < p.M) {
-                        lse = hd.lse[row];
-                        if (valid) g = hd.dloss ? hd.dloss[row] : 1.0f;
-                        if (hd.dlse) gl = hd.dlse[row];
-                    }
-                    r.lse = lse == -INFINITY ? INFINITY : lse;         // (a row without a class that is open: p is 0)
-                    r.weight = (g + gl) * up;
+                    if (asked.label >= p.head.classes && t.n == 0) atomicOr(p.status, kDevBadLabel);
+                    const float g = valid ? asked.dloss : 0.0f;
+                    r.lse = asked.lse == -INFINITY ? INFINITY : asked.lse;         // (a row without a class that is open: p is 0)
+                    r.weight = (g + asked.dlse) * up;
                     r.atLabel = g * up;
                 }
             }
@@ -532,13 +563,6 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
 #pragma unroll
                     for (int j = 0; j < 32; ++j) z[j] = 0.0f;
                 }
-                if (p.head.sums) {
-                    float v[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = z[j];
-                    const float sum = column_sum(v);
-                    if (o.col + h + lane < p.N) p.head.sums[(int64_t)(o.row / 32) * p.N + o.col + h + lane] = p.head.up ? sum / *p.head.up : sum;
-                }
             } else {
                 if constexpr (kInt8) {
                     if (e.xs) {
@@ -565,8 +589,14 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 if (e.residual) add_row(yPiece, lane, h / 8, z, e.type, 1.0f);
             }
             put_row(yPiece, lane, h / 8, z, e.type);
+            if constexpr (kForm == kLogitGrads) {
+                if (p.head.sums) {
+                    const float sum = column_sum(z), down = 1.0f / up;           // (powers of two)
+                    if (o.col + h + lane < p.N) p.head.sums[(int64_t)(o.row / 32) * p.N + o.col + h + lane] = sum * down;
+                }
+            }
         };
-        auto end_piece = [&](int u, int k, const Piece &o, int rowBase, bool mirror) {
+        auto end_piece = [&](const Unit &t, int u, int k, const Piece &o, int rowBase) {
             // (for the stores that leave from here by TMA, and for the next residual that TMA writes here: either comes after these ordinary writes)
             if (p.tmaY || p.tmaZ || p.tmaR) proxy_fence();
             __syncwarp();
@@ -581,7 +611,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             };
             send(p.tmaY, &mapY, yPiece, e.y, e.ldy, rowBase + o.base);
             if (kForm == kScaled) {
-                if (mirror && lane == 0) tma_store_2d(&mapZ, zPiece, o.row, o.base + o.col);
+                if (t.mirror && lane == 0) tma_store_2d(&mapZ, zPiece, o.row, o.base + o.col);
             } else if (e.z) {
                 send(p.tmaZ, &mapZ, zPiece, e.z, e.ldz, 0);
             }
@@ -589,7 +619,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             __syncwarp();
             if (p.tmaR && !alternate && lane == 0) {
                 bulk_wait_read<0>();
-                fetch(u, k + 2, 0);
+                fetch(t, u, k + 2, 0);
             }
             ++turn;
         };
@@ -598,15 +628,24 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-                if constexpr (kPair) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(leader_addr(&sh.accEmpty[buf])) : "memory");
+                if constexpr (kPair) asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(leader_addr(&sh.accEmpty[buf])) : "memory");
                 else mbar_arrive(&sh.accEmpty[buf]);
             }
         };
+        Unit next = first < p.units ? unit_of(p.walk, first) : Unit{};
+        Asked askedNext = first < p.units ? ask_row(next) : Asked{};
         for (int u = first; u < p.units && ok; u += step) {
-            const Unit t = unit_of(p.walk, u);
+            const Unit t = next;
+            const Asked asked = askedNext;
+            if (u + step < p.units) {
+                next = unit_of(p.walk, u + step);
+                askedNext = ask_row(next);
+            }
             const int rowBase = p.raw ? t.split * p.rowsPart : 0;
             const int row = t.m * rowsPerTile + rank * kRows + q * 32 + lane;
-            const Row mineRow = ask_row(t, row);
+            const uint32_t lanes = (uint32_t)(q * 32) << 16;
+            ask_columns(t);
+            const Row mineRow = row_of(t, asked);
             [[maybe_unused]] SumOfExp terms = no_terms();
             // kLoss: 32 columns join the row's sum, and its label's logit is noted
             [[maybe_unused]] auto take = [&](float (&z)[32], const Piece &o) {
@@ -630,8 +669,6 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 }
                 add_terms(terms, z);
             };
-            const uint32_t lanes = (uint32_t)(q * 32) << 16;
-            ask_columns(t);
             if constexpr (kChunks != 0) {
                 // Sums of chunks (see kChunkSlabs) in a lane's 128 registers, four times 32 columns; the next chunk is computed meanwhile.
                 float sum[4][32];
@@ -644,12 +681,16 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int col = wide == 64 ? (half + 2 * (i >> 1)) * 64 + (i & 1) * 32 : (half + 2 * i) * 32;
+                        // (16 columns at a time: with 32 the sums leave the registers for local memory, whose way is the one that operands come by)
                         if (col < p.tn) {
-                            uint32_t v[32];
-                            tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)col, v);
-                            tmem_load_wait();
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[i][j] = fresh ? __uint_as_float(v[j]) : sum[i][j] + __uint_as_float(v[j]);
+                            for (int h = 0; h < 32; h += 16) {
+                                uint32_t v[16];
+                                tmem_load_16cols(tmemBase + buf * 256 + lanes + (uint32_t)(col + h), v);
+                                tmem_load_wait();
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) sum[i][h + j] = fresh ? __uint_as_float(v[j]) : sum[i][h + j] + __uint_as_float(v[j]);
+                            }
                         }
                     }
                     release(buf);
@@ -658,17 +699,17 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 for (int i = 0; i < 4; ++i) {
                     const int k = wide == 64 ? half + 2 * (i >> 1) : half + 2 * i, h = wide == 64 ? (i & 1) * 32 : 0;
                     Piece o;
-                    if (ok && k < pieces && piece_of(u, k, &o)) {
+                    if (ok && k < pieces && piece_of(t, k, &o)) {
                         if constexpr (kForm == kLoss) {
                             columns_of(i);
                             take(sum[i], o);
                             continue;
                         }
-                        if (h == 0) ok = begin_piece(u, k, o);
+                        if (h == 0) ok = begin_piece(t, u, k, o);
                         if (ok) {
                             columns_of(i);
                             finish(sum[i], mineRow, h, o);
-                            if (h + 32 == wide) end_piece(u, k, o, rowBase, t.mirror);
+                            if (h + 32 == wide) end_piece(t, u, k, o, rowBase);
                         }
                     }
                 }
@@ -678,9 +719,9 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (int k = half; k < pieces; k += 2) {
                     Piece o;
-                    if (!piece_of(u, k, &o)) continue;
+                    if (!piece_of(t, k, &o)) continue;
                     if constexpr (kForm != kLoss) {
-                        if (!begin_piece(u, k, o)) { ok = false; break; }
+                        if (!begin_piece(t, u, k, o)) { ok = false; break; }
                     }
                     for (int h = 0; h < wide; h += 32) {
                         uint32_t v[32];
@@ -693,7 +734,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                         if constexpr (kForm == kLoss) take(z, o);
                         else finish(z, mineRow, h, o);
                     }
-                    if constexpr (kForm != kLoss) end_piece(u, k, o, rowBase, t.mirror);
+                    if constexpr (kForm != kLoss) end_piece(t, u, k, o, rowBase);
                 }
                 release(buf);
                 ++nt;
