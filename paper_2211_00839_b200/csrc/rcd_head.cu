@@ -22,6 +22,7 @@ namespace {
 __global__ void __launch_bounds__(1024) join_loss_kernel(const float2 *__restrict__ parts, int64_t count, int64_t rows, const float *__restrict__ picked,
                                                          const int32_t *__restrict__ labels, int32_t classes, float *__restrict__ loss, float *__restrict__ lse, int32_t *status)
 {
+    after_the_one_before();
     __shared__ SumOfExp sh[32][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int64_t row = (int64_t)blockIdx.x * 32 + lane;
@@ -37,18 +38,14 @@ __global__ void __launch_bounds__(1024) join_loss_kernel(const float2 *__restric
     __syncthreads();
     if (warp || row >= rows) return;
     for (int i = 1; i < warps; ++i) join_terms(s, sh[i][lane]);
-    const float all = s.top + logf(s.sum);
-    if (lse) lse[row] = all;
-    const int32_t label = labels[row];
-    const bool beyond = label >= classes;
-    if (beyond) atomicOr(status, kDevBadLabel);
-    loss[row] = beyond ? NAN : label < 0 ? 0.0f : all - picked[row];
+    finish_loss(s, labels[row], classes, picked[row], loss + row, lse ? lse + row : nullptr, status);
 }
 
 // fp16: a power of two that brings the largest gradient of a logit to 2^13..2^14, so that those 2^-38 of it are still held (p is small almost
 // everywhere, and a mean's dloss is 1 / rows); up[1] takes it out of the products again.
 __global__ void __launch_bounds__(1024) choose_up_kernel(const float *__restrict__ dloss, const float *__restrict__ dlse, int64_t rows, float *__restrict__ up)
 {
+    after_the_one_before();
     __shared__ float sh[32];
     float most = 0.0f;
     for (int64_t r = threadIdx.x; r < rows; r += 1024) most = fmaxf(most, fabsf(dloss ? dloss[r] : 1.0f) + (dlse ? fabsf(dlse[r]) : 0.0f));
@@ -68,6 +65,7 @@ __global__ void __launch_bounds__(1024) choose_up_kernel(const float *__restrict
 template <typename T>
 __global__ void __launch_bounds__(256) round_rows_kernel(const float *__restrict__ from, int64_t ld, int64_t rows, int64_t len, T *__restrict__ to, int64_t ldTo)
 {
+    after_the_one_before();
     const int64_t perRow = (len + 3) / 4;
     const bool whole = ((uintptr_t)to) % (4 * sizeof(T)) == 0 && ldTo % 4 == 0;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * perRow; i += (int64_t)gridDim.x * 256) {
@@ -132,11 +130,17 @@ ForwardPlan forward_plan(rcd_ctx *ctx, const rcd_cross_entropy_args &a, unsigned
     ForwardPlan f{};
     f.p = logits(a.rows, a.n, a.k, a.type, a.x_dev, a.ldx, a.w_dev, a.ldw, a.bias_dev_or_null, kLoss);
     f.parts = 2 * product_tile_columns(ctx, f.p);
+    f.p.head.labels = a.labels_dev;
+    f.p.head.classes = (int32_t)a.n;
+    if (f.parts == 2) {                    // one tile takes all classes
+        f.p.head.loss = a.loss_dev;
+        f.p.head.lseOut = a.lse_dev_or_null;
+        f.bytes = align_up(product_workspace(ctx, f.p));
+        return f;
+    }
     f.picked = align_up((size_t)(f.parts * a.rows) * sizeof(float2));
     f.product = f.picked + align_up((size_t)a.rows * 4);
     f.bytes = f.product + align_up(product_workspace(ctx, f.p));
-    f.p.head.labels = a.labels_dev;
-    f.p.head.classes = (int32_t)a.n;
     f.p.head.parts = (float2 *)ws;
     f.p.head.picked = (float *)(ws + f.picked);
     return f;
@@ -173,7 +177,9 @@ int64_t piece_of(const rcd_cross_entropy_back_args &a)
 struct BackPlan {
     int64_t piece, pieces, ldDz, ldSum;
     bool sumDx;                            // dx of several pieces: in fp32
-    size_t dz, sum, sums, up, product, bytes;
+    bool packX, packW;                     // copies whose rows start on 16 bytes, which all products read
+    int64_t ldPacked;
+    size_t dz, sum, sums, up, x, w, product, bytes;
     Product z, dx, dw;
 };
 BackPlan back_plan(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a, unsigned char *ws, int64_t first)
@@ -192,10 +198,16 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a, unsigned 
     b.sum = place(b.sumDx, (size_t)(a.rows * b.ldSum) * 4);
     b.sums = place(a.dbias_dev_or_null, (size_t)((a.rows + 31) / 32 * b.piece) * 4);
     b.up = place(a.type == RCD_ELEM_F16, 8);
+    b.packX = !rows_mappable(a.x_dev, a.ldx, eb);
+    b.packW = !rows_mappable(a.w_dev, a.ldw, eb);
+    b.ldPacked = (a.k + 7) / 8 * 8;
+    b.x = place(b.packX, (size_t)(a.rows * b.ldPacked) * 2);
+    b.w = place(b.packW, (size_t)(b.piece * b.ldPacked) * 2);
     b.product = at;
     const float *up = a.type == RCD_ELEM_F16 ? (const float *)(ws + b.up) : nullptr;
-    const unsigned char *w = (const unsigned char *)a.w_dev + first * a.ldw * eb;
-    b.z = logits(a.rows, n, a.k, a.type, a.x_dev, a.ldx, w, a.ldw, a.bias_dev_or_null ? a.bias_dev_or_null + first : nullptr, kLogitGrads);
+    const void *x = b.packX ? ws + b.x : a.x_dev, *w = b.packW ? ws + b.w : (const unsigned char *)a.w_dev + first * a.ldw * eb;
+    const int64_t ldx = b.packX ? b.ldPacked : a.ldx, ldw = b.packW ? b.ldPacked : a.ldw;
+    b.z = logits(a.rows, n, a.k, a.type, x, ldx, w, ldw, a.bias_dev_or_null ? a.bias_dev_or_null + first : nullptr, kLogitGrads);
     b.z.out.y = ws + b.dz;
     b.z.out.ldy = b.ldDz;
     b.z.head.labels = a.labels_dev;
@@ -211,7 +223,7 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a, unsigned 
     b.dx.form = b.dw.form = up ? kScaled : kPlain;
     b.dx.M = a.rows; b.dx.N = a.k; b.dx.K = n;
     b.dx.a = {ws + b.dz, b.ldDz, false};
-    b.dx.b = {w, a.ldw, true};
+    b.dx.b = {w, ldw, true};
     b.dx.out.type = b.sumDx ? RCD_ELEM_F32 : a.type;
     b.dx.out.y = b.sumDx ? (void *)(ws + b.sum) : a.dx_dev_or_null;
     b.dx.out.ldy = b.sumDx ? b.ldSum : a.ld_dx;
@@ -221,7 +233,7 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a, unsigned 
     }
     b.dw.M = n; b.dw.N = a.k; b.dw.K = a.rows;
     b.dw.a = {ws + b.dz, b.ldDz, true};
-    b.dw.b = {a.x_dev, a.ldx, true};
+    b.dw.b = {x, ldx, true};
     b.dw.out.type = a.dw_type;
     b.dw.out.y = a.dw_dev_or_null ? (unsigned char *)a.dw_dev_or_null + first * a.ld_dw * elem_bytes(a.dw_type) : nullptr;
     b.dw.out.ldy = a.ld_dw;
@@ -264,7 +276,7 @@ extern "C" rcd_status rcd_linear_cross_entropy(rcd_ctx *ctx, const rcd_cross_ent
     if (a.rows == 0) return RCD_OK;
     RCD_TRY(check_workspace(ctx, workspace_dev, workspace_bytes, need));
     const int64_t eb = elem_bytes(a.type);
-    const Area out[] = {{a.loss_dev, 1, a.rows, a.rows, 4}, {a.lse_dev_or_null, 1, a.rows, a.rows, 4}, {workspace_dev, 1, (int64_t)need, (int64_t)need, 1}};
+    const Area out[] = {{a.loss_dev, 1, a.rows, a.rows, 4}, {a.lse_dev_or_null, 1, a.rows, a.rows, 4}, {need ? workspace_dev : nullptr, 1, (int64_t)need, (int64_t)need, 1}};
     const Area in[] = {{a.x_dev, a.rows, a.ldx, a.k, eb}, {a.w_dev, a.n, a.ldw, a.k, eb}, {a.bias_dev_or_null, 1, a.n, a.n, 4}, {a.labels_dev, 1, a.rows, a.rows, 4}};
     RCD_TRY(check_apart(ctx, out, 3, in, 4));
     cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -272,12 +284,9 @@ extern "C" rcd_status rcd_linear_cross_entropy(rcd_ctx *ctx, const rcd_cross_ent
     unsigned char *ws = (unsigned char *)workspace_dev;
     const ForwardPlan f = forward_plan(ctx, a, ws);
     RCD_TRY(launch_product(ctx, f.p, ws + f.product, st));
-    const int threads = 32 * (int)std::min<int64_t>(f.parts, 32);
-    join_loss_kernel<<<(unsigned)((a.rows + 31) / 32), threads, 0, st>>>(f.p.head.parts, f.parts, a.rows, f.p.head.picked, a.labels_dev, (int32_t)a.n, a.loss_dev, a.lse_dev_or_null,
-                                                                         ctx->statusOwn + kOperatorStatus);
-    ctx->kernelLaunches++;
-    RCD_CUDA(ctx, cudaGetLastError());
-    return RCD_OK;
+    if (f.p.head.loss) return RCD_OK;
+    return launch_early(ctx, join_loss_kernel, dim3((unsigned)((a.rows + 31) / 32)), 32 * (unsigned)std::min<int64_t>(f.parts, 32), st, f.p.head.parts, f.parts, a.rows, f.p.head.picked,
+                        a.labels_dev, (int32_t)a.n, a.loss_dev, a.lse_dev_or_null, ctx->statusOwn + kOperatorStatus);
 }
 
 extern "C" rcd_status rcd_linear_cross_entropy_backward_workspace_bytes(rcd_ctx *ctx, const rcd_cross_entropy_back_args *args, size_t *bytes_out)
@@ -313,12 +322,12 @@ extern "C" rcd_status rcd_linear_cross_entropy_backward(rcd_ctx *ctx, const rcd_
     unsigned char *ws = (unsigned char *)workspace_dev;
     BackPlan b = back_plan(ctx, a, ws, 0);
     if (a.type == RCD_ELEM_F16) {
-        choose_up_kernel<<<1, 1024, 0, st>>>(a.dloss_dev_or_null, a.dlse_dev_or_null, a.rows, (float *)(ws + b.up));
-        ctx->kernelLaunches++;
-        RCD_CUDA(ctx, cudaGetLastError());
+        RCD_TRY(launch_early(ctx, choose_up_kernel, dim3(1), 1024, st, a.dloss_dev_or_null, a.dlse_dev_or_null, a.rows, (float *)(ws + b.up)));
     }
+    if (b.packX) RCD_TRY(launch_pack(ctx, a.x_dev, a.ldx, a.rows, a.k, eb, ws + b.x, b.ldPacked, st));
     for (int64_t i = 0; i < b.pieces; ++i) {
         if (i) b = back_plan(ctx, a, ws, i * b.piece);
+        if (b.packW) RCD_TRY(launch_pack(ctx, (const unsigned char *)a.w_dev + i * b.piece * a.ldw * eb, a.ldw, b.z.N, a.k, eb, ws + b.w, b.ldPacked, st));
         RCD_TRY(launch_product(ctx, b.z, ws + b.product, st));
         if (a.dbias_dev_or_null) RCD_TRY(launch_column_sums(ctx, b.z.head.sums, (a.rows + 31) / 32, b.z.N, a.dbias_dev_or_null + i * b.piece, st));
         if (a.dx_dev_or_null) RCD_TRY(launch_product(ctx, b.dx, ws + b.product, st));
@@ -326,10 +335,8 @@ extern "C" rcd_status rcd_linear_cross_entropy_backward(rcd_ctx *ctx, const rcd_
     }
     if (b.sumDx) {
         const unsigned grid = (unsigned)std::min<int64_t>((a.rows * ((a.k + 3) / 4) + 255) / 256, (int64_t)ctx->smCount * 16);
-        if (a.type == RCD_ELEM_BF16) round_rows_kernel<<<grid, 256, 0, st>>>((const float *)(ws + b.sum), b.ldSum, a.rows, a.k, (__nv_bfloat16 *)a.dx_dev_or_null, a.ld_dx);
-        else round_rows_kernel<<<grid, 256, 0, st>>>((const float *)(ws + b.sum), b.ldSum, a.rows, a.k, (__half *)a.dx_dev_or_null, a.ld_dx);
-        ctx->kernelLaunches++;
-        RCD_CUDA(ctx, cudaGetLastError());
+        return a.type == RCD_ELEM_BF16 ? launch_early(ctx, round_rows_kernel<__nv_bfloat16>, dim3(grid), 256, st, (const float *)(ws + b.sum), b.ldSum, a.rows, a.k, (__nv_bfloat16 *)a.dx_dev_or_null, a.ld_dx)
+                                       : launch_early(ctx, round_rows_kernel<__half>, dim3(grid), 256, st, (const float *)(ws + b.sum), b.ldSum, a.rows, a.k, (__half *)a.dx_dev_or_null, a.ld_dx);
     }
     return RCD_OK;
 }

@@ -71,6 +71,7 @@ __global__ void __launch_bounds__(256) slope_kernel(const T *__restrict__ dy, in
 // out[c] = sum over the rows of partial, in a fixed order: 32 columns per CTA, 32 warps take every 32nd row.
 __global__ void __launch_bounds__(1024) column_sums_kernel(const float *__restrict__ partial, int32_t rows, int64_t d, float *__restrict__ out)
 {
+    after_the_one_before();
     __shared__ float sh[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t col = (int64_t)blockIdx.x * 32 + lane;
@@ -217,10 +218,7 @@ rcd_status check_rows(rcd_ctx *ctx, const char *name, const void *p, int64_t row
 
 rcd_status launch_column_sums(rcd_ctx *ctx, const float *partial, int64_t rows, int64_t d, float *out, cudaStream_t st)
 {
-    column_sums_kernel<<<(unsigned)((d + 31) / 32), 1024, 0, st>>>(partial, (int32_t)rows, d, out);
-    ctx->kernelLaunches++;
-    RCD_CUDA(ctx, cudaGetLastError());
-    return RCD_OK;
+    return launch_early(ctx, column_sums_kernel, dim3((unsigned)((d + 31) / 32)), 1024, st, partial, (int32_t)rows, d, out);
 }
 
 }  // namespace rcd

@@ -30,6 +30,7 @@ struct Head {
     int32_t classes, firstClass;           // of all pieces; the class that column 0 is
     float2 *parts;                         // out [2 tile columns][rows]: reference and sum of exponentials of half a tile's columns
     float *picked;                         // out [rows]: the label's logit
+    float *loss, *lseOut;                  // out [rows] (lseOut may be null), in place of parts and picked: where one tile takes all classes
     const float *lse, *dloss, *dlse;       // [rows]; null: ones, zeros
     const float *up;                       // a power of two that the gradients are multiplied by; null: 1
     float *sums;                           // out [32-row groups][n], or null: columns of the gradients, not multiplied by it
@@ -69,6 +70,36 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
 // The product of few rows (rcd_linear_few.cu; no workspace), and whether it takes one.
 bool few_rows(const Product &p);
 rcd_status launch_few_rows(rcd_ctx *ctx, const Product &p, cudaStream_t st);
+
+// Rows of any start and distance to rows that start on 16 bytes.
+bool rows_mappable(const void *p, int64_t ld, int64_t eb);
+rcd_status launch_pack(rcd_ctx *ctx, const void *from, int64_t ld, int64_t rows, int64_t len, int64_t eb, void *to, int64_t ldTo, cudaStream_t st);
+
+// A launch that may overtake the end of the kernel before it in its stream; the kernel begins with after_the_one_before().
+template <typename... Args>
+rcd_status launch_early(rcd_ctx *ctx, void (*kernel)(Args...), dim3 grid, unsigned threads, cudaStream_t st, typename std::common_type<Args>::type... args)
+{
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid;
+    config.blockDim = dim3(threads);
+    config.stream = st;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    ctx->kernelLaunches++;
+    RCD_CUDA(ctx, cudaLaunchKernelEx(&config, kernel, args...));
+    return RCD_OK;
+}
+#ifdef __CUDACC__
+// Before a kernel's first access to memory: the one before it has ended; and the next one may come up, as far as it does not touch memory.
+__device__ __forceinline__ void after_the_one_before()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+#endif
 
 // out[c] = sum over the rows of partial[rows][d], in a fixed order
 rcd_status launch_column_sums(rcd_ctx *ctx, const float *partial, int64_t rows, int64_t d, float *out, cudaStream_t st);

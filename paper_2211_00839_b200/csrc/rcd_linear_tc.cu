@@ -12,6 +12,7 @@ template <bool kInt8>
 __global__ void __launch_bounds__(256) join_kernel(const void *__restrict__ parts, int32_t splits, int32_t M, int64_t rowsPart, int32_t N, int64_t ld, const __grid_constant__ Epilogue e,
                                                    const __grid_constant__ Scaling sc)
 {
+    after_the_one_before();
     const int perRow = (N + 3) / 4;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= (int64_t)M * perRow) return;
@@ -66,6 +67,7 @@ __global__ void __launch_bounds__(256) join_kernel(const void *__restrict__ part
 template <typename T>
 __global__ void __launch_bounds__(256) pack_kernel(const T *__restrict__ src, int64_t ld, int64_t rows, int64_t len, T *__restrict__ dst, int64_t ldDst)
 {
+    after_the_one_before();
     constexpr int V = 16 / sizeof(T);
     const int64_t perRow = ldDst / V, total = rows * perRow;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
@@ -110,7 +112,6 @@ struct Plan {
     size_t partAt, aAt, bAt, bytes;
 };
 
-bool mappable(const Operand &o, int64_t eb) { return ((uintptr_t)o.p) % 16 == 0 && o.ld * eb % 16 == 0 && o.ld * eb < (1LL << 40); }
 
 // Column tiles that are neighbours in the order of the work, where B has more bytes than stay in L2.
 constexpr int kBand = 8;
@@ -133,7 +134,7 @@ Plan make_plan(const rcd_ctx *ctx, const Product &p, bool packA, bool packB)
     const int64_t batch = std::max<int64_t>(p.batch, 1);
     double least = 1e300;
     for (int pair = 0; pair < 2; ++pair)
-        for (int tn = 64; tn <= 256; tn += 64) {
+        for (int tn = 64; tn <= 256; tn += p.form == kLoss && !pair ? 32 : 64) {       // (rounds of 64 columns where whole pieces of 16-bit output are stored)
             if (pair && p.b.across && tn % 128 != 0) continue;         // (boxes of 64 columns per CTA)
             if (pair && ctx->smCount < 2) continue;
             const int64_t tilesM = (p.M + (pair ? 256 : 128) - 1) / (pair ? 256 : 128), tilesN = (p.N + tn - 1) / tn;
@@ -146,7 +147,8 @@ Plan make_plan(const rcd_ctx *ctx, const Product &p, bool packA, bool packB)
                 tiles = blocks * (blocks + 1) / 2 * (block / rowsTile) * (block / tn);
             }
             if (tiles * batch > 0x3fffffffLL) continue;
-            const double slab = std::max(512.0 * tn / 256.0, (pair ? 128.0 + tn / 2 : 128.0 + tn) * kSlab / 56.0) + 10.0;
+            const double aRows = head && !pair ? (double)std::min<int64_t>(p.M, 128) : 128.0;
+            const double slab = std::max(512.0 * tn / 256.0, (aRows + (pair ? tn / 2 : tn)) * kSlab / 56.0) + 10.0;
             for (int splits = 1; splits <= 64; ++splits) {
                 if (splits > 1 && (whole || tiles * splits > 2 * slots || splits > slabs)) break;
                 const int64_t per = (slabs + splits - 1) / splits;
@@ -199,7 +201,7 @@ const Plan &plan_product(rcd_ctx *ctx, const Product &p)
     static_assert(sizeof(PlanCache) <= sizeof(ctx->productPlans) && std::is_trivially_copyable<PlanCache>::value, "the context has room for it");
     PlanCache &c = *reinterpret_cast<PlanCache *>(ctx->productPlans);      // (zeros at first: how 0 is nobody's)
     const int64_t eb = elem_bytes(p.type);
-    const bool packA = !mappable(p.a, eb), packB = !mappable(p.b, eb);
+    const bool packA = !rows_mappable(p.a.p, p.a.ld, eb), packB = !rows_mappable(p.b.p, p.b.ld, eb);
     const int how = 1 | (int)p.type << 1 | (int)p.a.across << 3 | (int)p.b.across << 4 | (int)packA << 5 | (int)packB << 6 | (int)p.form << 7 | (int)p.symmetric << 9;
     for (const PlanCache::Entry &e : c.of)
         if (e.how == how && e.M == p.M && e.N == p.N && e.K == p.K && e.ldA == p.a.ld && e.ldB == p.b.ld && e.batch == p.batch) return e.plan;
@@ -273,6 +275,15 @@ rcd_status launch_operator_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStre
 
 int64_t product_tile_columns(rcd_ctx *ctx, const Product &p) { return plan_product(ctx, p).tilesN; }
 
+bool rows_mappable(const void *p, int64_t ld, int64_t eb) { return ((uintptr_t)p) % 16 == 0 && ld * eb % 16 == 0 && ld * eb < (1LL << 40); }
+
+rcd_status launch_pack(rcd_ctx *ctx, const void *from, int64_t ld, int64_t rows, int64_t len, int64_t eb, void *to, int64_t ldTo, cudaStream_t st)
+{
+    const dim3 grid((unsigned)std::min<int64_t>((rows * (ldTo * eb / 16) + 255) / 256, (int64_t)ctx->smCount * 16));
+    return eb == 1 ? launch_early(ctx, pack_kernel<int8_t>, grid, 256, st, (const int8_t *)from, ld, rows, len, (int8_t *)to, ldTo)
+                   : launch_early(ctx, pack_kernel<uint16_t>, grid, 256, st, (const uint16_t *)from, ld, rows, len, (uint16_t *)to, ldTo);
+}
+
 size_t product_workspace(rcd_ctx *ctx, const Product &p) { return p.form == kPlain && few_rows(p) ? 0 : plan_product(ctx, p).bytes; }
 
 rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaStream_t st)
@@ -288,17 +299,15 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
         const int64_t rows = (batch - 1) * step + (o.across ? p.K : mn), len = o.across ? mn : p.K;
         const void *from = o.p;
         if (pack) {
-            const unsigned grid = (unsigned)std::min<int64_t>((rows * (ld * eb / 16) + 255) / 256, (int64_t)ctx->smCount * 16);
-            if (i8) pack_kernel<int8_t><<<grid, 256, 0, st>>>((const int8_t *)o.p, o.ld, rows, len, (int8_t *)(ws + at), ld);
-            else pack_kernel<uint16_t><<<grid, 256, 0, st>>>((const uint16_t *)o.p, o.ld, rows, len, (uint16_t *)(ws + at), ld);
-            ctx->kernelLaunches++;
-            RCD_CUDA(ctx, cudaGetLastError());
+            RCD_TRY(launch_pack(ctx, o.p, o.ld, rows, len, eb, ws + at, ld, st));
             from = ws + at;
         }
         return encode(ctx, map, map_type(p.type), from, len, rows, ld * eb, o.across ? 64 : (int)(kSlab / eb), o.across ? kSlabRows16 : boxRows);
     };
+    // (few rows take no place for 128: what the instruction reads behind them are rows that nobody looks at)
+    const int aRows = p.a.across || plan.pair ? kRows : (int)std::min<int64_t>(kRows, (p.M + 7) / 8 * 8);
     CUtensorMap maps[5] = {};
-    RCD_TRY(operand(p.a, p.M, plan.packA, plan.ldA, plan.aAt, kRows, p.aStep, &maps[0]));
+    RCD_TRY(operand(p.a, p.M, plan.packA, plan.ldA, plan.aAt, aRows, p.aStep, &maps[0]));
     RCD_TRY(operand(p.b, p.N, plan.packB, plan.ldB, plan.bAt, plan.pair ? plan.tn / 2 : plan.tn, p.bStep, &maps[1]));
 
     TcParams q{};
@@ -314,8 +323,10 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     const int chunk = p.head.sums ? kChunkSlabsSums : p.out.type == RCD_ELEM_F32 ? kChunkSlabs : kChunkSlabs16;
     const bool chunks = !i8 && plan.slabsPerSplit > (p.head.sums || p.out.type == RCD_ELEM_F32 ? chunk : 2 * chunk);
     q.chunk = chunks ? chunk : q.slabs;
-    q.stageBytes = kABytes + (plan.pair ? plan.tn / 2 : plan.tn) * kSlab;
-    q.stages = std::min(kMostStages, (kMostShared - kFixedShared) / q.stageBytes);
+    q.aRows = aRows;
+    q.stagingBytes = p.form == kLoss ? kJoinStaging : kStaging;
+    q.stageBytes = (q.aRows + (plan.pair ? plan.tn / 2 : plan.tn)) * kSlab;
+    q.stages = std::min(kMostStages, (kMostShared - q.stagingBytes - kFixedShared) / q.stageBytes);
     q.idesc = (i8 ? (2u << 4) | (1u << 7) | (1u << 10)                                     // S8 x S8 -> S32
                   : (1u << 4) | (p.type == RCD_ELEM_BF16 ? (1u << 7) | (1u << 10) : 0u)) | // BF16 x BF16 or F16 x F16 -> F32
               (p.a.across ? 1u << 15 : 0u) | (p.b.across ? 1u << 16 : 0u) | ((uint32_t)(plan.tn >> 3) << 17) | ((uint32_t)((plan.pair ? 256 : 128) >> 4) << 24);
@@ -343,7 +354,7 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
         RCD_TRY(encode(ctx, &maps[3], map_type(q.e.type), q.e.y, p.N, rows_of(p.yStep), q.e.ldy * yb, 32, 64, CU_TENSOR_MAP_SWIZZLE_NONE));
     }
     q.edgeByHand = !q.raw && p.N * yb % 16 != 0;           // (a piece of the k axis has rows of whole 128 bytes)
-    const size_t smem = (size_t)q.stages * q.stageBytes + kFixedShared;
+    const size_t smem = (size_t)q.stages * q.stageBytes + q.stagingBytes + kFixedShared;
     const int slots = plan.pair ? ctx->smCount / 2 : ctx->smCount;
     const int grid = std::min(slots, q.units) * (plan.pair ? 2 : 1);
     const int order = !p.a.across && !p.b.across ? 0 : !p.a.across ? 1 : 2;
@@ -354,11 +365,8 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     if (rs != RCD_OK || !q.raw) return rs;
     const Scaling scaling = p.form == kScaled ? p.scaling : Scaling{1.0f, 1.0f, nullptr, 0, 0, p.out.type};
     const int64_t threads = p.M * ((p.N + 3) / 4);
-    if (i8) join_kernel<true><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(ws + plan.partAt, plan.splits, (int32_t)p.M, plan.rowsPart, (int32_t)p.N, plan.ldPart, p.out, scaling);
-    else join_kernel<false><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(ws + plan.partAt, plan.splits, (int32_t)p.M, plan.rowsPart, (int32_t)p.N, plan.ldPart, p.out, scaling);
-    ctx->kernelLaunches++;
-    RCD_CUDA(ctx, cudaGetLastError());
-    return RCD_OK;
+    return launch_early(ctx, i8 ? join_kernel<true> : join_kernel<false>, dim3((unsigned)((threads + 255) / 256)), 256, st, ws + plan.partAt, plan.splits, (int32_t)p.M, plan.rowsPart,
+                        (int32_t)p.N, plan.ldPart, p.out, scaling);
 }
 
 }  // namespace rcd

@@ -25,6 +25,7 @@ struct Gradient { const void *p; int64_t ld, step; int32_t rows, cols; };
 template <typename T, int kVec>
 __global__ void __launch_bounds__(256) squares_kernel(Gradient g, double *__restrict__ parts)
 {
+    after_the_one_before();
     __shared__ double sh[8];
     const T *p = (const T *)g.p + blockIdx.y * g.step;
     const int64_t perRow = (g.cols + kVec - 1) / kVec, total = perRow * g.rows;
@@ -55,6 +56,7 @@ template <typename T, int kVec>
 __global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double *__restrict__ parts, int32_t count, float eps, __half *__restrict__ x, int32_t rowsX, int32_t colsX,
                                                        float *__restrict__ factor)
 {
+    after_the_one_before();
     __shared__ float scales[2];
     if (threadIdx.x < 32) {
         double s = 0.0;
@@ -98,6 +100,7 @@ __global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double 
 // X to the output where its matrices lie in a way that the last product cannot write.
 __global__ void __launch_bounds__(256) bring_out_kernel(const __half *__restrict__ x, int32_t rowsX, int32_t colsX, __nv_bfloat16 *__restrict__ o, int64_t ld, int64_t step, int32_t rows, int32_t cols)
 {
+    after_the_one_before();
     const int64_t total = (int64_t)rows * cols;
     x += (int64_t)blockIdx.y * rowsX * colsX;
     o += blockIdx.y * step;
@@ -270,23 +273,18 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
     const Layout l = layout_of(ctx, a);
     const Gradient g{a.g_dev, a.ld_g, a.batch > 1 ? a.step_g : 0, (int32_t)a.rows, (int32_t)a.cols};
     const bool aligned = rows_aligned(a.g_dev, a.ld_g, eb, 16) && (a.batch == 1 || a.step_g * eb % 16 == 0);
-    auto bring_up = [&](auto t, auto vec) {
+    auto bring_up = [&](auto t, auto vec) -> rcd_status {
         using T = decltype(t);
         constexpr int kVec = decltype(vec)::value;
-        squares_kernel<T, kVec><<<dim3((unsigned)l.parts, (unsigned)a.batch), 256, 0, st>>>(g, (double *)(ws + l.squares));
+        RCD_TRY(launch_early(ctx, squares_kernel<T, kVec>, dim3((unsigned)l.parts, (unsigned)a.batch), 256, st, g, (double *)(ws + l.squares)));
         const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((l.rows * l.cols / 8 + 255) / 256, 8 * ctx->smCount / a.batch));
-        bring_up_kernel<T, kVec><<<dim3(grid, (unsigned)a.batch), 256, 0, st>>>(g, (const double *)(ws + l.squares), l.parts, a.eps, (__half *)(ws + l.x[0]), (int32_t)l.rows, (int32_t)l.cols,
-                                                                                (float *)(ws + l.factor));
+        return launch_early(ctx, bring_up_kernel<T, kVec>, dim3(grid, (unsigned)a.batch), 256, st, g, (const double *)(ws + l.squares), l.parts, a.eps, (__half *)(ws + l.x[0]), (int32_t)l.rows,
+                            (int32_t)l.cols, (float *)(ws + l.factor));
     };
     auto by_type = [&](auto t) {
-        if (aligned) bring_up(t, std::integral_constant<int, 16 / sizeof(t)>());
-        else bring_up(t, std::integral_constant<int, 1>());
+        return aligned ? bring_up(t, std::integral_constant<int, 16 / sizeof(t)>()) : bring_up(t, std::integral_constant<int, 1>());
     };
-    if (a.type == RCD_ELEM_BF16) by_type(__nv_bfloat16());
-    else if (a.type == RCD_ELEM_F16) by_type(__half());
-    else by_type(0.0f);
-    ctx->kernelLaunches += 2;
-    RCD_CUDA(ctx, cudaGetLastError());
+    RCD_TRY(a.type == RCD_ELEM_BF16 ? by_type(__nv_bfloat16()) : a.type == RCD_ELEM_F16 ? by_type(__half()) : by_type(0.0f));
     const bool direct = direct_output(a);
     for (int i = 0; i < a.steps; ++i) {
         const Step s = step_of(a, l, ws, i, direct && i == a.steps - 1);
@@ -294,10 +292,8 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
     }
     if (!direct) {
         const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((a.rows * a.cols + 1023) / 1024, 8 * ctx->smCount / a.batch));
-        bring_out_kernel<<<dim3(grid, (unsigned)a.batch), 256, 0, st>>>((const __half *)(ws + l.x[a.steps & 1]), (int32_t)l.rows, (int32_t)l.cols, (__nv_bfloat16 *)a.o_dev, a.ld_o, a.step_o, (int32_t)a.rows,
-                                                                        (int32_t)a.cols);
-        ctx->kernelLaunches++;
-        RCD_CUDA(ctx, cudaGetLastError());
+        return launch_early(ctx, bring_out_kernel, dim3(grid, (unsigned)a.batch), 256, st, (const __half *)(ws + l.x[a.steps & 1]), (int32_t)l.rows, (int32_t)l.cols, (__nv_bfloat16 *)a.o_dev, a.ld_o,
+                            a.step_o, (int32_t)a.rows, (int32_t)a.cols);
     }
     return RCD_OK;
 }

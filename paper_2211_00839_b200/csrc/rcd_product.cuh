@@ -27,7 +27,6 @@ constexpr int kRows = 128;                              // rows of A per CTA
 constexpr int kSlab = 128;                              // bytes of k per operand row and stage
 constexpr int kSlabRows16 = 64;                         // k elements of 16 bits per slab
 constexpr int kBox = 64 * kSlab;                        // 8 KB: 64 k rows of 64 elements
-constexpr int kABytes = kRows * kSlab;
 constexpr int kMostStages = 8;
 constexpr int kEpiWarps = 8;
 // The tensor cores cut an fp32 sum off where they cannot hold it, towards zero: products of fp16 and of one sign lose 6.5e-9 of the result
@@ -47,7 +46,7 @@ constexpr int kLaunchRegs = 168, kIssueRegs = 40, kEpiRegs = 232;
 static_assert(128 * kIssueRegs + 32 * kEpiWarps * kEpiRegs <= kThreads * kLaunchRegs, "what one warpgroup gets the other has to have given");
 constexpr int kPiece = 32 * 128;                        // an epilogue warp's piece of the output: 32 rows of 128 bytes
 constexpr int kStaging = kEpiWarps * 2 * kPiece;
-constexpr int kColumnBytes = kEpiWarps * 2 * 32 * 4;    // 32 biases and 32 scales per warp
+constexpr int kColumnBytes = kEpiWarps * 2 * 128 * 4;   // a warp's 128 columns of a tile: biases and scales
 constexpr uint32_t kWaitTurns = 1u << 16;               // of at most 20 us: a second or so
 constexpr int kMostShared = 227 * 1024;
 
@@ -55,13 +54,15 @@ struct __align__(8) ProductShared {
     uint64_t full[kMostStages], empty[kMostStages];     // full: CTA 0's of a pair
     uint64_t accFull[2], accEmpty[2];                   // accEmpty: CTA 0's of a pair
     uint64_t residual[kEpiWarps][2];
+    uint64_t handed[4][2];                              // kLoss: the quarter's second warp has left its half of a tile, two tiles in turn
     uint32_t tmemBase;
     int32_t abort;
 };
-constexpr int kFixedShared = kStaging + kColumnBytes + (int)sizeof(ProductShared);
+constexpr int kFixedShared = kColumnBytes + (int)sizeof(ProductShared);
+constexpr int kJoinStaging = 2 * 4 * 3 * 32 * 4;        // kLoss: what the second warp of a quarter hands to the first, two tiles in turn
 
 struct TcParams {
-    int32_t M, N, units, slabs, slabsPerSplit, chunk, tn, stages, stageBytes, rowsPart;
+    int32_t M, N, units, slabs, slabsPerSplit, chunk, tn, stages, stageBytes, stagingBytes, aRows, rowsPart;
     uint32_t idesc;
     Walk walk;
     int32_t aStep, bStep, yStep, rStep;                        // rows from one matrix of a batch to the next (rows of k, where an operand is across)
@@ -107,6 +108,11 @@ template <int kLeft>
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" :: "n"(kLeft) : "memory"); }
 __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void copy_float(float *to, const float *from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" :: "r"(smem_addr(to)), "l"(from) : "memory");
+}
 
 // Descriptor of an operand whose m (n) elements lie next to each other: boxes of 64 of them (128 bytes) by 64 k, 8 KB apart; groups of 8 k
 // are 1024 bytes apart.
@@ -236,22 +242,29 @@ __device__ __forceinline__ void join_terms(SumOfExp &s, const SumOfExp &o)
     s.top = top;
 }
 
-// Sums of 32 columns over the warp's 32 rows, a lane's row in v: lane j ends with column j's.  A lane passes on half of what it holds at
-// every step: 31 exchanges.
-__device__ __forceinline__ float column_sum(float (&v)[32])
+// A row's loss from its sum and its label's logit.
+__device__ __forceinline__ void finish_loss(const SumOfExp &s, int32_t label, int32_t classes, float picked, float *loss, float *lse, int32_t *status)
+{
+    const float all = s.top + logf(s.sum);
+    if (lse) *lse = all;
+    const bool beyond = label >= classes;
+    if (beyond) atomicOr(status, kDevBadLabel);
+    *loss = beyond ? NAN : label < 0 ? 0.0f : all - picked;
+}
+
+// Sums of 32 columns over the warp's 32 rows, a lane's row in v: lane j ends with column j's, added up in the rows' order by fours.  Through 4 KB of
+// shared memory, a word of row r and column c at 32 r + (c ^ r): lanes meet no other's bank on either way.
+__device__ __forceinline__ float column_sum(const float (&v)[32], float *place)
 {
     const int lane = threadIdx.x & 31;
+    __syncwarp();
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const bool upper = lane & o;
+    for (int j = 0; j < 32; ++j) place[32 * lane + (j ^ lane)] = v[j];
+    __syncwarp();
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (i < o) {
-                const float mine = upper ? v[i + o] : v[i], other = upper ? v[i] : v[i + o];
-                v[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
-            }
-    }
-    return v[0];
+    for (int r = 0; r < 32; ++r) sum[r & 3] += place[32 * r + (lane ^ r)];
+    return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 // kChunks: 0, or the columns of a piece of the output, whose sums are taken in chunks.
@@ -261,8 +274,8 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char *const tiles = smem;
     unsigned char *const staging = smem + (size_t)p.stages * p.stageBytes;
-    float *const columns = reinterpret_cast<float *>(staging + kStaging);
-    ProductShared &sh = *reinterpret_cast<ProductShared *>(staging + kStaging + kColumnBytes);
+    float *const columns = reinterpret_cast<float *>(staging + p.stagingBytes);
+    ProductShared &sh = *reinterpret_cast<ProductShared *>(staging + p.stagingBytes + kColumnBytes);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
@@ -275,6 +288,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         for (int s = 0; s < kMostStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&sh.accFull[b], 1); mbar_init(&sh.accEmpty[b], (kPair ? 2 : 1) * kEpiWarps); }
         for (int w = 0; w < kEpiWarps; ++w) { mbar_init(&sh.residual[w][0], 1); mbar_init(&sh.residual[w][1], 1); }
+        for (int w = 0; w < 4; ++w) { mbar_init(&sh.handed[w][0], 1); mbar_init(&sh.handed[w][1], 1); }
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -291,9 +305,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
     __syncthreads();
     if constexpr (kPair) cluster_barrier();              // the other CTA's barriers exist
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    // Up to here the kernel before this one may still be running (see run_product), from here on it has ended; and the next one may come up.
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    after_the_one_before();
     const uint32_t tmemBase = sh.tmemBase;
     const int rowsPerTile = kPair ? 2 * kRows : kRows;
     const int nMine = kPair ? p.tn / 2 : p.tn;           // B's rows that this CTA brings in
@@ -309,7 +321,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         uint32_t phase = 1;
         bool ok = true;
         const int slabElems = kInt8 ? kSlab : kSlab / 2;
-        const uint32_t bytes = (uint32_t)(kPair ? 2 : 1) * (uint32_t)(kABytes + nMine * kSlab);
+        const uint32_t bytes = (uint32_t)(kPair ? 2 : 1) * (uint32_t)((p.aRows + nMine) * kSlab);
         for (int u = first; u < p.units && ok; u += step) {
             const Unit t = unit_of(p.walk, u);
             const int m0 = t.m * rowsPerTile + rank * kRows, n0 = t.n * p.tn + rank * nMine;
@@ -317,7 +329,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
             for (int kb = t.split * p.slabsPerSplit; kb < end; ++kb) {
                 if (!warp_wait_for(&sh.empty[s], phase, &sh)) { ok = false; break; }
-                unsigned char *a = tiles + s * p.stageBytes, *b = a + kABytes;
+                unsigned char *a = tiles + s * p.stageBytes, *b = a + p.aRows * kSlab;
                 if (leader) {
                     if (rank == 0) mbar_expect_tx(&sh.full[s], bytes);
                     uint32_t bar = smem_addr(&sh.full[s]);
@@ -364,7 +376,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                     for (int kb = begin; kb < stop; ++kb) {
                         if (!warp_wait_for(&sh.full[s], phase, &sh)) { ok = false; break; }
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint32_t aAddr = tile0 + (uint32_t)(s * p.stageBytes), bAddr = aAddr + kABytes;
+                        const uint32_t aAddr = tile0 + (uint32_t)(s * p.stageBytes), bAddr = aAddr + (uint32_t)(p.aRows * kSlab);
                         const uint64_t descA = kAcrossA ? across_desc(aAddr) : make_smem_desc(aAddr);
                         const uint64_t descB = kAcrossB ? across_desc(bAddr) : make_smem_desc(bAddr);
                         // one MMA takes 32 bytes of k per row, or 16 rows of k of 128 bytes each
@@ -395,7 +407,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         // ---------------- epilogue: this CTA's 128 rows ----------------
         const int q = warp & 3, ew = warp - kFirstEpiWarp, half = ew >> 2;       // TMEM lanes 32 q ..; pieces half, half + 2, ...
         unsigned char *const mine = staging + ew * 2 * kPiece;
-        float *const biases = columns + ew * 64, *const scales = biases + 32;
+        float *const biases = columns + ew * 256, *const scales = biases + 128;
         const Epilogue &e = p.e;
         const int wide = kChunks ? kChunks : e.type == RCD_ELEM_F32 ? 32 : 64;        // columns of a piece
         const int pieces = p.tn / wide;
@@ -424,8 +436,10 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             }
         };
         const bool mirrors = kForm == kScaled && p.walk.subM != 0;
-        const bool alternate = e.z == nullptr && !mirrors;            // two buffers in turn, or one for y and one for z or the transpose
+        const bool sums = kForm == kLogitGrads && p.head.sums != nullptr;
+        const bool alternate = e.z == nullptr && !mirrors && !sums;   // two buffers in turn, or one for y and one for z, the transpose or sums
         uint32_t nt = 0, turn = 0;
+        [[maybe_unused]] uint32_t tile = 0;
         if (p.tmaR && lane == 0 && first < p.units) fetch(unit_of(p.walk, first), first, half, 0);
         bool ok = true;
         unsigned char *yPiece = mine;
@@ -452,27 +466,26 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             }
             return true;
         };
-        // The biases and scales of the warp's columns of a tile, 32 at a time (up to four times): asked for before the tile is ready, since
-        // memory takes longer to answer than 32 columns take to finish; and those of one time to all lanes.
-        const bool anyColumns = !p.raw && (e.bias || e.ws);
-        float bias4[4], scale4[4];
+        // The biases and scales of the warp's columns of a tile (up to four times 32), on their way into shared memory while the tile is computed.
+        const bool anyColumns = !p.raw && (e.bias || (kInt8 && e.ws));
         auto ask_columns = [&](const Unit &t) {
             if (!anyColumns) return;
+            __syncwarp();                                              // (all have read the last tile's)
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const int col = t.n * p.tn + (wide == 64 ? (half + 2 * (c >> 1)) * 64 + (c & 1) * 32 : (half + 2 * c) * 32) + lane;
-                bias4[c] = e.bias && col < p.N ? e.bias[col] : 0.0f;
-                scale4[c] = e.ws && col < p.N ? e.ws[col] : 1.0f;
+                if (col < p.N) {
+                    if (e.bias) copy_float(biases + c * 32 + lane, e.bias + col);
+                    if (kInt8 && e.ws) copy_float(scales + c * 32 + lane, e.ws + col);
+                }
             }
         };
-        auto columns_of = [&](int c) {
+        auto have_columns = [&] {
             if (!anyColumns) return;
-            __syncwarp();
-            biases[lane] = c == 0 ? bias4[0] : c == 1 ? bias4[1] : c == 2 ? bias4[2] : bias4[3];
-            scales[lane] = c == 0 ? scale4[0] : c == 1 ? scale4[1] : c == 2 ? scale4[2] : scale4[3];
+            asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();
         };
-        // What the lane's row brings along: asked for a tile ahead (memory answers in a tenth of what a small tile takes), worked out when its tile comes.
+        // What the lane's row brings along: asked for when the tile before is about to be finished, worked out when its own comes.
         struct Asked { int label; float sx, lse, dloss, dlse; };
         auto ask_row = [&](const Unit &t) {
             Asked r{-1, 1.0f, 0.0f, 0.0f, 0.0f};
@@ -522,8 +535,8 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             }
             return r;
         };
-        // 32 columns of the lane's row, from column h of the piece on
-        auto finish = [&](float (&z)[32], const Row &r, int h, const Piece &o) {
+        // 32 columns of the lane's row, from column h of the piece on, the warp's c-th
+        auto finish = [&](float (&z)[32], const Row &r, int h, int c, const Piece &o) {
             if (p.raw) {
                 // (as they are)
             } else if constexpr (kForm == kScaled) {
@@ -542,7 +555,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 if (e.bias) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
-                        const float4 b = reinterpret_cast<const float4 *>(biases)[j / 4];
+                        const float4 b = reinterpret_cast<const float4 *>(biases + c * 32)[j / 4];
                         z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
                     }
                 }
@@ -572,7 +585,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                     if (e.ws) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
-                            const float4 w = reinterpret_cast<const float4 *>(scales)[j / 4];
+                            const float4 w = reinterpret_cast<const float4 *>(scales + c * 32)[j / 4];
                             z[j] *= w.x; z[j + 1] *= w.y; z[j + 2] *= w.z; z[j + 3] *= w.w;
                         }
                     }
@@ -580,7 +593,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 if (e.bias) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
-                        const float4 b = reinterpret_cast<const float4 *>(biases)[j / 4];
+                        const float4 b = reinterpret_cast<const float4 *>(biases + c * 32)[j / 4];
                         z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
                     }
                 }
@@ -591,7 +604,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             put_row(yPiece, lane, h / 8, z, e.type);
             if constexpr (kForm == kLogitGrads) {
                 if (p.head.sums) {
-                    const float sum = column_sum(z), down = 1.0f / up;           // (powers of two)
+                    const float sum = column_sum(z, reinterpret_cast<float *>(zPiece)), down = 1.0f / up;           // (powers of two)
                     if (o.col + h + lane < p.N) p.head.sums[(int64_t)(o.row / 32) * p.N + o.col + h + lane] = sum * down;
                 }
             }
@@ -637,22 +650,21 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         for (int u = first; u < p.units && ok; u += step) {
             const Unit t = next;
             const Asked asked = askedNext;
-            if (u + step < p.units) {
-                next = unit_of(p.walk, u + step);
-                askedNext = ask_row(next);
-            }
+            if (u + step < p.units) next = unit_of(p.walk, u + step);
             const int rowBase = p.raw ? t.split * p.rowsPart : 0;
             const int row = t.m * rowsPerTile + rank * kRows + q * 32 + lane;
             const uint32_t lanes = (uint32_t)(q * 32) << 16;
             ask_columns(t);
             const Row mineRow = row_of(t, asked);
             [[maybe_unused]] SumOfExp terms = no_terms();
+            [[maybe_unused]] float picked = 0.0f;
+            [[maybe_unused]] bool found = false;
             // kLoss: 32 columns join the row's sum, and its label's logit is noted
-            [[maybe_unused]] auto take = [&](float (&z)[32], const Piece &o) {
+            [[maybe_unused]] auto take = [&](float (&z)[32], int c, const Piece &o) {
                 if (e.bias) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
-                        const float4 b = reinterpret_cast<const float4 *>(biases)[j / 4];
+                        const float4 b = reinterpret_cast<const float4 *>(biases + c * 32)[j / 4];
                         z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
                     }
                 }
@@ -662,86 +674,94 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 }
                 const int at = mineRow.label - o.col;
                 if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
-                    float picked = 0.0f;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) picked = at == j ? z[j] : picked;
-                    if (at >= 0 && at < 32) p.head.picked[row] = picked;
+                    found = found || (at >= 0 && at < 32);
                 }
                 add_terms(terms, z);
             };
+            uint32_t buf = nt & 1;
             if constexpr (kChunks != 0) {
-                // Sums of chunks (see kChunkSlabs) in a lane's 128 registers, four times 32 columns; the next chunk is computed meanwhile.
-                float sum[4][32];
+                // Sums of chunks (see kChunkSlabs) in a lane's 128 registers, four times 32 columns, while the next chunk is computed; what they come to goes back
+                // into the last chunk's place and is finished from there as any accumulator.  (Finished from the registers, the code has four copies of what finishes 32 columns and
+                // leaves the instruction cache, 2400 cycles for each; in a loop the sums leave the registers.)
+                float sum[8][16];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[i][j] = 0.0f;
+                auto column = [&](int i) { return wide == 64 ? (half + 2 * (i >> 2)) * 64 + (i & 3) * 16 : (half + 2 * (i >> 1)) * 32 + (i & 1) * 16; };
                 const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
-                for (int begin = t.split * p.slabsPerSplit; begin < end && ok; begin += p.chunk, ++nt) {
-                    const uint32_t buf = nt & 1;
+#pragma unroll 1
+                for (int begin = t.split * p.slabsPerSplit; begin < end; begin += p.chunk, ++nt) {
+                    buf = nt & 1;
                     if (!warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const bool fresh = begin == t.split * p.slabsPerSplit;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int col = wide == 64 ? (half + 2 * (i >> 1)) * 64 + (i & 1) * 32 : (half + 2 * i) * 32;
-                        // (16 columns at a time: with 32 the sums leave the registers for local memory, whose way is the one that operands come by)
-                        if (col < p.tn) {
+                    for (int i = 0; i < 8; ++i) {
+                        // (columns behind the tile are loaded, too: nobody looks at them)
+                        uint32_t v[16];
+                        tmem_load_16cols(tmemBase + buf * 256 + lanes + (uint32_t)column(i), v);
+                        tmem_load_wait();
 #pragma unroll
-                            for (int h = 0; h < 32; h += 16) {
-                                uint32_t v[16];
-                                tmem_load_16cols(tmemBase + buf * 256 + lanes + (uint32_t)(col + h), v);
-                                tmem_load_wait();
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) sum[i][h + j] = fresh ? __uint_as_float(v[j]) : sum[i][h + j] + __uint_as_float(v[j]);
-                            }
-                        }
+                        for (int j = 0; j < 16; ++j) sum[i][j] += __uint_as_float(v[j]);
                     }
-                    release(buf);
+                    if (begin + p.chunk < end) release(buf);
                 }
+                if (!ok) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int k = wide == 64 ? half + 2 * (i >> 1) : half + 2 * i, h = wide == 64 ? (i & 1) * 32 : 0;
-                    Piece o;
-                    if (ok && k < pieces && piece_of(t, k, &o)) {
-                        if constexpr (kForm == kLoss) {
-                            columns_of(i);
-                            take(sum[i], o);
-                            continue;
-                        }
-                        if (h == 0) ok = begin_piece(t, u, k, o);
-                        if (ok) {
-                            columns_of(i);
-                            finish(sum[i], mineRow, h, o);
-                            if (h + 32 == wide) end_piece(t, u, k, o, rowBase);
-                        }
-                    }
-                }
+                for (int i = 0; i < 8; ++i) tmem_store_16cols(tmemBase + buf * 256 + lanes + (uint32_t)column(i), sum[i]);
+                tmem_store_wait();
             } else {
-                const uint32_t buf = nt & 1;
                 if (!warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh)) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int k = half; k < pieces; k += 2) {
-                    Piece o;
-                    if (!piece_of(t, k, &o)) continue;
-                    if constexpr (kForm != kLoss) {
-                        if (!begin_piece(t, u, k, o)) { ok = false; break; }
-                    }
-                    for (int h = 0; h < wide; h += 32) {
-                        uint32_t v[32];
-                        tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)(k * wide + h), v);
-                        columns_of(wide == 64 ? (k - half) + h / 32 : (k - half) / 2);
-                        tmem_load_wait();
-                        float z[32];
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) z[j] = kInt8 && !p.raw ? (float)(int32_t)v[j] : __uint_as_float(v[j]);      // (raw integers stay what they are)
-                        if constexpr (kForm == kLoss) take(z, o);
-                        else finish(z, mineRow, h, o);
-                    }
-                    if constexpr (kForm != kLoss) end_piece(t, u, k, o, rowBase);
-                }
-                release(buf);
                 ++nt;
             }
-            if constexpr (kForm == kLoss) {
-                if (row < p.M) p.head.parts[((int64_t)t.n * 2 + half) * p.M + row] = make_float2(terms.top, terms.sum);
+            have_columns();
+            if (u + step < p.units) askedNext = ask_row(next);
+            for (int k = half; k < pieces; k += 2) {
+                Piece o;
+                if (!piece_of(t, k, &o)) continue;
+                if constexpr (kForm != kLoss) {
+                    if (!begin_piece(t, u, k, o)) { ok = false; break; }
+                }
+                for (int h = 0; h < wide; h += 32) {
+                    uint32_t v[32];
+                    tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)(k * wide + h), v);
+                    const int c = wide == 64 ? (k - half) + h / 32 : (k - half) / 2;
+                    tmem_load_wait();
+                    float z[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[j] = kInt8 && !p.raw ? (float)(int32_t)v[j] : __uint_as_float(v[j]);      // (raw integers stay what they are)
+                    if constexpr (kForm == kLoss) take(z, c, o);
+                    else finish(z, mineRow, h, c, o);
+                }
+                if constexpr (kForm != kLoss) end_piece(t, u, k, o, rowBase);
             }
+            if constexpr (kForm == kLoss) {
+                const Head &hd = p.head;
+                if (!hd.loss) {
+                    if (row < p.M) hd.parts[((int64_t)t.n * 2 + half) * p.M + row] = make_float2(terms.top, terms.sum);
+                    if (found) hd.picked[row] = picked;
+                } else {
+                    // One tile takes all classes: the quarter's second warp hands its half to the first, which gives the accumulator back only when it has read it.
+                    // So the second is a tile ahead at most, and place and barrier are free again two tiles later.
+                    float *const place = reinterpret_cast<float *>(staging) + ((tile & 1) * 4 + q) * 96;
+                    if (half) {
+                        place[lane] = terms.top;
+                        place[32 + lane] = terms.sum;
+                        place[64 + lane] = picked;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh.handed[q][tile & 1]);
+                    } else {
+                        if (!warp_wait_for(&sh.handed[q][tile & 1], (tile >> 1) & 1, &sh)) break;
+                        join_terms(terms, {place[lane], place[32 + lane]});
+                        if (row < p.M) finish_loss(terms, asked.label, hd.classes, found ? picked : place[64 + lane], hd.loss + row, hd.lseOut ? hd.lseOut + row : nullptr, p.status);
+                    }
+                    ++tile;
+                }
+            }
+            release(buf);
         }
         if (lane == 0) bulk_wait();
         if (!ok || *(volatile int32_t *)&sh.abort)                    // a residual may be on its way

@@ -408,7 +408,7 @@ def test_refusals(rcd, ctx):
     import ctypes as C
     import torch
     g = seeded("refusals")
-    x, w, b, y = head(g, 20, 30, 64, torch.bfloat16)
+    x, w, b, y = head(g, 20, 600, 64, torch.bfloat16)             # (more classes than one tile takes: the call has a workspace)
     _, lse = ctx.rcd_linear_cross_entropy(x, w, y, bias=b)
     for call in (lambda **kw: ctx.rcd_linear_cross_entropy(**{**dict(x=x, w=w, labels=y, bias=b), **kw}),
                  lambda **kw: ctx.rcd_linear_cross_entropy_backward(**{**dict(x=x, w=w, labels=y, lse=lse, bias=b), **kw})):
@@ -439,7 +439,7 @@ def test_refusals(rcd, ctx):
     with pytest.raises(rcd.RcdError):
         ctx.rcd_linear_cross_entropy_backward(x, w, y, lse, bias=b, dw_dtype=torch.float16)
     loss = torch.empty(20, device="cuda")
-    ok = dict(rows=20, n=30, k=64, type=1, x=x.data_ptr(), ldx=64, w=w.data_ptr(), ldw=64, bias=b.data_ptr(), labels=y.data_ptr(), loss=loss.data_ptr(), lse=lse.data_ptr())
+    ok = dict(rows=20, n=600, k=64, type=1, x=x.data_ptr(), ldx=64, w=w.data_ptr(), ldw=64, bias=b.data_ptr(), labels=y.data_ptr(), loss=loss.data_ptr(), lse=lse.data_ptr())
     need = C.c_size_t()
 
     def refused(status, ws=None, size=0, **change):
