@@ -8,6 +8,7 @@
 // itself to bf16 takes 1.7e-3).  G is brought into range by a power of two alone, so that a 16-bit G is held exactly; what is left of its norm, a factor between 1 and 2, goes into the
 // first step's products as a number that their epilogue reads.  A and B are symmetric: tiles on and below the diagonal are computed and
 // stored both ways.
+#include "rcd_orthogonal.h"
 #include "rcd_product.cuh"
 
 namespace rcd {
@@ -16,7 +17,6 @@ KernelChoice scaled_kernel(int order, int wide, bool pair) { return product_choi
 
 namespace {
 
-constexpr int kUp = 10;                    // X, A and B are held times 2^kUp
 constexpr int kMostParts = 256;            // sums of squares per matrix
 
 struct Gradient { const void *p; int64_t ld, step; int32_t rows, cols; };
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(256) squares_kernel(Gradient g, double *__rest
 // G times the power of two that brings |G| + eps to 2^(kUp - 1) .. 2^kUp, and the factor that is left of 2^kUp / (|G| + eps); zeros up to whole 64 rows and columns.
 template <typename T, int kVec>
 __global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double *__restrict__ parts, int32_t count, float eps, __half *__restrict__ x, int32_t rowsX, int32_t colsX,
-                                                       float *__restrict__ factor)
+                                                       float *__restrict__ factor, uint32_t *__restrict__ counters)
 {
     after_the_one_before();
     __shared__ float scales[2];
@@ -76,6 +76,8 @@ __global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double 
         }
     }
     __syncthreads();
+    if (counters && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < kFusedCounters; i += 256) counters[i] = 0;
     const float up0 = scales[0], up1 = scales[1];
     const T *p = (const T *)g.p + blockIdx.y * g.step;
     __half *to = x + (int64_t)blockIdx.y * rowsX * colsX;
@@ -116,7 +118,7 @@ rcd_status check(rcd_ctx *ctx, const rcd_orthogonalize_args &a)
     if (!elem_is_float(a.type)) return fail(ctx, RCD_ERR_INVALID_ARG, "g must be bf16, fp16 or fp32, got type %d", (int)a.type);
     if (a.batch < 0 || a.rows < 0 || a.cols < 0) return fail(ctx, RCD_ERR_INVALID_ARG, "batch=%lld, rows=%lld or cols=%lld is negative", (long long)a.batch, (long long)a.rows, (long long)a.cols);
     if (a.batch >= most || a.rows > most || a.cols > most) return fail(ctx, RCD_ERR_UNSUPPORTED, "batch=%lld, rows=%lld, cols=%lld: 65535 matrices of 65536 x 65536 at most", (long long)a.batch, (long long)a.rows, (long long)a.cols);
-    if (a.steps < 1 || a.steps > 64) return fail(ctx, RCD_ERR_INVALID_ARG, "steps=%d must be from 1 to 64", (int)a.steps);
+    if (a.steps < 1 || a.steps > kMostSteps) return fail(ctx, RCD_ERR_INVALID_ARG, "steps=%d must be from 1 to 64", (int)a.steps);
     if (!a.coefficients_host) return fail(ctx, RCD_ERR_INVALID_ARG, "coefficients is null");
     for (int i = 0; i < 3 * a.steps; ++i)
         if (!(fabsf(a.coefficients_host[i]) <= 1e4f)) return fail(ctx, RCD_ERR_INVALID_ARG, "coefficient %d is not within 1e4", i);
@@ -136,7 +138,8 @@ struct Layout {
     bool tall;
     int64_t rows, cols, side;              // of X, A and B, whole 64s
     int32_t parts;
-    size_t x[2], a, b, squares, factor, product, bytes;
+    FusedPlan fused;
+    size_t x[2], a, b, squares, factor, counters, product, bytes;      // product: the products' workspace, or the parts of the form of one launch
 };
 // Step i's products; (first of them, second, third).
 struct Step { Product gram, poly, x; };
@@ -225,7 +228,13 @@ Layout layout_of(rcd_ctx *ctx, const rcd_orthogonalize_args &a)
     l.b = place((size_t)(a.batch * l.side * l.side) * 2);
     l.squares = place((size_t)(a.batch * l.parts) * 8);
     l.factor = place((size_t)a.batch * 4);
+    l.fused = fused_plan(ctx, a.batch, l.rows, l.cols);
+    l.counters = place(l.fused.use ? kFusedCounters * 4 : 0);
     l.product = at;
+    if (l.fused.use) {
+        l.bytes = at + align_up(l.fused.parts);
+        return l;
+    }
     size_t most = 0;
     for (const bool direct : {false, true}) {
         const Step s = step_of(a, l, nullptr, 0, direct && direct_output(a));
@@ -279,12 +288,34 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
         RCD_TRY(launch_early(ctx, squares_kernel<T, kVec>, dim3((unsigned)l.parts, (unsigned)a.batch), 256, st, g, (double *)(ws + l.squares)));
         const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((l.rows * l.cols / 8 + 255) / 256, 8 * ctx->smCount / a.batch));
         return launch_early(ctx, bring_up_kernel<T, kVec>, dim3(grid, (unsigned)a.batch), 256, st, g, (const double *)(ws + l.squares), l.parts, a.eps, (__half *)(ws + l.x[0]), (int32_t)l.rows,
-                            (int32_t)l.cols, (float *)(ws + l.factor));
+                            (int32_t)l.cols, (float *)(ws + l.factor), l.fused.use ? (uint32_t *)(ws + l.counters) : nullptr);
     };
     auto by_type = [&](auto t) {
         return aligned ? bring_up(t, std::integral_constant<int, 16 / sizeof(t)>()) : bring_up(t, std::integral_constant<int, 1>());
     };
     RCD_TRY(a.type == RCD_ELEM_BF16 ? by_type(__nv_bfloat16()) : a.type == RCD_ELEM_F16 ? by_type(__half()) : by_type(0.0f));
+    if (l.fused.use) {
+        FusedParams p{};
+        p.x0 = (__half *)(ws + l.x[0]);
+        p.x1 = (__half *)(ws + l.x[1]);
+        p.a = (__half *)(ws + l.a);
+        p.b = (__half *)(ws + l.b);
+        p.factor = (const float *)(ws + l.factor);
+        p.parts = (float *)(ws + l.product);
+        p.counters = (uint32_t *)(ws + l.counters);
+        p.o = (__nv_bfloat16 *)a.o_dev;
+        p.ldO = a.ld_o;
+        p.stepO = a.batch > 1 ? a.step_o : 0;
+        p.rowsO = (int32_t)a.rows; p.colsO = (int32_t)a.cols;
+        p.rows = (int32_t)l.rows; p.cols = (int32_t)l.cols; p.side = (int32_t)l.side;
+        p.batch = (int32_t)a.batch;
+        p.steps = a.steps;
+        p.tall = l.tall;
+        for (int k = 0; k < 3; ++k) p.splits[k] = l.fused.splits[k];
+        p.status = ctx->statusOwn + kOperatorStatus;
+        for (int i = 0; i < 3 * a.steps; ++i) p.coefficients[i] = a.coefficients_host[i];
+        return launch_fused(ctx, p, l.fused, st);
+    }
     const bool direct = direct_output(a);
     for (int i = 0; i < a.steps; ++i) {
         const Step s = step_of(a, l, ws, i, direct && i == a.steps - 1);
