@@ -71,6 +71,8 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
 bool few_rows(const Product &p);
 rcd_status launch_few_rows(rcd_ctx *ctx, const Product &p, cudaStream_t st);
 
+double product_cycles(rcd_ctx *ctx, const Product &p);                 // the estimate that the choice of tiles goes by
+
 // Rows of any start and distance to rows that start on 16 bytes.
 bool rows_mappable(const void *p, int64_t ld, int64_t eb);
 rcd_status launch_pack(rcd_ctx *ctx, const void *from, int64_t ld, int64_t rows, int64_t len, int64_t eb, void *to, int64_t ldTo, cudaStream_t st);

@@ -106,6 +106,7 @@ __global__ void __launch_bounds__(64) operator_wait_selftest_kernel(int32_t *sta
 struct Plan {
     bool pair;
     int tn, splits, slabsPerSplit, band, subM, subN;
+    double cycles;                                       // an estimate
     int64_t slabs, tilesM, tilesN, tiles, rowsPart, ldPart;     // rowsPart: whole pieces of 32 rows, which are stored whole
     bool packA, packB;
     int64_t ldA, ldB;
@@ -157,7 +158,7 @@ Plan make_plan(const rcd_ctx *ctx, const Product &p, bool packA, bool packB)
                 double t = (double)waves * std::max((double)per * slab, head ? 12.0 * tn : 0.0) + 2500.0 + 9.0 * tn;
                 if (splits > 1) t += 6000.0 + (double)p.M * (double)p.N * 8.0 * splits / 5000.0;
                 if (t < least) {
-                    least = t;
+                    least = best.cycles = t;
                     best.pair = pair != 0;
                     best.tn = tn;
                     best.splits = splits;
@@ -274,6 +275,7 @@ rcd_status launch_operator_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStre
 }
 
 int64_t product_tile_columns(rcd_ctx *ctx, const Product &p) { return plan_product(ctx, p).tilesN; }
+double product_cycles(rcd_ctx *ctx, const Product &p) { return plan_product(ctx, p).cycles; }
 
 bool rows_mappable(const void *p, int64_t ld, int64_t eb) { return ((uintptr_t)p) % 16 == 0 && ld * eb % 16 == 0 && ld * eb < (1LL << 40); }
 

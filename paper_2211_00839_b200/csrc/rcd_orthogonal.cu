@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(256) squares_kernel(Gradient g, double *__rest
 // G times the power of two that brings |G| + eps to 2^(kUp - 1) .. 2^kUp, and the factor that is left of 2^kUp / (|G| + eps); zeros up to whole 64 rows and columns.
 template <typename T, int kVec>
 __global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double *__restrict__ parts, int32_t count, float eps, __half *__restrict__ x, int32_t rowsX, int32_t colsX,
-                                                       float *__restrict__ factor, uint32_t *__restrict__ counters)
+                                                       float *__restrict__ factor, uint32_t *__restrict__ counter)
 {
     after_the_one_before();
     __shared__ float scales[2];
@@ -76,8 +76,7 @@ __global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double 
         }
     }
     __syncthreads();
-    if (counters && blockIdx.x == 0 && blockIdx.y == 0)
-        for (int i = threadIdx.x; i < kFusedCounters; i += 256) counters[i] = 0;
+    if (counter && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *counter = 0;
     const float up0 = scales[0], up1 = scales[1];
     const T *p = (const T *)g.p + blockIdx.y * g.step;
     __half *to = x + (int64_t)blockIdx.y * rowsX * colsX;
@@ -139,7 +138,8 @@ struct Layout {
     int64_t rows, cols, side;              // of X, A and B, whole 64s
     int32_t parts;
     FusedPlan fused;
-    size_t x[2], a, b, squares, factor, counters, product, bytes;      // product: the products' workspace, or the parts of the form of one launch
+    bool inOne;                            // all steps in one launch
+    size_t x[2], a, b, squares, factor, counter, product, bytes;
 };
 // Step i's products; (first of them, second, third).
 struct Step { Product gram, poly, x; };
@@ -228,13 +228,18 @@ Layout layout_of(rcd_ctx *ctx, const rcd_orthogonalize_args &a)
     l.b = place((size_t)(a.batch * l.side * l.side) * 2);
     l.squares = place((size_t)(a.batch * l.parts) * 8);
     l.factor = place((size_t)a.batch * 4);
-    l.fused = fused_plan(ctx, a.batch, l.rows, l.cols);
-    l.counters = place(l.fused.use ? kFusedCounters * 4 : 0);
-    l.product = at;
-    if (l.fused.use) {
-        l.bytes = at + align_up(l.fused.parts);
-        return l;
+    l.fused = fused_plan(ctx, a.batch, l.rows, l.cols, l.tall);
+    if (l.fused.possible) {
+        // Launches of their own take 4.3 us each besides the products.  (Both measured: 512 x 512 97 us in one launch, 123 in 17; 1024 x 2048 192 and 190; 1536 x 1536
+        // 341 and 214.)
+        const Step s = step_of(a, l, nullptr, 0, false);
+        double us = 0.0;
+        for (const Product *p : {&s.gram, &s.poly, &s.x}) us += 4.3 + product_cycles(ctx, *p) / 1900.0;
+        l.inOne = l.fused.stepUs < us;
     }
+    l.counter = place(l.inOne ? 4 : 0);
+    l.product = l.bytes = at;
+    if (l.inOne) return l;
     size_t most = 0;
     for (const bool direct : {false, true}) {
         const Step s = step_of(a, l, nullptr, 0, direct && direct_output(a));
@@ -288,21 +293,20 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
         RCD_TRY(launch_early(ctx, squares_kernel<T, kVec>, dim3((unsigned)l.parts, (unsigned)a.batch), 256, st, g, (double *)(ws + l.squares)));
         const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((l.rows * l.cols / 8 + 255) / 256, 8 * ctx->smCount / a.batch));
         return launch_early(ctx, bring_up_kernel<T, kVec>, dim3(grid, (unsigned)a.batch), 256, st, g, (const double *)(ws + l.squares), l.parts, a.eps, (__half *)(ws + l.x[0]), (int32_t)l.rows,
-                            (int32_t)l.cols, (float *)(ws + l.factor), l.fused.use ? (uint32_t *)(ws + l.counters) : nullptr);
+                            (int32_t)l.cols, (float *)(ws + l.factor), l.inOne ? (uint32_t *)(ws + l.counter) : nullptr);
     };
     auto by_type = [&](auto t) {
         return aligned ? bring_up(t, std::integral_constant<int, 16 / sizeof(t)>()) : bring_up(t, std::integral_constant<int, 1>());
     };
     RCD_TRY(a.type == RCD_ELEM_BF16 ? by_type(__nv_bfloat16()) : a.type == RCD_ELEM_F16 ? by_type(__half()) : by_type(0.0f));
-    if (l.fused.use) {
+    if (l.inOne) {
         FusedParams p{};
         p.x0 = (__half *)(ws + l.x[0]);
         p.x1 = (__half *)(ws + l.x[1]);
         p.a = (__half *)(ws + l.a);
         p.b = (__half *)(ws + l.b);
         p.factor = (const float *)(ws + l.factor);
-        p.parts = (float *)(ws + l.product);
-        p.counters = (uint32_t *)(ws + l.counters);
+        p.counter = (uint32_t *)(ws + l.counter);
         p.o = (__nv_bfloat16 *)a.o_dev;
         p.ldO = a.ld_o;
         p.stepO = a.batch > 1 ? a.step_o : 0;
@@ -311,7 +315,7 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
         p.batch = (int32_t)a.batch;
         p.steps = a.steps;
         p.tall = l.tall;
-        for (int k = 0; k < 3; ++k) p.splits[k] = l.fused.splits[k];
+        for (int k = 0; k < 3; ++k) p.phases[k] = l.fused.phases[k];
         p.status = ctx->statusOwn + kOperatorStatus;
         for (int i = 0; i < 3 * a.steps; ++i) p.coefficients[i] = a.coefficients_host[i];
         return launch_fused(ctx, p, l.fused, st);

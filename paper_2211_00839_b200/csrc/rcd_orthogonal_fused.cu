@@ -11,22 +11,26 @@
 #include "rcd_tc.cuh"
 #include "rcd_walk.h"
 
-#ifndef FUSED_RULE
-#define FUSED_RULE true
-#endif
 namespace rcd {
 
 namespace {
 
-constexpr int kRows = 128, kCols = 64, kBoxBytes = 64 * 128, kStage = 3 * kBoxBytes, kStages = 8, kThreads = 384, kFirstFinisher = 4, kFinishers = 8;
-constexpr uint32_t kWaitTurns = 1u << 16, kPolls = 1u << 22;           // about a second either
+constexpr int kRows = 128, kCols = 64, kBoxBytes = 64 * 128, kStage = 3 * kBoxBytes, kStages = 7, kThreads = 384, kFirstFinisher = 4, kFinishers = 8;
+constexpr int kCluster = 4;                                            // CTAs: those that may share a tile
+constexpr int kPartial = kRows * kCols * 4;
+constexpr uint32_t kWaitTurns = 1u << 16, kPolls = 1u << 21;           // about a second either
 
 struct __align__(8) FusedShared {
     uint64_t full[kStages], empty[kStages], accFull[2], accEmpty[2];
+    uint64_t open;                         // the phase before is complete on all SMs
+    uint64_t done;                         // this phase is on this one
+    uint64_t partials;                     // the team's sums of this CTA's rows are here
     uint32_t tmemBase;
-    int32_t abort, leave;
+    int32_t abort;
+    Unit units[3][kFusedUnits];            // what this CTA does in the phases of a step
+    int32_t count[3];
 };
-constexpr int kSharedBytes = kStages * kStage + (int)sizeof(FusedShared);
+constexpr int kSharedBytes = kStages * kStage + kPartial + (int)sizeof(FusedShared);
 
 __device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, FusedShared *sh)
 {
@@ -48,20 +52,33 @@ __device__ __forceinline__ bool elect_one()
     return mine != 0;
 }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async;" ::: "memory"); }
-__device__ __forceinline__ uint32_t load_acquire(const uint32_t *p)
+// The grid's barrier: a count of CTAs that have finished a phase.
+__device__ __forceinline__ void count_in(uint32_t *counter) { asm volatile("red.release.gpu.global.add.u32 [%0], 1;" :: "l"(counter) : "memory"); }
+__device__ __forceinline__ bool wait_for_count(const uint32_t *counter, uint32_t target, FusedShared *sh)
 {
-    uint32_t v;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
-// Adds one to a counter that others wait for, and waits until it has reached `target` (one thread; what its CTA wrote before is visible to whoever sees it).
-__device__ __forceinline__ void meet_at(uint32_t *counter, uint32_t target, FusedShared *sh)
-{
-    __threadfence();
-    atomicAdd(counter, 1u);
-    for (uint32_t poll = 0; poll < kPolls; ++poll)
-        if ((int32_t)(load_acquire(counter) - target) >= 0) return;
+    for (uint32_t poll = 0; poll < kPolls; ++poll) {
+        uint32_t v;
+        asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+        if ((int32_t)(v - target) >= 0) {
+            __threadfence();                                           // (what was written before the others' reports)
+            return true;
+        }
+        if (*(volatile int32_t *)&sh->abort) return false;
+    }
     atomicExch(&sh->abort, 1);
+    return false;
+}
+// The address of the same variable in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t team_addr(const void *p, int rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    return a;
+}
+// Four numbers to another CTA's shared memory, reported to its barrier when they are there.
+__device__ __forceinline__ void push(uint32_t to, uint32_t bar, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%2, %3, %4, %5}, [%1];" :: "r"(to), "r"(bar), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
 // The same descriptor as make_smem_desc for an operand whose k elements lie next to each other; for the other order boxes of 64 x 64 follow one another.
@@ -71,79 +88,20 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool across)
     return across ? (d & ~((uint64_t)0x3fff << 16)) | (uint64_t)(kBoxBytes >> 4) << 16 : d;
 }
 
-struct Phase {
-    int32_t M, N, slabs, splits, per;      // per: slabs of a piece
-    bool acrossA, acrossB, symmetric, residual, last;
-    int32_t stepA, stepB, stepOut;         // rows from matrix to matrix
-    int32_t tilesN, tiles;
-    float alpha, beta;
-    int32_t power;                         // of the matrix's factor, on alpha (and beta)
-    int kind;
-};
-__device__ __forceinline__ Phase phase_of(const FusedParams &p, int ph)
-{
-    Phase f{};
-    const int i = ph / 3, kind = ph - 3 * i;
-    const float down = 1.0f / (1 << kUp), *c = p.coefficients + 3 * i;
-    f.kind = kind;
-    f.splits = p.splits[kind];
-    f.symmetric = kind < 2;
-    f.residual = kind > 0;
-    f.last = ph == 3 * p.steps - 1;
-    if (kind == 0) {
-        f.M = f.N = p.side;
-        f.slabs = (p.tall ? p.rows : p.cols) / 64;
-        f.acrossA = f.acrossB = p.tall;
-        f.stepA = f.stepB = p.rows;
-        f.stepOut = p.side;
-        f.alpha = down;
-        f.power = i == 0 ? 2 : 0;
-    } else if (kind == 1) {
-        f.M = f.N = p.side;
-        f.slabs = p.side / 64;
-        f.stepA = f.stepB = f.stepOut = p.side;
-        f.alpha = c[2] * down;
-        f.beta = c[1];
-    } else {
-        f.M = p.rows;
-        f.N = p.cols;
-        f.slabs = p.side / 64;
-        f.acrossB = !p.tall;
-        f.stepA = p.tall ? p.rows : p.side;
-        f.stepB = p.tall ? p.side : p.rows;
-        f.stepOut = p.rows;
-        f.alpha = f.last ? down * down : down;
-        f.beta = f.last ? c[0] * down : c[0];
-        f.power = i == 0 ? 1 : 0;
-    }
-    const int32_t tilesM = (f.M + kRows - 1) / kRows;
-    f.tilesN = f.N / kCols;
-    f.tiles = f.symmetric ? tilesM * (tilesM + 1) : tilesM * f.tilesN;
-    f.per = (f.slabs + f.splits - 1) / f.splits;
-    return f;
-}
-__device__ __forceinline__ Unit tile_of(const Phase &f, int32_t u)
-{
-    const Walk w{0, f.tilesN, f.tiles, f.tilesN, f.splits, f.symmetric ? 1 : 0, f.symmetric ? 2 : 0};
-    if (f.symmetric) return unit_of(w, u);
-    Unit t{};
-    const int32_t piece = u / f.tiles, r = u - piece * f.tiles;
-    t.batch = piece / f.splits;
-    t.split = piece - t.batch * f.splits;
-    t.m = r / f.tilesN;
-    t.n = r - t.m * f.tilesN;
-    return t;
-}
-
-__global__ void __launch_bounds__(kThreads, 1) newton_schulz_kernel(const __grid_constant__ CUtensorMap mapX0, const __grid_constant__ CUtensorMap mapX1, const __grid_constant__ CUtensorMap mapA,
-                                                                     const __grid_constant__ CUtensorMap mapB, const __grid_constant__ FusedParams p)
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1)
+newton_schulz_kernel(const __grid_constant__ CUtensorMap mapX0, const __grid_constant__ CUtensorMap mapX1, const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+                     const __grid_constant__ FusedParams p)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
-    FusedShared &sh = *reinterpret_cast<FusedShared *>(smem + kStages * kStage);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float *const partial = reinterpret_cast<float *>(smem + kStages * kStage);
+    FusedShared &sh = *reinterpret_cast<FusedShared *>(smem + kStages * kStage + kPartial);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)(blockIdx.x % kCluster);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&sh.accFull[b], 1); mbar_init(&sh.accEmpty[b], kFinishers); }
+        mbar_init(&sh.partials, 1);
+        mbar_init(&sh.open, 1);
+        mbar_init(&sh.done, kFinishers);
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -151,30 +109,49 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_kernel(const __grid
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_addr(&sh.tmemBase)), "r"(2 * kCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    if (warp == 2 && lane < 3) {
+        // the tiles of this CTA, of each kind of phase (a tile in pieces: a team's)
+        const FusedPhase &f = p.phases[lane];
+        const Walk w{f.tiles / f.tilesN, f.tilesN, f.tiles, f.tilesN, 1, f.symmetric ? 1 : 0, f.symmetric ? 2 : 0};
+        const int tiles = f.tiles * p.batch, first = (int)blockIdx.x / f.team, step = (int)gridDim.x / f.team;
+        int n = 0;
+        for (int u = first; u < tiles && n < kFusedUnits; u += step) {
+            Unit t = unit_of(w, u % f.tiles);
+            t.batch = u / f.tiles;
+            sh.units[lane][n++] = t;
+        }
+        sh.count[lane] = n;
+    }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    cluster_barrier();                     // the team's barriers exist
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmemBase = sh.tmemBase;
-    const int first = (int)blockIdx.x, step = (int)gridDim.x, phases = 3 * p.steps;
+    const int phases = 3 * p.steps;
+    const float down = 1.0f / (1 << kUp);
 
-    int s = 0;                             // the ring's place and phase, the accumulators' turn: they go on from phase to phase
-    uint32_t parity = warp == 0 ? 1 : 0, nt = 0;
-    for (int ph = 0; ph < phases; ++ph) {
-        const Phase f = phase_of(p, ph);
-        const int i = ph / 3, units = f.tiles * f.splits * p.batch;
-        const __half *const x = (i & 1) ? p.x1 : p.x0;
-        if (warp == 0) {
-            // ---------------- operands ----------------
-            const CUtensorMap *const mapX = (i & 1) ? &mapX1 : &mapX0;
-            const CUtensorMap *const a = f.kind == 0 ? mapX : f.kind == 1 ? &mapA : p.tall ? mapX : &mapB;
-            const CUtensorMap *const b = f.kind == 0 ? mapX : f.kind == 1 ? &mapA : p.tall ? &mapB : mapX;
-            const bool leader = elect_one();
-            proxy_fence();
-            bool ok = true;
-            for (int u = first; u < units && ok; u += step) {
-                const Unit t = tile_of(f, u);
-                const int m0 = t.m * kRows, n0 = t.n * kCols, aRow = t.batch * f.stepA, bRow = t.batch * f.stepB, end = min(f.slabs, (t.split + 1) * f.per);
-                for (int kb = t.split * f.per; kb < end; ++kb) {
+    // Every role goes through the phases by itself; where it has waited in vain it leaves, and the others behind it.
+    if (warp == 0) {
+        // ---------------- operands; and whether the phase before is complete ----------------
+        const bool leader = elect_one();
+        int s = 0;
+        uint32_t parity = 1;
+        bool ok = true;
+        for (int ph = 0, kind = 0, odd = 0; ph < phases && ok; ++ph) {
+            const FusedPhase &f = p.phases[kind];
+            const CUtensorMap *const mapX = odd ? &mapX1 : &mapX0;
+            const CUtensorMap *const a = kind == 0 ? mapX : kind == 1 ? &mapA : p.tall ? mapX : &mapB;
+            const CUtensorMap *const b = kind == 0 ? mapX : kind == 1 ? &mapA : p.tall ? &mapB : mapX;
+            const int begin = rank % f.team * f.per, end = min(f.slabs, begin + f.per), count = sh.count[kind];
+            if (ph > 0) {
+                if (!__all_sync(0xffffffffu, wait_for_count(p.counter, (uint32_t)ph * gridDim.x, &sh))) break;
+                proxy_fence();                                         // (what was written there by ordinary stores is read by TMA from here on)
+                if (leader) mbar_arrive(&sh.open);
+            }
+            for (int n = 0; n < count && ok; ++n) {
+                const Unit t = sh.units[kind][n];
+                const int m0 = t.m * kRows, n0 = t.n * kCols, aRow = t.batch * f.stepA, bRow = t.batch * f.stepB;
+                for (int kb = begin; kb < end; ++kb) {
                     if (!warp_wait_for(&sh.empty[s], parity, &sh)) { ok = false; break; }
                     if (leader) {
                         unsigned char *const to = smem + s * kStage;
@@ -191,18 +168,23 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_kernel(const __grid
                     if (++s == kStages) { s = 0; parity ^= 1; }
                 }
             }
-        } else if (warp == 1) {
-            // ---------------- products ----------------
+            if (++kind == 3) { kind = 0; odd ^= 1; }
+        }
+    } else if (warp == 1) {
+        // ---------------- products ----------------
+        const bool leader = elect_one();
+        int s = 0;
+        uint32_t parity = 0, nt = 0;
+        bool ok = true;
+        for (int ph = 0, kind = 0; ph < phases && ok; ++ph) {
+            const FusedPhase &f = p.phases[kind];
             const uint32_t idesc = (1u << 4) | (f.acrossA ? 1u << 15 : 0u) | (f.acrossB ? 1u << 16 : 0u) | ((uint32_t)(kCols >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
-            const bool leader = elect_one();
             const uint64_t stepA = f.acrossA ? 128 : 2, stepB = f.acrossB ? 128 : 2;
-            bool ok = true;
-            for (int u = first; u < units && ok; u += step, ++nt) {
-                const Unit t = tile_of(f, u);
+            const int begin = rank % f.team * f.per, end = min(f.slabs, begin + f.per), count = sh.count[kind];
+            for (int n = 0; n < count && ok; ++n, ++nt) {
                 const uint32_t buf = nt & 1;
-                if (!warp_wait_for(&sh.accEmpty[buf], ((nt >> 1) & 1) ^ 1, &sh)) break;
+                if (!warp_wait_for(&sh.accEmpty[buf], ((nt >> 1) & 1) ^ 1, &sh)) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const int begin = t.split * f.per, end = min(f.slabs, begin + f.per);
                 for (int kb = begin; kb < end; ++kb) {
                     if (!warp_wait_for(&sh.full[s], parity, &sh)) { ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -219,25 +201,42 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_kernel(const __grid
                 if (leader) mma_commit(&sh.accFull[buf]);
                 __syncwarp();
             }
-        } else if (warp >= kFirstFinisher) {
-            // ---------------- finish: quarter q of the rows, half of the columns ----------------
-            const int q = warp & 3, half = (warp - kFirstFinisher) >> 2;
-            for (int u = first; u < units; u += step, ++nt) {
-                const Unit t = tile_of(f, u);
+            if (++kind == 3) kind = 0;
+        }
+    } else if (warp == 2) {
+        // ---------------- one report per CTA and phase (eight, from every warp that finishes, queue up at the counter: 2 us with 128 CTAs) ----------------
+        for (int ph = 0; ph + 1 < phases; ++ph) {
+            if (!warp_wait_for(&sh.done, ph & 1, &sh)) break;
+            if (lane == 0) count_in(p.counter);
+        }
+    } else if (warp >= kFirstFinisher) {
+        // ---------------- finish: quarter q of the rows, half of the columns ----------------
+        const int q = warp & 3, half = (warp - kFirstFinisher) >> 2, me = (int)threadIdx.x - 32 * kFirstFinisher;
+        uint32_t nt = 0, shares = 0;
+        bool ok = true;
+        for (int ph = 0, kind = 0, odd = 0; ph < phases && ok; ++ph) {
+            const FusedPhase &f = p.phases[kind];
+            const bool last = ph == phases - 1, residualWanted = kind > 0;
+            const float *const c = p.coefficients + ph - kind;
+            const float alpha0 = kind == 0 ? down : kind == 1 ? c[2] * down : last ? down * down : down, beta0 = kind == 1 ? c[1] : last ? c[0] * down : c[0];
+            const int64_t square = (int64_t)p.side * p.side, whole = (int64_t)p.rows * p.cols;
+            const int count = sh.count[kind];
+            if (ph > 0 && !warp_wait_for(&sh.open, (ph - 1) & 1, &sh)) break;
+            for (int n = 0; n < count && ok; ++n, ++nt) {
+                const Unit t = sh.units[kind][n];
                 const uint32_t buf = nt & 1;
-                const float factor = f.power ? p.factor[t.batch] : 1.0f;
-                const float alpha = f.alpha * (f.power == 2 ? factor * factor : factor), beta = f.beta * factor;
+                const float factor = ph < 3 && kind != 1 ? p.factor[t.batch] : 1.0f;        // (of the first step: G is brought up by a power of two alone)
+                const float alpha = kind == 0 ? alpha0 * (factor * factor) : alpha0 * factor, beta = beta0 * factor;
                 const int row0 = t.m * kRows, col0 = t.n * kCols;
-                const __half *const from = f.kind == 1 ? p.a + (int64_t)t.batch * p.side * p.side : x + (int64_t)t.batch * p.rows * p.cols;       // residual: [M][N]
-                __half *const to = f.kind == 0 ? p.a + (int64_t)t.batch * p.side * p.side
-                                   : f.kind == 1 ? p.b + (int64_t)t.batch * p.side * p.side : ((i & 1) ? p.x0 : p.x1) + (int64_t)t.batch * p.rows * p.cols;
-                // eight neighbours of a row, from fp32 sums on
+                const __half *const from = kind == 1 ? p.a + t.batch * square : (odd ? p.x1 : p.x0) + t.batch * whole;      // residual: [M][N]
+                __half *const to = kind == 0 ? p.a + t.batch * square : kind == 1 ? p.b + t.batch * square : (odd ? p.x0 : p.x1) + t.batch * whole;
                 auto residual_of = [&](int row, int col) { return __ldcg(reinterpret_cast<const uint4 *>(from + (int64_t)row * f.N + col)); };
+                // eight neighbours of a row, from fp32 sums on
                 auto put = [&](int row, int col, float (&z)[8], const uint4 &r) {
                     const int64_t at = (int64_t)row * f.N + col;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) z[j] *= alpha;
-                    if (f.residual) {
+                    if (residualWanted) {
                         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -246,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_kernel(const __grid
                             z[2 * j + 1] = fmaf(beta, v.y, z[2 * j + 1]);
                         }
                     }
-                    if (f.last) {
+                    if (last) {
                         __nv_bfloat16 *const o = p.o + t.batch * p.stepO + (int64_t)row * p.ldO + col;
                         if (row >= p.rowsO) return;
                         if (col + 8 <= p.colsO && ((uintptr_t)o) % 16 == 0) store_pack<8>(o, z);
@@ -263,75 +262,65 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_kernel(const __grid
                 const int row = row0 + q * 32 + lane;
                 const bool inside = row < f.M && col0 < f.N;           // (a diagonal block's second tile may lie behind the last column)
                 uint4 residual[4] = {};
-                if (f.residual && f.splits == 1 && inside) {
+                if (residualWanted && f.team == 1 && inside) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) residual[c] = residual_of(row, col0 + half * 32 + 8 * c);
+                    for (int k = 0; k < 4; ++k) residual[k] = residual_of(row, col0 + half * 32 + 8 * k);
                 }
-                const bool ok = warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh);
+                if (!warp_wait_for(&sh.accFull[buf], (nt >> 1) & 1, &sh)) { ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 uint32_t v[32];
-                if (ok) {
-                    tmem_load_32cols(tmemBase + buf * kCols + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * 32), v);
-                    tmem_load_wait();
-                }
+                tmem_load_32cols(tmemBase + buf * kCols + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * 32), v);
+                tmem_load_wait();
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.accEmpty[buf]);
-                if (f.splits == 1) {
-                    if (ok && inside) {
+                if (f.team == 1) {
+                    if (inside) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
+                        for (int k = 0; k < 4; ++k) {
                             float z[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(v[8 * c + j]);
-                            put(row, col0 + half * 32 + 8 * c, z, residual[c]);
+                            for (int j = 0; j < 8; ++j) z[j] = __uint_as_float(v[8 * k + j]);
+                            put(row, col0 + half * 32 + 8 * k, z, residual[k]);
                         }
                     }
                 } else {
-                    // (units are no more than CTAs here: whoever shares the tile is at work)
-                    const int64_t tile = (int64_t)t.batch * f.tiles + (u % f.tiles), size = kRows * kCols;
-                    float *const parts = p.parts + tile * f.splits * size;
-                    if (ok) {
-                        float4 *const mine = reinterpret_cast<float4 *>(parts + t.split * size + (q * 32 + lane) * kCols + half * 32);
+                    // Each of the team finishes its share of the rows, whole quarters: all send it their pieces' sums of them (16 bytes at a time, turned by the row: no bank
+                    // twice).  One tile per team and phase: a phase has ended on all SMs between two uses of the place.
+                    if (me == 0) mbar_expect_tx(&sh.partials, kPartial);
+                    const int team = f.team, share = kRows / team, member = rank % team, source = kPartial / 4 / team;       // source: floats that come from one of the team
+                    const int owner = rank - member + q * team / 4, at = (q % (4 / team)) * 32 + lane;
+                    const uint32_t to = team_addr(partial + member * source + at * kCols, owner), bar = team_addr(&sh.partials, owner);
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) mine[c] = make_float4(__uint_as_float(v[4 * c]), __uint_as_float(v[4 * c + 1]), __uint_as_float(v[4 * c + 2]), __uint_as_float(v[4 * c + 3]));
-                    }
-                    asm volatile("bar.sync 1, %0;" :: "n"(32 * kFinishers) : "memory");
-                    const int me = (int)threadIdx.x - 32 * kFirstFinisher;
-                    if (me == 0) meet_at(p.counters + 1 + f.kind * kFusedTileCounters + tile, (uint32_t)((i + 1) * f.splits), &sh);
-                    asm volatile("bar.sync 1, %0;" :: "n"(32 * kFinishers) : "memory");
-                    if (!*(volatile int32_t *)&sh.abort) {
-                        const int share = (kRows + f.splits - 1) / f.splits, r0 = t.split * share, r1 = min(kRows, r0 + share);
-                        for (int e = me; e < (r1 - r0) * (kCols / 8); e += 32 * kFinishers) {
-                            const int r = r0 + e / (kCols / 8), c = e % (kCols / 8) * 8;
-                            if (row0 + r >= f.M || col0 >= f.N) continue;
-                            const uint4 r0c = f.residual ? residual_of(row0 + r, col0 + c) : uint4{};
-                            float z[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                            for (int k = 0; k < f.splits; ++k) {
-                                const float4 *const at = reinterpret_cast<const float4 *>(parts + k * size + r * kCols + c);
-                                const float4 lo = __ldcg(at), hi = __ldcg(at + 1);
-                                z[0] += lo.x; z[1] += lo.y; z[2] += lo.z; z[3] += lo.w;
-                                z[4] += hi.x; z[5] += hi.y; z[6] += hi.z; z[7] += hi.w;
-                            }
-                            put(row0 + r, col0 + c, z, r0c);
+                    for (int k = 0; k < 8; ++k) push(to + (((half * 8 + k) ^ (lane & 15)) << 4), bar, v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                    if (!warp_wait_for(&sh.partials, shares & 1, &sh)) { ok = false; break; }
+                    ++shares;
+                    const int col = me % (kCols / 8) * 8;              // 256 threads: 32 rows of 8 times 8 columns at a time
+                    for (int r = me / (kCols / 8); r < share; r += 32) {
+                        const int mine = row0 + member * share + r;
+                        if (mine >= f.M || col0 >= f.N) break;
+                        const uint4 old = residualWanted ? residual_of(mine, col0 + col) : uint4{};
+                        float z[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                        for (int k = 0; k < team; ++k) {
+                            const float *const from = partial + k * source + r * kCols;
+                            const float4 lo = *reinterpret_cast<const float4 *>(from + (((col / 4) ^ (r & 15)) << 2)), hi = *reinterpret_cast<const float4 *>(from + (((col / 4 + 1) ^ (r & 15)) << 2));
+                            z[0] += lo.x; z[1] += lo.y; z[2] += lo.z; z[3] += lo.w;
+                            z[4] += hi.x; z[5] += hi.y; z[6] += hi.z; z[7] += hi.w;
                         }
+                        put(mine, col0 + col, z, old);
                     }
                 }
             }
-            proxy_fence();                                             // (the next phase reads by TMA what was written here)
+            if (!ok || last) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.done);
+            if (++kind == 3) { kind = 0; odd ^= 1; }
         }
-        if (ph == phases - 1) break;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            meet_at(p.counters, (uint32_t)(ph + 1) * gridDim.x, &sh);
-            sh.leave = *(volatile int32_t *)&sh.abort;
-        }
-        __syncthreads();
-        if (*(volatile int32_t *)&sh.leave) break;
     }
     if (*(volatile int32_t *)&sh.abort) let_copies_land();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    cluster_barrier();                     // nobody reads this CTA's place any more
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmemBase), "r"(2 * kCols) : "memory");
@@ -341,30 +330,62 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_kernel(const __grid
 
 }  // namespace
 
-// Pieces: the least of slabs (a quarter of a microsecond each) and of what a tile in pieces takes besides.
-FusedPlan fused_plan(const rcd_ctx *ctx, int64_t batch, int64_t rows, int64_t cols)
+// Clusters that the device takes at once (some of its groups of SMs are not whole fours).
+static int teams_of(rcd_ctx *ctx)
+{
+    if (ctx->fusedTeams < 0) {
+        ctx->fusedTeams = 0;
+        if (!ctx->cooperative || allow_shared(newton_schulz_kernel, kSharedBytes) != cudaSuccess) return 0;
+        cudaLaunchConfig_t config{};
+        config.gridDim = dim3((unsigned)(ctx->smCount / kCluster * kCluster));
+        config.blockDim = dim3(kThreads);
+        config.dynamicSmemBytes = kSharedBytes;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel, &config) == cudaSuccess) ctx->fusedTeams = std::min(n, ctx->smCount / kCluster);
+        else cudaGetLastError();
+    }
+    return ctx->fusedTeams;
+}
+
+FusedPlan fused_plan(rcd_ctx *ctx, int64_t batch, int64_t rows, int64_t cols, bool tall)
 {
     FusedPlan f{};
-    const int64_t side = std::min(rows, cols), tilesSide = (side + kRows - 1) / kRows;
-    const int64_t tiles[3] = {batch * tilesSide * (tilesSide + 1), batch * tilesSide * (tilesSide + 1), batch * ((rows + kRows - 1) / kRows) * (cols / kCols)};
-    const int64_t slabs[3] = {std::max(rows, cols) / 64, side / 64, side / 64};
+    const int teams = teams_of(ctx);
+    const int64_t side = std::min(rows, cols), sideTiles = (side + kRows - 1) / kRows;
+    if (teams == 0 || side > 4096 || rows > (1 << 20) || cols > (1 << 20)) return f;
+    const int64_t ctas = (int64_t)teams * kCluster;
     int64_t most = 0;
     for (int k = 0; k < 3; ++k) {
+        FusedPhase &ph = f.phases[k];
+        ph.symmetric = k < 2;
+        ph.M = (int32_t)(k < 2 ? side : rows);
+        ph.N = (int32_t)(k < 2 ? side : cols);
+        ph.slabs = (int32_t)((k == 0 ? std::max(rows, cols) : side) / 64);
+        ph.acrossA = k == 0 && tall;
+        ph.acrossB = k == 0 ? tall : k == 2 && !tall;
+        ph.stepA = (int32_t)(k == 0 ? rows : k == 1 ? side : tall ? rows : side);
+        ph.stepB = (int32_t)(k == 0 ? rows : k == 1 ? side : tall ? side : rows);
+        ph.tilesN = (int32_t)(ph.N / kCols);
+        const int64_t tiles = k < 2 ? sideTiles * (sideTiles + 1) : (rows + kRows - 1) / kRows * (cols / kCols);
+        if (tiles * batch > ctas * kFusedUnits) return FusedPlan{};
+        ph.tiles = (int32_t)tiles;
+        // A phase takes 2.7 us besides its slabs of 0.36 each (the barrier over the grid 1.6, the first slab's way and the last tile's end); a tile in pieces 1.8 more.
         double least = 1e300;
-        for (int64_t s = 1; s <= slabs[k] && s <= 16; ++s) {
-            if (s > 1 && (tiles[k] * s > ctx->smCount || tiles[k] > kFusedTileCounters)) break;
-            if (s > 1 && (s - 1) * ((slabs[k] + s - 1) / s) >= slabs[k]) continue;       // (an empty piece)
-            const double t = 0.25 * (double)((slabs[k] + s - 1) / s) + (s > 1 ? 1.8 : 0.0);
+        for (int team = 1; team <= kCluster; team *= 2) {
+            const int64_t per = (ph.slabs + team - 1) / team;
+            if (team > 1 && (tiles * batch * team > ctas || (team - 1) * per >= ph.slabs)) continue;       // (a tile for every team, and no empty piece)
+            const double t = 2.7 + (double)((tiles * batch * team + ctas - 1) / ctas) * 0.36 * (double)per + (team > 1 ? 1.8 : 0.0);
             if (t < least) {
                 least = t;
-                f.splits[k] = (int32_t)s;
+                ph.team = team;
+                ph.per = (int32_t)per;
             }
         }
-        most = std::max(most, tiles[k] * f.splits[k]);
-        if (f.splits[k] > 1) f.parts = std::max(f.parts, (size_t)(tiles[k] * f.splits[k]) * kFusedTile);
+        f.stepUs += least;
+        most = std::max(most, tiles * batch * ph.team);
     }
-    f.grid = (int32_t)std::min<int64_t>(most, ctx->smCount);
-    f.use = ctx->cooperative && FUSED_RULE;
+    f.grid = (int32_t)(std::min<int64_t>((most + kCluster - 1) / kCluster, teams) * kCluster);
+    f.possible = true;
     return f;
 }
 
@@ -382,10 +403,6 @@ rcd_status launch_fused(rcd_ctx *ctx, const FusedParams &p, const FusedPlan &pla
         const CUresult cr = fn(&maps[k], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base[k], dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
         if (cr != CUDA_SUCCESS) return fail(ctx, RCD_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)cr);
-    }
-    if (!ctx->fusedReady) {
-        RCD_CUDA(ctx, allow_shared(newton_schulz_kernel, kSharedBytes));
-        ctx->fusedReady = true;
     }
     void *args[5] = {&maps[0], &maps[1], &maps[2], &maps[3], const_cast<FusedParams *>(&p)};
     ctx->kernelLaunches++;
