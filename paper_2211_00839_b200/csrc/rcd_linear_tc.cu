@@ -21,6 +21,7 @@ __global__ void __launch_bounds__(256) join_kernel(const void *__restrict__ part
     float z[4];
     if constexpr (kInt8) {
         int4 s = make_int4(0, 0, 0, 0);
+#pragma unroll 8
         for (int k = 0; k < splits; ++k) {
             const int4 x = __ldcs((const int4 *)((const int32_t *)parts + (k * rowsPart + m) * ld + n));
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
@@ -28,6 +29,7 @@ __global__ void __launch_bounds__(256) join_kernel(const void *__restrict__ part
         z[0] = (float)s.x; z[1] = (float)s.y; z[2] = (float)s.z; z[3] = (float)s.w;
     } else {
         float4 s = make_float4(0, 0, 0, 0);
+#pragma unroll 8
         for (int k = 0; k < splits; ++k) {
             const float4 x = __ldcs((const float4 *)((const float *)parts + (k * rowsPart + m) * ld + n));
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;

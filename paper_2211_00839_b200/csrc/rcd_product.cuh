@@ -132,6 +132,25 @@ __device__ __forceinline__ void move_piece(unsigned char *piece, T *at, int64_t 
     constexpr int kCols = 128 / sizeof(T);
     const int lane = threadIdx.x & 31;
     rows = min(rows, 32);
+    if constexpr (!kLoad && sizeof(T) == 2) {
+        // Two elements in a store wherever a row starts: it is the stores that take the time.
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+#pragma unroll
+            for (int r = r0; r < r0 + 8; ++r) {
+                if (r >= rows) break;
+                T *const row = at + (int64_t)r * ld;
+                const int odd = (int)((uintptr_t)row >> 1 & 1), col = 2 * lane - odd;
+                auto here = [&](int c) { return *reinterpret_cast<const T *>(piece + piece_at(r, c >> 3) + (c & 7) * 2); };
+                if (col >= 0 && col + 1 < cols) *reinterpret_cast<uint32_t *>(row + col) = (uint32_t)here(col) | (uint32_t)here(col + 1) << 16;
+                else if (col >= 0 && col < cols) row[col] = here(col);
+                else if (col < 0) {                                    // (the first lane: the row's first element and, of a whole piece, its last)
+                    if (cols > 0) row[0] = here(0);
+                    if (cols > kCols - 1) row[kCols - 1] = here(kCols - 1);
+                }
+            }
+        }
+        return;
+    }
     // (eight rows' accesses under way at once)
     for (int r0 = 0; r0 < rows; r0 += 8) {
         T v[8][kCols / 32];
