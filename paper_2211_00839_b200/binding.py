@@ -744,8 +744,7 @@ class Context:
             b = self._vector(bias, "bias", n, torch.float32)
             a.bias = b.data_ptr()
             keep.append(b)
-        loss = torch.empty(shape, dtype=torch.float32, device=self.torch_device)
-        lse = torch.empty(shape, dtype=torch.float32, device=self.torch_device)
+        loss, lse = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
         a.loss, a.lse = loss.data_ptr(), lse.data_ptr()
         need = C.c_size_t()
         self._check(lib.rcd_linear_cross_entropy_workspace_bytes(self._h, C.byref(a), C.byref(need)))
@@ -784,15 +783,15 @@ class Context:
             keep.append(b)
         dx = dw = db = None
         if want_dx:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=self.torch_device)
+            dx = x.new_empty(x.shape)
             a.dx, a.ld_dx = dx.data_ptr(), k
         kind = x.dtype if dw_dtype is None else dw_dtype
         a.dw_type = _elem(kind, "dw_dtype")
         if want_dw:
-            dw = torch.empty((n, k), dtype=kind, device=self.torch_device)
+            dw = w.new_empty((n, k)) if kind == w.dtype else w.new_empty((n, k), dtype=kind)
             a.dw, a.ld_dw = dw.data_ptr(), k
         if want_dbias:
-            db = torch.empty(n, dtype=torch.float32, device=self.torch_device)
+            db = x.new_empty(n, dtype=torch.float32)
             a.dbias = db.data_ptr()
         need = C.c_size_t()
         self._check(lib.rcd_linear_cross_entropy_backward_workspace_bytes(self._h, C.byref(a), C.byref(need)))
@@ -810,36 +809,45 @@ class Context:
             raise ValueError("g is on %s, the context on %s" % (g.device, self.torch_device))
         if g.dim() < 2:
             raise ValueError("g must be [..., rows, cols], got shape %s" % (tuple(g.shape),))
-        c = np.ascontiguousarray(coefficients, dtype=np.float32)
-        if c.shape == (3,):
-            c = np.ascontiguousarray(np.broadcast_to(c, (max(int(steps), 0), 3)))
-        if c.shape != (max(int(steps), 0), 3):
+        steps = int(steps)
+        each = tuple(coefficients)
+        if len(each) == 3 and not hasattr(each[0], "__len__"):
+            each = (each,) * max(steps, 0)
+        if len(each) != max(steps, 0) or any(len(c) != 3 for c in each):
             raise ValueError("coefficients must be (a, b, c), or %d of them" % steps)
+        c = (C.c_float * (3 * len(each)))(*(v for abc in each for v in abc))
 
         def matrices(t):
-            """[batch, rows, cols] of it with dense rows, as it lies."""
-            v = t if t.dim() == 3 else t.unsqueeze(0) if t.dim() == 2 else t.flatten(0, -3)
-            s0, s1, s2 = v.stride()
-            rows, cols = v.shape[1:]
-            dense = (cols <= 1 or s2 == 1) and (rows <= 1 or s1 >= cols) and (v.shape[0] <= 1 or s0 >= max(rows - 1, 0) * max(s1, cols) + cols)
-            ld = max(s1, cols) if rows > 1 else cols
-            return v, dense, ld, s0 if v.shape[0] > 1 else rows * ld
+            """(tensor, batch, elements from row to row and from matrix to matrix) of [..., rows, cols] as it lies, or None where its rows are not dense or its
+            matrices not equally far apart."""
+            rows, cols = t.shape[-2:]
+            if t.is_contiguous():
+                return t, math.prod(t.shape[:-2]), max(cols, 1), rows * cols
+            if t.dim() > 3:
+                v = t.flatten(0, -3)
+                if v.data_ptr() != t.data_ptr():              # (a copy: no view of it has one leading dimension)
+                    return None
+                t = v
+            s1, s2 = t.stride()[-2:]
+            batch, s0 = (t.shape[0], t.stride(0)) if t.dim() == 3 else (1, 0)
+            ld = max(s1, cols, 1) if rows > 1 else max(cols, 1)
+            if (cols > 1 and s2 != 1) or (rows > 1 and s1 < cols) or (batch > 1 and s0 < (rows - 1) * ld + cols):
+                return None
+            return t, batch, ld, s0 if batch > 1 else rows * ld
 
         a = RcdOrthogonalizeArgs()
-        v, dense, ld, step = matrices(g)
-        if not dense:
-            v, _, ld, step = matrices(v.contiguous())
-        a.batch, a.rows, a.cols = v.shape
-        a.type, a.g, a.ld_g, a.step_g, a.eps, a.steps = _elem(g.dtype, "g"), v.data_ptr(), ld, step, eps, steps
-        a.coefficients_host = c.ctypes.data
+        v, a.batch, a.ld_g, a.step_g = matrices(g) or matrices(g.contiguous())
+        a.rows, a.cols = g.shape[-2:]
+        a.type, a.g, a.eps, a.steps, a.coefficients_host = _elem(g.dtype, "g"), v.data_ptr(), eps, steps, C.addressof(c)
         if out is None:
-            out = torch.empty(g.shape, dtype=torch.bfloat16, device=self.torch_device)
+            out = g.new_empty(g.shape, dtype=torch.bfloat16)
         elif out.device != self.torch_device or out.dtype != torch.bfloat16 or out.shape != g.shape:
             raise ValueError("out must be bfloat16 of shape %s on %s" % (tuple(g.shape), self.torch_device))
-        o, dense, a.ld_o, a.step_o = matrices(out)
-        if not dense or (out.numel() and o.data_ptr() != out.data_ptr()):
+        o = matrices(out)
+        if o is None:
             raise ValueError("out: the elements of a row must lie next to each other, and its matrices equally far apart")
-        a.o = o.data_ptr()
+        _, _, a.ld_o, a.step_o = o
+        a.o = out.data_ptr()
         need = C.c_size_t()
         self._check(lib.rcd_orthogonalize_workspace_bytes(self._h, C.byref(a), C.byref(need)))
         ws = self._scratch(need.value)

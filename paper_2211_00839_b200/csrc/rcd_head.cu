@@ -184,6 +184,7 @@ int64_t piece_of(const rcd_cross_entropy_back_args &a)
 struct BackPlan {
     int64_t piece, pieces, ldDz, ldSum;
     bool sumDx;                            // dx of several pieces: in fp32
+    bool sumRows;                          // dbias: over groups of 32 rows, where there are several
     bool packX, packW;                     // copies whose rows start on 16 bytes, which all products read
     int64_t ldPacked;
     size_t dz, sum, sums, up, x, w, product, bytes;
@@ -199,11 +200,12 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a, unsigned 
     b.ldDz = (b.piece + 63) / 64 * 64;
     b.ldSum = (a.k + 3) / 4 * 4;
     b.sumDx = a.dx_dev_or_null && b.pieces > 1;
+    b.sumRows = a.dbias_dev_or_null && a.rows > 32;
     size_t at = 0;
     auto place = [&](bool wanted, size_t bytes) { const size_t here = at; if (wanted) at += align_up(bytes); return here; };
     b.dz = place(true, (size_t)(a.rows * b.ldDz) * 2);
     b.sum = place(b.sumDx, (size_t)(a.rows * b.ldSum) * 4);
-    b.sums = place(a.dbias_dev_or_null, (size_t)((a.rows + 31) / 32 * b.piece) * 4);
+    b.sums = place(b.sumRows, (size_t)((a.rows + 31) / 32 * b.piece) * 4);
     b.up = place(a.type == RCD_ELEM_F16, 8);
     b.packX = !rows_mappable(a.x_dev, a.ldx, eb);
     b.packW = !rows_mappable(a.w_dev, a.ldw, eb);
@@ -224,7 +226,7 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a, unsigned 
     b.z.head.dloss = a.dloss_dev_or_null;
     b.z.head.dlse = a.dlse_dev_or_null;
     b.z.head.up = up;
-    b.z.head.sums = a.dbias_dev_or_null ? (float *)(ws + b.sums) : nullptr;
+    b.z.head.sums = b.sumRows ? (float *)(ws + b.sums) : a.dbias_dev_or_null ? a.dbias_dev_or_null + first : nullptr;
     // (fp16: the power of two is taken out again)
     b.dx.type = b.dw.type = a.type;
     b.dx.form = b.dw.form = up ? kScaled : kPlain;
@@ -339,7 +341,7 @@ extern "C" rcd_status rcd_linear_cross_entropy_backward(rcd_ctx *ctx, const rcd_
         if (i) b = back_plan(ctx, a, ws, i * b.piece);
         if (b.packW) RCD_TRY(launch_pack(ctx, (const unsigned char *)a.w_dev + i * b.piece * a.ldw * eb, a.ldw, b.z.N, a.k, eb, ws + b.w, b.ldPacked, st));
         RCD_TRY(launch_product(ctx, b.z, ws + b.product, st));
-        if (a.dbias_dev_or_null) RCD_TRY(launch_column_sums(ctx, b.z.head.sums, (a.rows + 31) / 32, b.z.N, a.dbias_dev_or_null + i * b.piece, st));
+        if (b.sumRows) RCD_TRY(launch_column_sums(ctx, b.z.head.sums, (a.rows + 31) / 32, b.z.N, a.dbias_dev_or_null + i * b.piece, st));
         if (a.dx_dev_or_null) RCD_TRY(launch_product(ctx, b.dx, ws + b.product, st));
         if (a.dw_dev_or_null) RCD_TRY(launch_product(ctx, b.dw, ws + b.product, st));
     }

@@ -54,9 +54,9 @@ __device__ __forceinline__ bool elect_one()
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async;" ::: "memory"); }
 // The grid's barrier: a count of CTAs that have finished a phase.
 __device__ __forceinline__ void count_in(uint32_t *counter) { asm volatile("red.release.gpu.global.add.u32 [%0], 1;" :: "l"(counter) : "memory"); }
-__device__ __forceinline__ bool wait_for_count(const uint32_t *counter, uint32_t target, FusedShared *sh)
+__device__ __forceinline__ bool wait_for_count(const uint32_t *counter, uint32_t target, FusedShared *sh, uint32_t polls = kPolls)
 {
-    for (uint32_t poll = 0; poll < kPolls; ++poll) {
+    for (uint32_t poll = 0; poll < polls; ++poll) {
         uint32_t v;
         asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
         if ((int32_t)(v - target) >= 0) {
@@ -328,7 +328,32 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap mapX0, const __grid_con
     if (threadIdx.x == 0 && sh.abort) atomicOr(p.status, kDevTimeout);
 }
 
+// The waits of all steps in one launch for a count that nobody reaches and for an arrival that nobody makes: the first has to run out for every thread, and the one
+// behind it to be given up at once.
+__global__ void __launch_bounds__(64) fused_wait_selftest_kernel(uint32_t *counter, int32_t *status)
+{
+    __shared__ FusedShared sh;
+    if (threadIdx.x == 0) {
+        sh.abort = 0;
+        mbar_init(&sh.open, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    const bool came = wait_for_count(counter, *(volatile uint32_t *)counter + 1, &sh, 1u << 10);
+    const bool then = wait_for(&sh.open, 0, &sh);
+    const bool wrong = __syncthreads_or(came || then);
+    if (threadIdx.x == 0) atomicOr(status, wrong || !sh.abort ? kDevBadState : kDevTimeout);
+}
+
 }  // namespace
+
+rcd_status launch_fused_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st)
+{
+    fused_wait_selftest_kernel<<<1, 64, 0, st>>>((uint32_t *)ctx->statusOwn + kSelftestCount, status);
+    ctx->kernelLaunches++;
+    RCD_CUDA(ctx, cudaGetLastError());
+    return RCD_OK;
+}
 
 // Clusters that the device takes at once (some of its groups of SMs are not whole fours).
 static int teams_of(rcd_ctx *ctx)

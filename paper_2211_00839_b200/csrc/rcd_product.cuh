@@ -34,14 +34,13 @@ constexpr int kEpiWarps = 8;
 // fp32 outputs: 512 k (2.4e-6 within a chunk, bf16 2.3e-7, and half a unit of fp32 at most for each of them).  16-bit outputs: 2048 k (1.3e-5)
 // where a piece has more than 4096, up to which the loss is a twentieth of fp16's half step.  (Gradients of 2048 x 2048 weights over 600 000
 // rows: 3.56 ms in chunks, 3.45 in one sum.)
-#ifndef CS
-#define CS 4
-#endif
-constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32, kChunkSlabsSums = CS;
+// Logits whose gradients are summed over the rows in fp32 (a head's dbias, where p and the labels nearly cancel): 256 k.  Of 5000 x 2048 over 1000 classes dbias is
+// 1.5e-5 off in one sum, 3.3e-6 in chunks of 512, 1.6e-6 of 256, 7.8e-7 of 128 (fp32 products 8e-7); the call takes 89, 96, 99 and 106 us.
+constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32, kChunkSlabsSums = 4;
 constexpr int kFirstEpiWarp = 4;                        // (a warpgroup for the two that issue: registers are handed over by warpgroups)
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
-// Registers per thread at launch (65536 over 12 warps in whole eights), and how the warpgroups split them: 128 x 40 + 256 x 232 = 384 x 168.  (168 for
-// all left a third of the sums of chunks in local memory, whose way is the one that operands come by: DESCRIBE.)
+// Registers per thread at launch (65536 over 12 warps in whole eights), and how the warpgroups split them: 128 x 40 + 256 x 232 = 384 x 168.  (With 168 for all, sums of
+// chunks leave the registers at their ends: gradients of 5000 x 2048 over 1000 classes 100 us for 98, of 8192 x 4096 over 8192 with dbias 1257 for 1232.)
 constexpr int kLaunchRegs = 168, kIssueRegs = 40, kEpiRegs = 232;
 static_assert(128 * kIssueRegs + 32 * kEpiWarps * kEpiRegs <= kThreads * kLaunchRegs, "what one warpgroup gets the other has to have given");
 constexpr int kPiece = 32 * 128;                        // an epilogue warp's piece of the output: 32 rows of 128 bytes
@@ -149,26 +148,26 @@ __device__ __forceinline__ void move_piece(unsigned char *piece, T *at, int64_t 
                 }
             }
         }
-        return;
-    }
-    // (eight rows' accesses under way at once)
-    for (int r0 = 0; r0 < rows; r0 += 8) {
-        T v[8][kCols / 32];
-        auto each = [&](auto go) {
+    } else {
+        // (eight rows' accesses under way at once)
+        for (int r0 = 0; r0 < rows; r0 += 8) {
+            T v[8][kCols / 32];
+            auto each = [&](auto go) {
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
+                for (int r = 0; r < 8; ++r)
 #pragma unroll
-                for (int c = 0; c < kCols / 32; ++c) {
-                    const int row = r0 + r, col = c * 32 + lane;
-                    if (row < rows && col < cols) go(v[r][c], *reinterpret_cast<T *>(piece + piece_at(row, col * (int)sizeof(T) / 16) + col * (int)sizeof(T) % 16), at[(int64_t)row * ld + col]);
-                }
-        };
-        if constexpr (kLoad) {
-            each([](T &x, T &, T &there) { x = there; });
-            each([](T &x, T &here, T &) { here = x; });
-        } else {
-            each([](T &x, T &here, T &) { x = here; });
-            each([](T &x, T &, T &there) { there = x; });
+                    for (int c = 0; c < kCols / 32; ++c) {
+                        const int row = r0 + r, col = c * 32 + lane;
+                        if (row < rows && col < cols) go(v[r][c], *reinterpret_cast<T *>(piece + piece_at(row, col * (int)sizeof(T) / 16) + col * (int)sizeof(T) % 16), at[(int64_t)row * ld + col]);
+                    }
+            };
+            if constexpr (kLoad) {
+                each([](T &x, T &, T &there) { x = there; });
+                each([](T &x, T &here, T &) { here = x; });
+            } else {
+                each([](T &x, T &here, T &) { x = here; });
+                each([](T &x, T &, T &there) { there = x; });
+            }
         }
     }
 }
