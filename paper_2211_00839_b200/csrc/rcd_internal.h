@@ -270,7 +270,7 @@ struct rcd_ctx {
     unsigned simReady = 0;              // tensor-core similarity kernels whose shared memory has been asked for, a bit each
     uint64_t productReady = 0;          // the same of rcd_linear's kernels
     alignas(16) unsigned char productPlans[4096] = {};   // how rcd_linear goes about the last few sizes
-    int fusedTeams = -1;                // clusters of rcd_orthogonalize's kernel of all steps resident at once (-1: not asked yet)
+    int fusedCtas[3] = {-1, -1, -1};    // CTAs of rcd_orthogonalize's kernel of all steps resident at once, in clusters of 1, 2 and 4 (-1: not asked yet)
     unsigned simTurn = 0;               // similarity launches so far: each takes the next ticket
     size_t hostStageInts = 0;
     unsigned char *hostBlob = nullptr;  // pinned, what a call's host side hands to its kernels

@@ -314,6 +314,7 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
         p.rows = (int32_t)l.rows; p.cols = (int32_t)l.cols; p.side = (int32_t)l.side;
         p.batch = (int32_t)a.batch;
         p.steps = a.steps;
+        p.cluster = l.fused.cluster;
         p.tall = l.tall;
         for (int k = 0; k < 3; ++k) p.phases[k] = l.fused.phases[k];
         p.status = ctx->statusOwn + kOperatorStatus;

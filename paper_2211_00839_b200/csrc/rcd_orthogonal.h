@@ -17,7 +17,7 @@ struct FusedPhase {
     bool acrossA, acrossB, symmetric;
 };
 constexpr int kFusedUnits = 8;             // tiles per CTA and phase at most
-struct FusedPlan { bool possible; int32_t grid; double stepUs; FusedPhase phases[3]; };        // stepUs: an estimate
+struct FusedPlan { bool possible; int32_t grid, cluster; double stepUs; FusedPhase phases[3]; };        // stepUs: an estimate
 struct FusedParams {
     __half *x0, *x1, *a, *b;               // [batch][rows][cols] twice, [batch][side][side] twice; whole 64s
     const float *factor;                   // [batch], of the first step
@@ -25,7 +25,7 @@ struct FusedParams {
     __nv_bfloat16 *o;
     int64_t ldO, stepO;
     int32_t rowsO, colsO;                  // of the output
-    int32_t rows, cols, side, batch, steps;
+    int32_t rows, cols, side, batch, steps, cluster;
     bool tall;
     FusedPhase phases[3];
     int32_t *status;

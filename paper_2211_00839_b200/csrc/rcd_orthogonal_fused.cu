@@ -16,7 +16,7 @@ namespace rcd {
 namespace {
 
 constexpr int kRows = 128, kCols = 64, kBoxBytes = 64 * 128, kStage = 3 * kBoxBytes, kStages = 7, kThreads = 384, kFirstFinisher = 4, kFinishers = 8;
-constexpr int kCluster = 4;                                            // CTAs: those that may share a tile
+constexpr int kMostTeam = 4;                                           // CTAs that share a tile; a cluster is a team of the phase with the largest
 constexpr int kPartial = kRows * kCols * 4;
 constexpr uint32_t kWaitTurns = 1u << 16, kPolls = 1u << 21;           // about a second either
 
@@ -88,14 +88,14 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool across)
     return across ? (d & ~((uint64_t)0x3fff << 16)) | (uint64_t)(kBoxBytes >> 4) << 16 : d;
 }
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 newton_schulz_kernel(const __grid_constant__ CUtensorMap mapX0, const __grid_constant__ CUtensorMap mapX1, const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                      const __grid_constant__ FusedParams p)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
     float *const partial = reinterpret_cast<float *>(smem + kStages * kStage);
     FusedShared &sh = *reinterpret_cast<FusedShared *>(smem + kStages * kStage + kPartial);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)(blockIdx.x % kCluster);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)blockIdx.x & (p.cluster - 1);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&sh.accFull[b], 1); mbar_init(&sh.accEmpty[b], kFinishers); }
@@ -355,63 +355,85 @@ rcd_status launch_fused_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_
     return RCD_OK;
 }
 
-// Clusters that the device takes at once (some of its groups of SMs are not whole fours).
-static int teams_of(rcd_ctx *ctx)
+static cudaLaunchConfig_t fused_launch(int64_t grid, int cluster, cudaLaunchAttribute (&attrs)[2])
 {
-    if (ctx->fusedTeams < 0) {
-        ctx->fusedTeams = 0;
+    attrs[0].id = cudaLaunchAttributeClusterDimension;
+    attrs[0].val.clusterDim.x = (unsigned)cluster;
+    attrs[0].val.clusterDim.y = attrs[0].val.clusterDim.z = 1;
+    attrs[1].id = cudaLaunchAttributeCooperative;
+    attrs[1].val.cooperative = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3((unsigned)grid);
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = kSharedBytes;
+    config.attrs = attrs;
+    config.numAttrs = 2;
+    return config;
+}
+
+// CTAs in clusters of 1, 2 and 4 that the device takes at once (some of its groups of SMs are not whole fours: 148, 148 and 132 of 148).
+static int ctas_of(rcd_ctx *ctx, int log2Cluster)
+{
+    int &known = ctx->fusedCtas[log2Cluster];
+    if (known < 0) {
+        known = 0;
         if (!ctx->cooperative || allow_shared(newton_schulz_kernel, kSharedBytes) != cudaSuccess) return 0;
-        cudaLaunchConfig_t config{};
-        config.gridDim = dim3((unsigned)(ctx->smCount / kCluster * kCluster));
-        config.blockDim = dim3(kThreads);
-        config.dynamicSmemBytes = kSharedBytes;
+        const int cluster = 1 << log2Cluster;
+        cudaLaunchAttribute attrs[2];
+        const cudaLaunchConfig_t config = fused_launch(ctx->smCount / cluster * cluster, cluster, attrs);
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel, &config) == cudaSuccess) ctx->fusedTeams = std::min(n, ctx->smCount / kCluster);
+        if (cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel, &config) == cudaSuccess) known = std::min(n * cluster, ctx->smCount);
         else cudaGetLastError();
     }
-    return ctx->fusedTeams;
+    return known;
 }
 
 FusedPlan fused_plan(rcd_ctx *ctx, int64_t batch, int64_t rows, int64_t cols, bool tall)
 {
-    FusedPlan f{};
-    const int teams = teams_of(ctx);
+    FusedPlan best{};
     const int64_t side = std::min(rows, cols), sideTiles = (side + kRows - 1) / kRows;
-    if (teams == 0 || side > 4096 || rows > (1 << 20) || cols > (1 << 20)) return f;
-    const int64_t ctas = (int64_t)teams * kCluster;
-    int64_t most = 0;
-    for (int k = 0; k < 3; ++k) {
-        FusedPhase &ph = f.phases[k];
-        ph.symmetric = k < 2;
-        ph.M = (int32_t)(k < 2 ? side : rows);
-        ph.N = (int32_t)(k < 2 ? side : cols);
-        ph.slabs = (int32_t)((k == 0 ? std::max(rows, cols) : side) / 64);
-        ph.acrossA = k == 0 && tall;
-        ph.acrossB = k == 0 ? tall : k == 2 && !tall;
-        ph.stepA = (int32_t)(k == 0 ? rows : k == 1 ? side : tall ? rows : side);
-        ph.stepB = (int32_t)(k == 0 ? rows : k == 1 ? side : tall ? side : rows);
-        ph.tilesN = (int32_t)(ph.N / kCols);
-        const int64_t tiles = k < 2 ? sideTiles * (sideTiles + 1) : (rows + kRows - 1) / kRows * (cols / kCols);
-        if (tiles * batch > ctas * kFusedUnits) return FusedPlan{};
-        ph.tiles = (int32_t)tiles;
-        // A phase takes 2.7 us besides its slabs of 0.36 each (the barrier over the grid 1.6, the first slab's way and the last tile's end); a tile in pieces 1.8 more.
-        double least = 1e300;
-        for (int team = 1; team <= kCluster; team *= 2) {
-            const int64_t per = (ph.slabs + team - 1) / team;
-            if (team > 1 && (tiles * batch * team > ctas || (team - 1) * per >= ph.slabs)) continue;       // (a tile for every team, and no empty piece)
-            const double t = 2.7 + (double)((tiles * batch * team + ctas - 1) / ctas) * 0.36 * (double)per + (team > 1 ? 1.8 : 0.0);
-            if (t < least) {
-                least = t;
-                ph.team = team;
-                ph.per = (int32_t)per;
+    if (side > 4096 || rows > (1 << 20) || cols > (1 << 20)) return best;
+    for (int log2Cluster = 0; (1 << log2Cluster) <= kMostTeam; ++log2Cluster) {
+        FusedPlan f{};
+        f.cluster = 1 << log2Cluster;
+        const int64_t ctas = ctas_of(ctx, log2Cluster);
+        int64_t most = 0;
+        bool fits = ctas > 0;
+        for (int k = 0; k < 3 && fits; ++k) {
+            FusedPhase &ph = f.phases[k];
+            ph.symmetric = k < 2;
+            ph.M = (int32_t)(k < 2 ? side : rows);
+            ph.N = (int32_t)(k < 2 ? side : cols);
+            ph.slabs = (int32_t)((k == 0 ? std::max(rows, cols) : side) / 64);
+            ph.acrossA = k == 0 && tall;
+            ph.acrossB = k == 0 ? tall : k == 2 && !tall;
+            ph.stepA = (int32_t)(k == 0 ? rows : k == 1 ? side : tall ? rows : side);
+            ph.stepB = (int32_t)(k == 0 ? rows : k == 1 ? side : tall ? side : rows);
+            ph.tilesN = (int32_t)(ph.N / kCols);
+            const int64_t tiles = k < 2 ? sideTiles * (sideTiles + 1) : (rows + kRows - 1) / kRows * (cols / kCols);
+            fits = tiles * batch <= ctas * kFusedUnits;
+            ph.tiles = (int32_t)tiles;
+            // A phase takes 2.7 us besides its slabs of 0.36 each (the barrier over the grid 1.6, the first slab's way and the last tile's end); a tile in pieces 1.8 more.
+            double least = 1e300;
+            for (int team = 1; team <= f.cluster; team *= 2) {
+                const int64_t per = (ph.slabs + team - 1) / team;
+                if (team > 1 && (tiles * batch * team > ctas || (team - 1) * per >= ph.slabs)) continue;       // (a tile for every team, and no empty piece)
+                const double t = 2.7 + (double)((tiles * batch * team + ctas - 1) / ctas) * 0.36 * (double)per + (team > 1 ? 1.8 : 0.0);
+                if (t < least) {
+                    least = t;
+                    ph.team = team;
+                    ph.per = (int32_t)per;
+                }
             }
+            f.stepUs += least;
+            most = std::max(most, tiles * batch * ph.team);
         }
-        f.stepUs += least;
-        most = std::max(most, tiles * batch * ph.team);
+        if (!fits || (best.possible && f.stepUs >= best.stepUs)) continue;
+        f.grid = (int32_t)(std::min<int64_t>((most + f.cluster - 1) / f.cluster, ctas / f.cluster) * f.cluster);
+        f.possible = true;
+        best = f;
     }
-    f.grid = (int32_t)(std::min<int64_t>((most + kCluster - 1) / kCluster, teams) * kCluster);
-    f.possible = true;
-    return f;
+    return best;
 }
 
 rcd_status launch_fused(rcd_ctx *ctx, const FusedParams &p, const FusedPlan &plan, cudaStream_t st)
@@ -430,9 +452,12 @@ rcd_status launch_fused(rcd_ctx *ctx, const FusedParams &p, const FusedPlan &pla
         if (cr != CUDA_SUCCESS) return fail(ctx, RCD_ERR_CUDA, "cuTensorMapEncodeTiled failed with %d", (int)cr);
     }
     void *args[5] = {&maps[0], &maps[1], &maps[2], &maps[3], const_cast<FusedParams *>(&p)};
+    cudaLaunchAttribute attrs[2];
+    cudaLaunchConfig_t config = fused_launch(plan.grid, plan.cluster, attrs);
+    config.stream = st;
     ctx->kernelLaunches++;
     ctx->tcLaunches++;
-    RCD_CUDA(ctx, cudaLaunchCooperativeKernel((const void *)newton_schulz_kernel, dim3((unsigned)plan.grid), dim3(kThreads), args, kSharedBytes, st));
+    RCD_CUDA(ctx, cudaLaunchKernelExC(&config, (const void *)newton_schulz_kernel, args));
     return RCD_OK;
 }
 
