@@ -357,17 +357,17 @@ rcd_status launch_fused_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_
 
 static cudaLaunchConfig_t fused_launch(int64_t grid, int cluster, cudaLaunchAttribute (&attrs)[2])
 {
-    attrs[0].id = cudaLaunchAttributeClusterDimension;
-    attrs[0].val.clusterDim.x = (unsigned)cluster;
-    attrs[0].val.clusterDim.y = attrs[0].val.clusterDim.z = 1;
-    attrs[1].id = cudaLaunchAttributeCooperative;
-    attrs[1].val.cooperative = 1;
+    attrs[0].id = cudaLaunchAttributeCooperative;
+    attrs[0].val.cooperative = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = (unsigned)cluster;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t config{};
     config.gridDim = dim3((unsigned)grid);
     config.blockDim = dim3(kThreads);
     config.dynamicSmemBytes = kSharedBytes;
     config.attrs = attrs;
-    config.numAttrs = 2;
+    config.numAttrs = cluster > 1 ? 2 : 1;                // (a profiler may not take both: ncu 2025 does not)
     return config;
 }
 
@@ -382,7 +382,8 @@ static int ctas_of(rcd_ctx *ctx, int log2Cluster)
         cudaLaunchAttribute attrs[2];
         const cudaLaunchConfig_t config = fused_launch(ctx->smCount / cluster * cluster, cluster, attrs);
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel, &config) == cudaSuccess) known = std::min(n * cluster, ctx->smCount);
+        if (cluster == 1) known = ctx->smCount;            // (one of them fills an SM's shared memory)
+        else if (cudaOccupancyMaxActiveClusters(&n, newton_schulz_kernel, &config) == cudaSuccess) known = std::min(n * cluster, ctx->smCount);
         else cudaGetLastError();
     }
     return known;
