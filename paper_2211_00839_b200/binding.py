@@ -720,9 +720,9 @@ class Context:
             raise ValueError("%s is on %s, the context on %s" % (name, t.device, self.torch_device))
         if t.dtype != dtype:
             raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-        if tuple(t.shape) != tuple(shape):
+        if t.shape != shape:
             raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-        return t.contiguous()
+        return t if t.is_contiguous() else t.contiguous()
 
     def rcd_linear_cross_entropy(self, x, w, labels, bias=None):
         """Softmax cross entropy of the head x w^T + bias on the samples' labels, without its logits in memory: (loss, lse), float32 of the rows' shape.
@@ -730,22 +730,17 @@ class Context:
         x [..., k] and w [n, k] in bfloat16 or float16, labels [...] int32 (a negative one: the row is passed over), bias [n] float32 (-inf closes
         a class).  lse is the log of the sum of exponentials, which ``rcd_linear_cross_entropy_backward`` reads.  Autograd does not record the call."""
         torch = _torch()
-        a = RcdCrossEntropyArgs()
-        xk, rows, k, a.ldx = self._rows(x, "x")
+        f32 = torch.float32
+        xk, rows, k, ldx = self._rows(x, "x")
         if w.dim() != 2:
             raise ValueError("w must be [n, k]")
-        wk, n, _, a.ldw = self._rows(w, "w", k, None, x.dtype)
-        a.rows, a.n, a.k, a.type, a.x, a.w = rows, n, k, _elem(x.dtype, "x"), xk.data_ptr(), wk.data_ptr()
+        wk, n, _, ldw = self._rows(w, "w", k, None, x.dtype)
         shape = x.shape[:-1]
         lk = self._per_row(labels, "labels", shape, torch.int32)
-        a.labels = lk.data_ptr()
-        keep = [xk, wk, lk]
-        if bias is not None:
-            b = self._vector(bias, "bias", n, torch.float32)
-            a.bias = b.data_ptr()
-            keep.append(b)
-        loss, lse = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
-        a.loss, a.lse = loss.data_ptr(), lse.data_ptr()
+        b = None if bias is None else self._vector(bias, "bias", n, f32)
+        loss, lse = torch.empty_like(lk, dtype=f32), torch.empty_like(lk, dtype=f32)
+        a = RcdCrossEntropyArgs(rows, n, k, _elem(x.dtype, "x"), xk.data_ptr(), ldx, wk.data_ptr(), ldw, None if b is None else b.data_ptr(), lk.data_ptr(),
+                                loss.data_ptr(), lse.data_ptr())
         need = C.c_size_t()
         self._check(lib.rcd_linear_cross_entropy_workspace_bytes(self._h, C.byref(a), C.byref(need)))
         ws = self._scratch(need.value)
@@ -759,40 +754,25 @@ class Context:
 
         The logits are made again, ``piece`` classes at a time (0: as many as take 512 MB of workspace).  ``dw_dtype``: default x's type, or float32."""
         torch = _torch()
-        a = RcdCrossEntropyBackArgs()
-        xk, rows, k, a.ldx = self._rows(x, "x")
+        f32 = torch.float32
+        xk, rows, k, ldx = self._rows(x, "x")
         if w.dim() != 2:
             raise ValueError("w must be [n, k]")
-        wk, n, _, a.ldw = self._rows(w, "w", k, None, x.dtype)
-        a.rows, a.n, a.k, a.type, a.x, a.w, a.piece = rows, n, k, _elem(x.dtype, "x"), xk.data_ptr(), wk.data_ptr(), piece
+        wk, n, _, ldw = self._rows(w, "w", k, None, x.dtype)
         shape = x.shape[:-1]
-        lk, sk = self._per_row(labels, "labels", shape, torch.int32), self._per_row(lse, "lse", shape, torch.float32)
-        a.labels, a.lse = lk.data_ptr(), sk.data_ptr()
-        keep = [xk, wk, lk, sk]
-        if bias is not None:
-            b = self._vector(bias, "bias", n, torch.float32)
-            a.bias = b.data_ptr()
-            keep.append(b)
-        if dloss is not None:
-            b = self._per_row(dloss, "dloss", shape, torch.float32)
-            a.dloss = b.data_ptr()
-            keep.append(b)
-        if dlse is not None:
-            b = self._per_row(dlse, "dlse", shape, torch.float32)
-            a.dlse = b.data_ptr()
-            keep.append(b)
-        dx = dw = db = None
-        if want_dx:
-            dx = x.new_empty(x.shape)
-            a.dx, a.ld_dx = dx.data_ptr(), k
+        lk, sk = self._per_row(labels, "labels", shape, torch.int32), self._per_row(lse, "lse", shape, f32)
+        b = None if bias is None else self._vector(bias, "bias", n, f32)
+        gk = None if dloss is None else self._per_row(dloss, "dloss", shape, f32)
+        hk = None if dlse is None else self._per_row(dlse, "dlse", shape, f32)
         kind = x.dtype if dw_dtype is None else dw_dtype
-        a.dw_type = _elem(kind, "dw_dtype")
-        if want_dw:
-            dw = w.new_empty((n, k)) if kind == w.dtype else w.new_empty((n, k), dtype=kind)
-            a.dw, a.ld_dw = dw.data_ptr(), k
-        if want_dbias:
-            db = x.new_empty(n, dtype=torch.float32)
-            a.dbias = db.data_ptr()
+        dx = x.new_empty(x.shape) if want_dx else None
+        dw = (w.new_empty((n, k)) if kind == w.dtype else w.new_empty((n, k), dtype=kind)) if want_dw else None
+        db = x.new_empty(n, dtype=f32) if want_dbias else None
+
+        def at(t):
+            return None if t is None else t.data_ptr()
+        a = RcdCrossEntropyBackArgs(rows, n, k, _elem(x.dtype, "x"), xk.data_ptr(), ldx, wk.data_ptr(), ldw, at(b), lk.data_ptr(), sk.data_ptr(), at(gk), at(hk), piece,
+                                    at(dx), k, _elem(kind, "dw_dtype"), at(dw), k, at(db))
         need = C.c_size_t()
         self._check(lib.rcd_linear_cross_entropy_backward_workspace_bytes(self._h, C.byref(a), C.byref(need)))
         ws = self._scratch(need.value)

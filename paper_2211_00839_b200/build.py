@@ -17,7 +17,7 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "librcd.so")
 
 SOURCES = ["rcd_api.cu", "rcd_group.cu", "rcd_similarity.cu", "rcd_similarity_tc.cu", "rcd_greedy.cu", "rcd_cluster.cu", "rcd_rounds.cu", "rcd_small.cu",
-           "rcd_objective.cu", "rcd_objective_static.cu", "rcd_gaussian.cu", "rcd_cut.cu", "rcd_yardstick.cu", "rcd_norm.cu", "rcd_norm_ring.cu", "rcd_norm_ring_back.cu", "rcd_linear.cu", "rcd_linear_tc.cu", "rcd_linear_few.cu", "rcd_head.cu", "rcd_orthogonal.cu", "rcd_orthogonal_fused.cu"]
+           "rcd_objective.cu", "rcd_objective_static.cu", "rcd_gaussian.cu", "rcd_cut.cu", "rcd_yardstick.cu", "rcd_norm.cu", "rcd_norm_ring.cu", "rcd_norm_ring_back.cu", "rcd_linear.cu", "rcd_linear_tc.cu", "rcd_linear_few.cu", "rcd_head.cu", "rcd_orthogonal.cu", "rcd_orthogonal_fused.cu", "rcd_orthogonal_cluster.cu"]
 HEADERS = [os.path.join(CSRC, "rcd_internal.h"), os.path.join(CSRC, "rcd_exact.cuh"), os.path.join(CSRC, "rcd_cut_plan.h"),
            os.path.join(CSRC, "rcd_elem.cuh"), os.path.join(CSRC, "rcd_act.cuh"), os.path.join(CSRC, "rcd_linear.h"), os.path.join(CSRC, "rcd_tc.cuh"), os.path.join(CSRC, "rcd_norm.cuh"),
            os.path.join(CSRC, "rcd_ring.h"), os.path.join(CSRC, "rcd_walk.h"), os.path.join(CSRC, "rcd_product.cuh"), os.path.join(CSRC, "rcd_orthogonal.h"),

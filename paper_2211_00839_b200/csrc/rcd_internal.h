@@ -270,6 +270,8 @@ struct rcd_ctx {
     unsigned simReady = 0;              // tensor-core similarity kernels whose shared memory has been asked for, a bit each
     uint64_t productReady = 0;          // the same of rcd_linear's kernels
     alignas(16) unsigned char productPlans[4096] = {};   // how rcd_linear goes about the last few sizes
+    unsigned clusterReady = 0;          // kernels of rcd_orthogonalize's cluster per matrix whose shared memory has been asked for
+    int clusterSixteen = -1;            // whether it may have 16 CTAs (-1: not asked yet)
     int fusedCtas[3] = {-1, -1, -1};    // CTAs of rcd_orthogonalize's kernel of all steps resident at once, in clusters of 1, 2 and 4 (-1: not asked yet)
     unsigned simTurn = 0;               // similarity launches so far: each takes the next ticket
     size_t hostStageInts = 0;

@@ -260,7 +260,7 @@ extern "C" rcd_status rcd_orthogonalize_workspace_bytes(rcd_ctx *ctx, const rcd_
     if (!ctx) return RCD_ERR_INVALID_ARG;
     if (!args || !bytes_out) return fail(ctx, RCD_ERR_INVALID_ARG, "args or output is null");
     RCD_TRY(check(ctx, *args));
-    *bytes_out = args->batch == 0 || args->rows == 0 || args->cols == 0 ? 0 : layout_of(ctx, *args).bytes;
+    *bytes_out = args->batch == 0 || args->rows == 0 || args->cols == 0 || cluster_for(ctx, args->rows, args->cols) ? 0 : layout_of(ctx, *args).bytes;
     return RCD_OK;
 }
 
@@ -270,7 +270,7 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
     RCD_TRY(rcd_orthogonalize_workspace_bytes(ctx, args, &need));
     const rcd_orthogonalize_args &a = *args;
     begin_operator(ctx);
-    if (need == 0) return RCD_OK;
+    if (a.batch == 0 || a.rows == 0 || a.cols == 0) return RCD_OK;
     RCD_TRY(check_workspace(ctx, workspace_dev, workspace_bytes, need));
     const int64_t eb = elem_bytes(a.type);
     // (of a batch the bytes from the first matrix to the last; of one its rows)
@@ -278,11 +278,12 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
         const int64_t all = (a.batch - 1) * step + (a.rows - 1) * ld + a.cols;
         return a.batch > 1 ? Area{p, 1, all, all, bytes} : Area{p, a.rows, ld, a.cols, bytes};
     };
-    const Area out[] = {area(a.o_dev, a.ld_o, a.step_o, 2), {workspace_dev, 1, (int64_t)need, (int64_t)need, 1}};
+    const Area out[] = {area(a.o_dev, a.ld_o, a.step_o, 2), {need ? workspace_dev : nullptr, 1, (int64_t)need, (int64_t)need, 1}};
     const Area in[] = {area(a.g_dev, a.ld_g, a.step_g, eb)};
     RCD_TRY(check_apart(ctx, out, 2, in, 1));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     RCD_CUDA(ctx, cudaSetDevice(ctx->device));
+    if (const int cluster = cluster_for(ctx, a.rows, a.cols)) return launch_cluster(ctx, a, cluster, st);
     unsigned char *ws = (unsigned char *)workspace_dev;
     const Layout l = layout_of(ctx, a);
     const Gradient g{a.g_dev, a.ld_g, a.batch > 1 ? a.step_g : 0, (int32_t)a.rows, (int32_t)a.cols};

@@ -34,4 +34,8 @@ struct FusedParams {
 FusedPlan fused_plan(rcd_ctx *ctx, int64_t batch, int64_t rows, int64_t cols, bool tall);
 rcd_status launch_fused(rcd_ctx *ctx, const FusedParams &p, const FusedPlan &plan, cudaStream_t st);
 
+// A cluster per matrix (rcd_orthogonal_cluster.cu): of how many CTAs, 0 where it does not take the size; no workspace.
+int cluster_for(rcd_ctx *ctx, int64_t rows, int64_t cols);
+rcd_status launch_cluster(rcd_ctx *ctx, const rcd_orthogonalize_args &a, int cluster, cudaStream_t st);
+
 }  // namespace rcd

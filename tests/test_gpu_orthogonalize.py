@@ -59,7 +59,7 @@ def check(o, g, **kw):
 
 
 SIZES = [(1, 1, 1), (1, 1, 64), (2, 3, 1), (1, 16, 16), (3, 33, 65), (1, 64, 64), (2, 64, 200), (1, 127, 129), (1, 128, 128), (5, 130, 70), (1, 200, 1000), (2, 256, 256), (1, 333, 1001),
-         (3, 320, 320), (1, 512, 2048), (2, 513, 300), (1, 777, 777), (1, 1024, 1024), (1, 2048, 512), (16, 96, 160), (150, 40, 64)]
+         (3, 320, 320), (1, 512, 2048), (2, 513, 300), (1, 777, 777), (1, 1024, 1024), (1, 2048, 512), (16, 96, 160), (150, 40, 64), (2, 128, 384), (1, 100, 500), (2, 1500, 60), (1, 128, 2050), (1, 30, 4096), (2, 6100, 128), (40, 77, 300)]
 
 
 @pytest.mark.parametrize("batch,rows,cols", SIZES)
@@ -215,7 +215,7 @@ def test_refusals(rcd, ctx):
     import ctypes as C
     import numpy as np
     import torch
-    g = gradient(seeded("refusals"), 2, 20, 30, torch.bfloat16)
+    g = gradient(seeded("refusals"), 2, 200, 300, torch.bfloat16)        # (larger than what takes no workspace)
     for bad in (g.cpu(), g[0, 0]):
         with pytest.raises(ValueError):
             ctx.rcd_orthogonalize(bad)
@@ -224,14 +224,14 @@ def test_refusals(rcd, ctx):
     for kw in (dict(steps=0), dict(steps=65), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(coefficients=(1.0, float("nan"), 0.0)), dict(coefficients=(1e5, 0.0, 0.0))):
         with pytest.raises(rcd.RcdError):
             ctx.rcd_orthogonalize(g, **kw)
-    for kw in (dict(coefficients=(1.0, 2.0)), dict(steps=3, coefficients=[QUINTIC, QUINTIC]), dict(out=g.half()), dict(out=g[:1].clone()), dict(out=torch.empty(2, 30, 20, device="cuda", dtype=torch.bfloat16).transpose(1, 2))):
+    for kw in (dict(coefficients=(1.0, 2.0)), dict(steps=3, coefficients=[QUINTIC, QUINTIC]), dict(out=g.half()), dict(out=g[:1].clone()), dict(out=torch.empty(2, 300, 200, device="cuda", dtype=torch.bfloat16).transpose(1, 2))):
         with pytest.raises(ValueError):
             ctx.rcd_orthogonalize(g, **kw)
     with pytest.raises(rcd.RcdError):
         ctx.rcd_orthogonalize(g, out=g)                       # the output is the input
     c = np.array(QUINTIC * 5, dtype=np.float32)
     o = torch.empty_like(g)
-    ok = dict(batch=2, rows=20, cols=30, type=1, g=g.data_ptr(), ld_g=30, step_g=600, steps=5, coefficients_host=c.ctypes.data, eps=0.0, o=o.data_ptr(), ld_o=30, step_o=600)
+    ok = dict(batch=2, rows=200, cols=300, type=1, g=g.data_ptr(), ld_g=300, step_g=60000, steps=5, coefficients_host=c.ctypes.data, eps=0.0, o=o.data_ptr(), ld_o=300, step_o=60000)
     need = C.c_size_t()
 
     def refused(status, ws=None, size=0, **change):
@@ -240,12 +240,17 @@ def test_refusals(rcd, ctx):
         assert got == status, (got, change)
     refused(0)
     big = torch.empty(need.value + 256, dtype=torch.uint8, device="cuda")
-    for change in (dict(g=None), dict(o=None), dict(coefficients_host=None), dict(type=0), dict(type=9), dict(batch=-1), dict(rows=-3), dict(ld_g=29), dict(ld_o=2), dict(step_g=599), dict(step_o=0),
+    for change in (dict(g=None), dict(o=None), dict(coefficients_host=None), dict(type=0), dict(type=9), dict(batch=-1), dict(rows=-3), dict(ld_g=299), dict(ld_o=2), dict(step_g=59999), dict(step_o=0),
                    dict(g=g.data_ptr() + 1), dict(o=o.data_ptr() + 1)):
         refused(1, **change)
-    refused(2, rows=1 << 17, ld_g=30)
+    refused(2, rows=1 << 17)
     refused(2, batch=1 << 16)
     refused(3, ws=big.data_ptr(), size=need.value - 1)
     refused(1, ws=big.data_ptr() + 16, size=need.value)
     refused(1, ws=big.data_ptr(), size=need.value, o=big.data_ptr())
+    small = dict(rows=20, cols=30)
+    refused(0, **small)
+    assert need.value == 0
+    refused(0, ws=C.c_void_p(None), size=0, **small)
+    refused(1, ws=C.c_void_p(None), size=0, **{**small, "o": g.data_ptr()})
     ctx.sync_status()
