@@ -47,13 +47,10 @@ __device__ __forceinline__ uint32_t cluster_addr(const void *p, int rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
     return a;
 }
-__device__ __forceinline__ void push4(uint32_t to, uint32_t bar, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+// `bytes` from this CTA's shared memory to another's, reported to its barrier when they are there.
+__device__ __forceinline__ void push(uint32_t to, const void *from, uint32_t bytes, uint32_t bar)
 {
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%2, %3, %4, %5}, [%1];" :: "r"(to), "r"(bar), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-__device__ __forceinline__ void push2(uint32_t to, uint32_t bar, uint32_t a, uint32_t b)
-{
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%2, %3}, [%1];" :: "r"(to), "r"(bar), "r"(a), "r"(b) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" :: "r"(to), "r"(smem_addr(from)), "r"(bytes), "r"(bar) : "memory");
 }
 // Byte of (row, 16-byte chunk) in a slab of 64 columns, as the 128-byte swizzle places it.
 __device__ __forceinline__ int slab_at(int row, int chunk) { return row * 128 + ((chunk ^ (row & 7)) << 4); }
@@ -195,6 +192,8 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
         __syncthreads();
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     };
+    // 128 rows of 128 bytes: the slabs of A, then of B
+    auto quarter = [&](int k) { return a + k * kSlabBytes; };
     bool ok = true;
     for (int i = 0; i < p.steps; ++i) {
         const float *const c = p.coefficients + 3 * i;
@@ -207,8 +206,8 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
             }
             mma_commit(&sh.product);
             if (C > 1) {
-                mbar_expect_tx(&sh.sums, kExchange);
-                mbar_expect_tx(&sh.square, kSquare);
+                mbar_expect_tx(&sh.sums, kExchange - owned * 512);     // (but for what comes from here)
+                mbar_expect_tx(&sh.square, kSquare - owned * 256);     // (but for my own rows)
             }
         }
         if (!(ok = complete())) break;
@@ -226,36 +225,38 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
                     *reinterpret_cast<uint4 *>(a + half * kSlabBytes + slab_at(row, 4 * h + k)) = make_uint4(halves(z(0), z(1)), halves(z(2), z(3)), halves(z(4), z(5)), halves(z(6), z(7)));
                 }
             } else {
-                const int owner = row / owned;
-                const uint32_t to = cluster_addr(exchange + (rank * owned + row % owned) * kSide, owner), bar = cluster_addr(&sh.sums, owner);
+                // a row's 128 sums are four times 128 bytes: those of my own rows where they are added up, the others' in the places of that row of A and B
+                const int piece = 2 * half + h;
+                unsigned char *const to = row / owned == rank ? (unsigned char *)exchange + ((rank * 4 + piece) * owned + row % owned) * 128 : quarter(piece) + row * 128;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) push4(to + (uint32_t)(((col / 4 + k) ^ (row & 7)) << 4), bar, v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);       // (turned by the row: fewer banks twice)
+                for (int k = 0; k < 8; ++k) *reinterpret_cast<uint4 *>(to + ((k ^ (row & 7)) << 4)) = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
             }
         }
         if (C > 1) {
+            // To the rows' owners.  (What an owner sends back comes into the place that its sums were read from; my own rows of A, which the others may still be waiting for, are
+            // written next when all have sent sums of the next step, and so have had them.)
+            ordered_for_products();
+            __syncthreads();
+            if (threadIdx.x < 4 * C && (int)threadIdx.x / 4 != rank) {
+                const int owner = threadIdx.x / 4, piece = threadIdx.x % 4;
+                push(cluster_addr(exchange + (rank * 4 + piece) * owned * 32, owner), quarter(piece) + owner * owned * 128, (uint32_t)owned * 128, cluster_addr(&sh.sums, owner));
+            }
             if (!(ok = all_wait_for(&sh.sums, i & 1, &sh))) break;
             // 2 C threads a row, 64 / C columns each: four at a time
-            const int r = threadIdx.x / (2 * C), mine = rank * owned + r, share = 64 / C, c0 = threadIdx.x % (2 * C) * share;
-            for (int col = c0; col < c0 + share; col += 8) {
-                float z[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                const int wide = min(share, 8);
+            const int r = threadIdx.x / (2 * C), mine = rank * owned + r, share = 64 / C;
+            for (int col = threadIdx.x % (2 * C) * share, end = col + share; col < end; col += 4) {
+                float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 for (int k = 0; k < C; ++k) {
-                    const float *const from = exchange + (k * owned + r) * kSide;
-                    const float4 lo = *reinterpret_cast<const float4 *>(from + (((col / 4) ^ (mine & 7)) << 2));
-                    z[0] += lo.x; z[1] += lo.y; z[2] += lo.z; z[3] += lo.w;
-                    if (wide == 8) {
-                        const float4 hi = *reinterpret_cast<const float4 *>(from + (((col / 4 + 1) ^ (mine & 7)) << 2));
-                        z[4] += hi.x; z[5] += hi.y; z[6] += hi.z; z[7] += hi.w;
-                    }
+                    const float4 from = *reinterpret_cast<const float4 *>(exchange + ((k * 4 + col / 32) * owned + r) * 32 + (((col % 32 / 4) ^ (mine & 7)) << 2));
+                    z.x += from.x; z.y += from.y; z.z += from.z; z.w += from.w;
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] *= alpha;
-                const unsigned char *const at = a + col / 64 * kSlabBytes + slab_at(mine, col % 64 / 8) + col % 8 * 2;
-                for (int k = 0; k < C; ++k) {
-                    const uint32_t to = cluster_addr(at, k), bar = cluster_addr(&sh.square, k);
-                    if (wide == 8) push4(to, bar, halves(z[0], z[1]), halves(z[2], z[3]), halves(z[4], z[5]), halves(z[6], z[7]));
-                    else push2(to, bar, halves(z[0], z[1]), halves(z[2], z[3]));
-                }
+                *reinterpret_cast<uint2 *>(a + col / 64 * kSlabBytes + slab_at(mine, col % 64 / 8) + col % 8 * 2) = make_uint2(halves(z.x * alpha, z.y * alpha), halves(z.z * alpha, z.w * alpha));
+            }
+            ordered_for_products();
+            __syncthreads();
+            if (threadIdx.x < 2 * C && (int)threadIdx.x / 2 != rank) {
+                unsigned char *const at = a + threadIdx.x % 2 * kSlabBytes + rank * owned * 128;
+                push(cluster_addr(at, threadIdx.x / 2), at, (uint32_t)owned * 128, cluster_addr(&sh.square, threadIdx.x / 2));
             }
             if (!(ok = all_wait_for(&sh.square, i & 1, &sh))) break;
         }
