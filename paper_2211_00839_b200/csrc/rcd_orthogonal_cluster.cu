@@ -5,6 +5,9 @@
 // CTAs' order and push their rows of A to all.  B = b A + c A A and the columns' update are then each CTA's own business.  Nothing but G and the result touches memory,
 // and what a step waits for are two exchanges within the cluster where the other forms wait for three barriers over the grid or three launches.
 //
+// 128 x 128 takes 23 us (all steps in one launch with barriers over the grid: 64), 128 x 2048 53 (82), 16 of 128 x 512 51 (81).  Of the last but one's 94 000 cycles a step takes
+// 15 000: the products 4500, the two exchanges with their sums 7300 (latency: 56 KB come and go per CTA), the finishing of B and X 3000.
+//
 // All 256 threads go through the stages together; thread 0 issues the products.  Every wait is bounded: whoever waits in vain makes its CTA leave, and the others of
 // the cluster behind it.
 #include "rcd_orthogonal.h"
@@ -78,17 +81,21 @@ struct ClusterParams {
 
 // Eight neighbours of a row of X, from column col on; zeros outside.
 template <typename T, bool kTall, bool kWhole>
-__device__ __forceinline__ void load_eight(float (&v)[8], const T *g, int64_t ld, int row, int col, int side, int len)
+__device__ __forceinline__ Pack<T, 8> load_eight(const T *g, int64_t ld, int row, int col, int side, int len)
 {
-    if (!kTall && kWhole && row < side && col + 8 <= len) {
-        load_pack<8>(v, g + row * ld + col);
-        return;
-    }
+    Pack<T, 8> v;
+    if constexpr (kWhole) {
+        if (row < side && col < len) return *reinterpret_cast<const Pack<T, 8> *>(g + row * ld + col);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = row < side && col + j < len ? to_float(kTall ? g[(int64_t)(col + j) * ld + row] : g[(int64_t)row * ld + col + j]) : 0.0f;
+        for (int j = 0; j < 8; ++j) v.v[j] = from_float<T>(0.0f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v.v[j] = row < side && col + j < len ? g[kTall ? (int64_t)(col + j) * ld + row : (int64_t)row * ld + col + j] : from_float<T>(0.0f);
+    }
+    return v;
 }
 
-// kWhole: rows of a G that is not tall start on 16 bytes.
+// kWhole: rows of a G that is not tall start on 16 bytes and are a multiple of eight long.
 template <typename T, bool kTall, bool kWhole>
 __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(const __grid_constant__ ClusterParams p)
 {
@@ -121,15 +128,17 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
         if (kTall) { *r = i % kSide; *c = i / kSide * 8; }
         else { *r = i / (columns / 8); *c = i % (columns / 8) * 8; }
     };
+    // (16-bit elements wait in their place in shared memory until the norm is known; fp32 is read again.  In registers, with the loops unrolled, the code itself took 9000 cycles to come.)
+    auto at_piece = [&](int r, int c) { return x + c / 64 * kSlabBytes + slab_at(r, c % 64 / 8); };
     double s = 0.0;
-#pragma unroll 4
+#pragma unroll (kWhole ? 4 : 1)
     for (int i = threadIdx.x; i < pieces; i += kThreads) {
         int r, c;
         place(i, &r, &c);
-        float v[8];
-        load_eight<T, kTall, kWhole>(v, g, p.ldG, r, first + c, p.side, p.len);
+        const Pack<T, 8> v = load_eight<T, kTall, kWhole>(g, p.ldG, r, first + c, p.side, p.len);
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<Pack<T, 8> *>(at_piece(r, c)) = v;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s += (double)v[j] * (double)v[j];
+        for (int j = 0; j < 8; ++j) s = fma((double)to_float(v.v[j]), (double)to_float(v.v[j]), s);
     }
     s = warp_sum(s);
     if (lane == 0) sh.reduce[warp] = s;
@@ -157,18 +166,15 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
         factor = (float)(ldexp(1.0, kUp) / ldexp(norm, e));
     }
     const float up0 = ldexpf(1.0f, e / 2), up1 = ldexpf(1.0f, e - e / 2);          // (2^e alone may be out of fp32's range)
-#pragma unroll 4
+#pragma unroll (kWhole || sizeof(T) == 2 ? 4 : 1)
     for (int i = threadIdx.x; i < pieces; i += kThreads) {
         int r, c;
         place(i, &r, &c);
-        float v[8];
-        load_eight<T, kTall, kWhole>(v, g, p.ldG, r, first + c, p.side, p.len);
-        uint4 w;
-        w.x = halves(v[0] * up0 * up1, v[1] * up0 * up1);
-        w.y = halves(v[2] * up0 * up1, v[3] * up0 * up1);
-        w.z = halves(v[4] * up0 * up1, v[5] * up0 * up1);
-        w.w = halves(v[6] * up0 * up1, v[7] * up0 * up1);
-        *reinterpret_cast<uint4 *>(x + c / 64 * kSlabBytes + slab_at(r, c % 64 / 8)) = w;
+        Pack<T, 8> v;
+        if constexpr (sizeof(T) == 2) v = *reinterpret_cast<const Pack<T, 8> *>(at_piece(r, c));
+        else v = load_eight<T, kTall, kWhole>(g, p.ldG, r, first + c, p.side, p.len);
+        auto z = [&](int j) { return to_float(v.v[j]) * up0 * up1; };
+        *reinterpret_cast<uint4 *>(at_piece(r, c)) = make_uint4(halves(z(0), z(1)), halves(z(2), z(3)), halves(z(4), z(5)), halves(z(6), z(7)));
     }
     ordered_for_products();
     __syncthreads();
@@ -412,7 +418,7 @@ rcd_status launch_cluster(rcd_ctx *ctx, const rcd_orthogonalize_args &a, int clu
     p.status = ctx->statusOwn + kOperatorStatus;
     for (int i = 0; i < 3 * a.steps; ++i) p.coefficients[i] = a.coefficients_host[i];
     const int64_t eb = elem_bytes(a.type);
-    const bool whole = rows_aligned(a.g_dev, a.ld_g, eb, 16) && (a.batch == 1 || a.step_g * eb % 16 == 0);
+    const bool whole = rows_aligned(a.g_dev, a.ld_g, eb, 16) && a.cols % 8 == 0 && (a.batch == 1 || a.step_g * eb % 16 == 0);
     const ClusterKernel kernel = a.type == RCD_ELEM_BF16 ? kernel_for<__nv_bfloat16>(p.tall, whole) : a.type == RCD_ELEM_F16 ? kernel_for<__half>(p.tall, whole) : kernel_for<float>(p.tall, whole);
     const int bit = 3 * (a.type == RCD_ELEM_BF16 ? 0 : a.type == RCD_ELEM_F16 ? 1 : 2) + (p.tall ? 0 : whole ? 1 : 2);
     if (!(ctx->clusterReady >> bit & 1)) {

@@ -78,14 +78,20 @@ def test_against_the_formula(rcd, ctx, batch, rows, cols, dtype, pad):
     assert torch.equal(ctx.rcd_orthogonalize(g), o)
 
 
-@pytest.mark.parametrize("rows,cols", [(2300, 2300), (4200, 1100), (600, 5000)])
-def test_large(rcd, ctx, rows, cols):
-    """Pairs of SMs, sums in chunks (more than 4096 rows or columns), blocks that end inside a matrix."""
+@pytest.mark.parametrize("batch,rows,cols,dtype", [(1, 2300, 2300, "bf16"), (1, 4200, 1100, "fp16"), (1, 600, 5000, "bf16"), (3, 1500, 1100, "fp32"), (2, 1100, 1500, "bf16"), (2, 1600, 1536, "bf16"),
+                                                   (6, 900, 1000, "fp16")])
+def test_large(rcd, ctx, batch, rows, cols, dtype):
+    """Launches of their own: pairs of SMs, sums in chunks (more than 4096 rows or columns), blocks that end inside a matrix, matrices that the last product cannot write
+    (their rows are no multiple of 32)."""
     import torch
-    g = gradient(seeded("large", rows, cols), 1, rows, cols, torch.bfloat16)[0]
+    g = gradient(seeded("large", batch, rows, cols), batch, rows, cols, kind(dtype))
     o = ctx.rcd_orthogonalize(g)
     ctx.sync_status()
     check(o, g)
+    buf = torch.full((batch, rows + 1, cols + 24), 7.0, device="cuda", dtype=torch.bfloat16)
+    assert torch.equal(ctx.rcd_orthogonalize(g, out=buf[:, :-1, 8:cols + 8]), o)
+    buf[:, :-1, 8:cols + 8] = 7
+    assert bool((buf == 7).all())
 
 
 @pytest.mark.parametrize("rows,cols", [(100, 260), (260, 100)])
