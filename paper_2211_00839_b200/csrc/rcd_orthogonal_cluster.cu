@@ -380,7 +380,7 @@ static bool sixteen(rcd_ctx *ctx)
         config.dynamicSmemBytes = (size_t)bytes;
         config.attrs = &attr;
         config.numAttrs = 1;
-        if (allow_shared(kernel, bytes) == cudaSuccess && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+        if (cudaSetDevice(ctx->device) == cudaSuccess && allow_shared(kernel, bytes) == cudaSuccess && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
             cudaOccupancyMaxActiveClusters(&n, kernel, &config) == cudaSuccess)
             ctx->clusterSixteen = n > 0;
         else

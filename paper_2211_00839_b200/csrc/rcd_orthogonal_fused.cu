@@ -380,7 +380,7 @@ static int ctas_of(rcd_ctx *ctx, int log2Cluster)
     int &known = ctx->fusedCtas[log2Cluster];
     if (known < 0) {
         known = 0;
-        if (!ctx->cooperative || allow_shared(newton_schulz_kernel, kSharedBytes) != cudaSuccess) return 0;
+        if (!ctx->cooperative || cudaSetDevice(ctx->device) != cudaSuccess || allow_shared(newton_schulz_kernel, kSharedBytes) != cudaSuccess) return 0;
         const int cluster = 1 << log2Cluster;
         cudaLaunchAttribute attrs[2];
         const cudaLaunchConfig_t config = fused_launch(ctx->smCount / cluster * cluster, cluster, attrs);

@@ -80,3 +80,73 @@ def test_logits_beyond_32_bits(rcd, ctx):
         p -= (y.long()[:, None] == torch.arange(at.start, at.stop, device="cuda")).double()
         dw64 = p.t() @ x.double()
         assert float((dw[at].double() - dw64).norm() / dw64.norm()) < 3 * 2.0 ** -8
+
+
+def test_launches_behind_copies_fills_and_other_streams(rcd, ctx):
+    """Kernels that may overtake the end of the one before them, behind what is no kernel: copies and fills, in a captured graph and outside; and behind another stream's
+    work that an event brings in."""
+    import torch
+    g = seeded("behind")
+    m, n, k = 300, 700, 128
+    x, w = rows(g, m, k, torch.bfloat16), rows(g, n, k, torch.bfloat16, size=0.2)
+    y = torch.randint(0, n, (m,), generator=g, device="cuda", dtype=torch.int32)
+    wide = rows(g, 96, 700, torch.bfloat16)
+    want, want_lse = ctx.rcd_linear_cross_entropy(x, w, y)
+    o = ctx.rcd_orthogonalize(wide)
+    fx, fw, fy, fg = torch.empty_like(x), torch.empty_like(w), torch.empty_like(y), torch.empty_like(wide)
+    side = torch.cuda.Stream()
+
+    def run():
+        fx.zero_()
+        fx.copy_(x)
+        fg.copy_(wide)
+        # another stream's part
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            fw.copy_(w)
+            fy.copy_(y)
+            z, _ = ctx.rcd_linear(fx, fw)
+        torch.cuda.current_stream().wait_stream(side)
+        loss, lse = ctx.rcd_linear_cross_entropy(fx, fw, fy)
+        fx.fill_(float("nan"))
+        o2 = ctx.rcd_orthogonalize(fg)
+        fg.zero_()
+        fw.zero_()
+        return z, loss, lse, o2
+    z = ctx.rcd_linear(x, w)[0]
+    for _ in range(3):
+        assert all(torch.equal(p, q) for p, q in zip(run(), (z, want, want_lse, o)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for _ in range(3):
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, (z, want, want_lse, o)))
+    ctx.sync_status()
+
+
+def test_two_streams_at_once(rcd, ctx):
+    """Updates of the form that holds all SMs (its CTAs wait for one another), updates by clusters and products, enqueued on two streams without any order between them."""
+    import torch
+    g = seeded("two")
+    a, b, c = (torch.randn(*s, generator=g, device="cuda").bfloat16() for s in ((512, 1100), (700, 300), (128, 1500)))
+    x, w = rows(g, 2000, 512, torch.bfloat16), rows(g, 1500, 512, torch.bfloat16, size=0.05)
+    y = torch.randint(0, 1500, (2000,), generator=g, device="cuda", dtype=torch.int32)
+
+    def work():
+        loss, lse = ctx.rcd_linear_cross_entropy(x, w, y)
+        return [ctx.rcd_orthogonalize(a), loss, ctx.rcd_orthogonalize(b), ctx.rcd_orthogonalize(c), *ctx.rcd_linear_cross_entropy_backward(x, w, y, lse)]
+    want = work()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(work())
+    torch.cuda.synchronize()
+    ctx.sync_status()
+    assert all(torch.equal(p, q) for each in got for p, q in zip(each, want))
