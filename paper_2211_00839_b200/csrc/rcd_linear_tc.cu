@@ -116,6 +116,9 @@ struct Plan {
 };
 
 
+// Slabs of a tile from which on its warps have one place for their pieces: gradients of 8192 x 4096 x 4096 (64 and 128 slabs) 419 us for 438; from 16 on the int8 product of
+// 50 000 x 2048 x 2048 with its residual would take 193 us for 180.
+constexpr int kOnePlaceFrom = 48;
 // Column tiles that are neighbours in the order of the work, where B has more bytes than stay in L2.  (8192 x 4096 x 65 536: 3.36 ms, 4.25 row after row;
 // all gradients over 32 768 classes 5.10 ms and 5.64.)
 constexpr int kBand = 8;
@@ -329,14 +332,19 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     const bool chunks = !i8 && plan.slabsPerSplit > (p.head.sums || p.out.type == RCD_ELEM_F32 ? chunk : 2 * chunk);
     q.chunk = chunks ? chunk : q.slabs;
     q.aRows = aRows;
-    q.stagingBytes = p.form == kLoss ? kJoinStaging : kStaging;
-    q.stageBytes = (q.aRows + (plan.pair ? plan.tn / 2 : plan.tn)) * kSlab;
-    q.stages = std::min(kMostStages, (kMostShared - q.stagingBytes - kFixedShared) / q.stageBytes);
+    q.e = p.out;
+    q.raw = plan.splits > 1;
+    // What the ring leaves room for.  A second place per warp hides a store's way out behind the next piece, which does not matter where a tile's slabs take longer than
+    // its end; with one, and without columns, 256 x 256 tiles have a ring of six stages for four.
+    q.columnBytes = !q.raw && (q.e.bias || (i8 && q.e.ws)) ? kColumnBytes : 0;
+    q.places = !q.raw && (q.e.z || p.symmetric || p.head.sums) ? 2 : plan.slabsPerSplit >= kOnePlaceFrom ? 1 : 2;
+    q.stagingBytes = p.form == kLoss ? kJoinStaging : kEpiWarps * q.places * kPiece;
+    const OperandRing ring = ring_of(q.aRows, plan.pair ? plan.tn / 2 : plan.tn, q.stagingBytes + q.columnBytes + kFixedShared);
+    q.stageBytes = ring.stageBytes;
+    q.stages = ring.stages;
     q.idesc = (i8 ? (2u << 4) | (1u << 7) | (1u << 10)                                     // S8 x S8 -> S32
                   : (1u << 4) | (p.type == RCD_ELEM_BF16 ? (1u << 7) | (1u << 10) : 0u)) | // BF16 x BF16 or F16 x F16 -> F32
               (p.a.across ? 1u << 15 : 0u) | (p.b.across ? 1u << 16 : 0u) | ((uint32_t)(plan.tn >> 3) << 17) | ((uint32_t)((plan.pair ? 256 : 128) >> 4) << 24);
-    q.e = p.out;
-    q.raw = plan.splits > 1;
     if (q.raw) {
         q.e = Epilogue{};
         q.e.type = RCD_ELEM_F32;
@@ -359,7 +367,7 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
         RCD_TRY(encode(ctx, &maps[3], map_type(q.e.type), q.e.y, p.N, rows_of(p.yStep), q.e.ldy * yb, 32, 64, CU_TENSOR_MAP_SWIZZLE_NONE));
     }
     q.edgeByHand = !q.raw && p.N * yb % 16 != 0;           // (a piece of the k axis has rows of whole 128 bytes)
-    const size_t smem = (size_t)q.stages * q.stageBytes + q.stagingBytes + kFixedShared;
+    const size_t smem = (size_t)ring.bytes;
     const int slots = plan.pair ? ctx->smCount / 2 : ctx->smCount;
     const int grid = std::min(slots, q.units) * (plan.pair ? 2 : 1);
     const int order = !p.a.across && !p.b.across ? 0 : !p.a.across ? 1 : 2;

@@ -10,8 +10,8 @@
 // stored both ways.
 //
 // Three forms: a side of at most 128 in a cluster per matrix (rcd_orthogonal_cluster.cu); all steps in one launch (rcd_orthogonal_fused.cu), where the time goes into the
-// steps' waiting for one another; launches of their own with tiles of up to 256 x 256 on pairs of SMs, where it goes into the products (4096 x 4096: 1.25 to 1.35 ms, 1.02 PFLOP/s of what
-// has to be computed; 62 to 74 % of cuBLAS's rate).
+// steps' waiting for one another; launches of their own with tiles of up to 256 x 256 on pairs of SMs, where it goes into the products (4096 x 4096: 1.16 ms, 1.18 PFLOP/s of
+// what has to be computed, 71 % of cuBLAS's rate in bursts).
 #include "rcd_orthogonal.h"
 #include "rcd_product.cuh"
 

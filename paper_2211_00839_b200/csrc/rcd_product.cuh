@@ -23,11 +23,9 @@
 
 namespace rcd {
 
-constexpr int kRows = 128;                              // rows of A per CTA
-constexpr int kSlab = 128;                              // bytes of k per operand row and stage
+constexpr int kRows = kOperandRows, kSlab = kOperandSlab, kMostStages = kOperandStages, kMostShared = kBlockShared;
 constexpr int kSlabRows16 = 64;                         // k elements of 16 bits per slab
 constexpr int kBox = 64 * kSlab;                        // 8 KB: 64 k rows of 64 elements
-constexpr int kMostStages = 8;
 constexpr int kEpiWarps = 8;
 // The tensor cores cut an fp32 sum off where they cannot hold it, towards zero: products of fp16 and of one sign lose 6.5e-9 of the result
 // each, 3.2e-4 over 50 000 (two thirds of the type's half step).  So sums are taken in chunks that are added up outside with rounding.
@@ -44,10 +42,8 @@ constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
 constexpr int kLaunchRegs = 168, kIssueRegs = 40, kEpiRegs = 232;
 static_assert(128 * kIssueRegs + 32 * kEpiWarps * kEpiRegs <= kThreads * kLaunchRegs, "what one warpgroup gets the other has to have given");
 constexpr int kPiece = 32 * 128;                        // an epilogue warp's piece of the output: 32 rows of 128 bytes
-constexpr int kStaging = kEpiWarps * 2 * kPiece;
 constexpr int kColumnBytes = kEpiWarps * 2 * 128 * 4;   // a warp's 128 columns of a tile: biases and scales
 constexpr uint32_t kWaitTurns = 1u << 16;               // of at most 20 us: a second or so
-constexpr int kMostShared = 227 * 1024;
 
 struct __align__(8) ProductShared {
     uint64_t full[kMostStages], empty[kMostStages];     // full: CTA 0's of a pair
@@ -57,11 +53,11 @@ struct __align__(8) ProductShared {
     uint32_t tmemBase;
     int32_t abort;
 };
-constexpr int kFixedShared = kColumnBytes + (int)sizeof(ProductShared);
+constexpr int kFixedShared = (int)sizeof(ProductShared);
 constexpr int kJoinStaging = 2 * 4 * 3 * 32 * 4;        // kLoss: what the second warp of a quarter hands to the first, two tiles in turn
 
 struct TcParams {
-    int32_t M, N, units, slabs, slabsPerSplit, chunk, tn, stages, stageBytes, stagingBytes, aRows, rowsPart;
+    int32_t M, N, units, slabs, slabsPerSplit, chunk, tn, stages, stageBytes, stagingBytes, columnBytes, places, aRows, rowsPart;
     uint32_t idesc;
     Walk walk;
     int32_t aStep, bStep, yStep, rStep;                        // rows from one matrix of a batch to the next (rows of k, where an operand is across)
@@ -298,7 +294,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
     unsigned char *const tiles = smem;
     unsigned char *const staging = smem + (size_t)p.stages * p.stageBytes;
     float *const columns = reinterpret_cast<float *>(staging + p.stagingBytes);
-    ProductShared &sh = *reinterpret_cast<ProductShared *>(staging + p.stagingBytes + kColumnBytes);
+    ProductShared &sh = *reinterpret_cast<ProductShared *>(staging + p.stagingBytes + p.columnBytes);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = kPair ? (int)(blockIdx.x & 1) : 0;
@@ -429,7 +425,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kEpiRegs));
         // ---------------- epilogue: this CTA's 128 rows ----------------
         const int q = warp & 3, ew = warp - kFirstEpiWarp, half = ew >> 2;       // TMEM lanes 32 q ..; pieces half, half + 2, ...
-        unsigned char *const mine = staging + ew * 2 * kPiece;
+        unsigned char *const mine = staging + ew * p.places * kPiece;
         float *const biases = columns + ew * 256, *const scales = biases + 128;
         const Epilogue &e = p.e;
         const int wide = kChunks ? kChunks : e.type == RCD_ELEM_F32 ? 32 : 64;        // columns of a piece
@@ -460,7 +456,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         };
         const bool mirrors = kForm == kScaled && p.walk.subM != 0;
         const bool sums = kForm == kLogitGrads && p.head.sums != nullptr;
-        const bool alternate = e.z == nullptr && !mirrors && !sums;   // two buffers in turn, or one for y and one for z, the transpose or sums
+        const bool alternate = p.places == 2 && e.z == nullptr && !mirrors && !sums;      // two places in turn, or one for y and one for z, the transpose or sums; or only the one
         uint32_t nt = 0, turn = 0;
         [[maybe_unused]] uint32_t tile = 0;
         if (p.tmaR && lane == 0 && first < p.units) fetch(unit_of(p.walk, first), first, half, 0);

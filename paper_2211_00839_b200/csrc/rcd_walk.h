@@ -1,6 +1,7 @@
-// Which tile of a product a unit of work is (rcd_product.cuh).
+// Which tile of a product a unit of work is, and how its operands lie in shared memory (rcd_product.cuh).
 #pragma once
 
+#include <algorithm>
 #include <cstdint>
 
 #include <cuda_runtime.h>
@@ -45,6 +46,22 @@ __host__ __device__ inline Unit unit_of(const Walk &w, int32_t u)
     t.n = at * w.band + (r - t.m * width);
     t.mirror = false;
     return t;
+}
+
+constexpr int kOperandRows = 128;          // rows of A per CTA
+constexpr int kOperandSlab = 128;          // bytes of k per operand row and stage
+constexpr int kOperandStages = 8, kBlockShared = 227 * 1024;
+
+// The ring of operands: stages of aRows + bRows rows, `besides` bytes of other uses behind the last.
+struct OperandRing { int32_t stageBytes, stages, bytes; };
+inline OperandRing ring_of(int32_t aRows, int32_t bRows, int32_t besides)
+{
+    OperandRing r;
+    r.stageBytes = (aRows + bRows) * kOperandSlab;
+    r.stages = std::min(kOperandStages, (kBlockShared - besides) / r.stageBytes);
+    // (the instruction reads 128 rows of A wherever a stage begins: those behind few rows have to lie inside, too)
+    r.bytes = std::max(r.stages * r.stageBytes + besides, (r.stages - 1) * r.stageBytes + kOperandRows * kOperandSlab);
+    return r;
 }
 
 }  // namespace rcd

@@ -1,5 +1,5 @@
 // The order in which a product's tiles are walked through (csrc/rcd_walk.h): every tile once, whatever the bands; of symmetric products the blocks on
-// and below the diagonal, those below it with their transposes.
+// and below the diagonal, those below it with their transposes.  And the shared memory that a block asks for.
 #include <cmath>
 #include <cstdio>
 #include <set>
@@ -39,6 +39,16 @@ int main()
                     if (t.m < 0 || i >= blocks || t.n < 0 || j > i || t.mirror != (i != j) || t.batch || t.split) return fail("wrong", blocks, subM, u);
                     if (!seen.insert({t.m, t.n}).second) return fail("twice", blocks, subM, u);
                 }
+            }
+    // Shared memory: what an instruction reads of A (128 rows) and of B lies inside, whatever lies behind the ring; and a block gets no more than there is.
+    for (int rows = 1; rows <= 128; ++rows)
+        for (int tn = 16; tn <= 256; tn += 16)
+            for (int besides = 0; besides < 90 * 1024; besides += 1021) {
+                const int aRows = (rows + 7) / 8 * 8;
+                const OperandRing r = ring_of(aRows, tn, besides);
+                const int last = (r.stages - 1) * r.stageBytes;
+                if (r.stages < 2 || r.bytes > kBlockShared || r.stages * r.stageBytes + besides > r.bytes) return fail("shared memory", rows, tn, besides);
+                if (last + 128 * kOperandSlab > r.bytes || last + (aRows + tn) * kOperandSlab > r.bytes) return fail("read outside", rows, tn, besides);
             }
     return 0;
 }

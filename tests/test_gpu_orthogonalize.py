@@ -59,7 +59,8 @@ def check(o, g, **kw):
 
 
 SIZES = [(1, 1, 1), (1, 1, 64), (2, 3, 1), (1, 16, 16), (3, 33, 65), (1, 64, 64), (2, 64, 200), (1, 127, 129), (1, 128, 128), (5, 130, 70), (1, 200, 1000), (2, 256, 256), (1, 333, 1001),
-         (3, 320, 320), (1, 512, 2048), (2, 513, 300), (1, 777, 777), (1, 1024, 1024), (1, 2048, 512), (16, 96, 160), (150, 40, 64), (2, 128, 384), (1, 100, 500), (2, 1500, 60), (1, 128, 2050), (1, 30, 4096), (2, 6100, 128), (40, 77, 300)]
+         (3, 320, 320), (1, 512, 2048), (2, 513, 300), (1, 777, 777), (1, 1024, 1024), (1, 2048, 512), (16, 96, 160), (150, 40, 64), (2, 128, 384), (1, 100, 500), (2, 1500, 60), (1, 128, 2050), (1, 30, 4096), (2, 6100, 128), (40, 77, 300), (12, 300, 310), (20, 200, 150), (4, 300, 1000),
+         (4, 1100, 290)]
 
 
 @pytest.mark.parametrize("batch,rows,cols", SIZES)
