@@ -5,10 +5,10 @@
 // CTAs' order and push their rows of A to all.  B = b A + c A A and the columns' update are then each CTA's own business.  Nothing but G and the result touches memory,
 // and what a step waits for are two exchanges within the cluster where the other forms wait for three barriers over the grid or three launches.
 //
-// 128 x 128 takes 23 us (all steps in one launch with barriers over the grid: 64), 128 x 2048 53 (82), 16 of 128 x 512 51 (81).  Of the last but one's 94 000 cycles a step takes
-// 15 000: the products 4500, the two exchanges with their sums 7300 (latency: 56 KB come and go per CTA), the finishing of B and X 3000.
+// 128 x 128 takes 22 us (all steps in one launch with barriers over the grid: 64), 128 x 2048 51 (82), 16 of 128 x 512 46 (81).  Of the last but one's time a step takes
+// 14 000 cycles: the products 4500, the two exchanges with their sums 7000 (latency: 56 KB come and go per CTA), the finishing of B and X the rest.
 //
-// All 256 threads go through the stages together; thread 0 issues the products.  Every wait is bounded: whoever waits in vain makes its CTA leave, and the others of
+// All threads go through the stages together; thread 0 issues the products.  Every wait is bounded: whoever waits in vain makes its CTA leave, and the others of
 // the cluster behind it.
 #include "rcd_orthogonal.h"
 #include "rcd_tc.cuh"
@@ -17,7 +17,7 @@ namespace rcd {
 
 namespace {
 
-constexpr int kSide = 128, kThreads = 256, kSlabBytes = kSide * 128, kMostSlabs = 6, kMostCluster = 16;
+constexpr int kSide = 128, kMostThreads = 512, kSlabBytes = kSide * 128, kMostSlabs = 6, kMostCluster = 16;
 constexpr int kSquare = 2 * kSlabBytes;                                // A or B: 128 x 128 fp16
 constexpr int kExchange = kSide * kSide * 4;
 constexpr uint32_t kWaitTurns = 1u << 16;                              // of at most 20 us: a second or so
@@ -25,7 +25,7 @@ constexpr uint32_t kWaitTurns = 1u << 16;                              // of at 
 struct __align__(16) ClusterShared {
     uint64_t product, sums, square;        // a product is complete; the cluster's sums of my rows are here; all of A is
     double squares;                        // of this CTA's columns
-    double reduce[kThreads / 32];
+    double reduce[kMostThreads / 32];
     uint32_t tmemBase;
     int32_t abort;
 };
@@ -95,16 +95,23 @@ __device__ __forceinline__ Pack<T, 8> load_eight(const T *g, int64_t ld, int row
     return v;
 }
 
-// kWhole: rows of a G that is not tall start on 16 bytes and are a multiple of eight long.
-template <typename T, bool kTall, bool kWhole>
-__global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(const __grid_constant__ ClusterParams p)
+// 512 threads finish the sums of a cluster's CTA sooner (128 x 2048: 51.7 us with them, 53.8 with 256); of CTAs that are alone with a short matrix two go to an SM, if they have 256
+// (200 of 128 x 128: 31 us, 46 with 512).
+template <bool kAlone> constexpr int kThreadsFor = kAlone ? 256 : kMostThreads;
+
+// kAlone: a cluster of one.  kWhole: rows of a G that is not tall start on 16 bytes and are a multiple of eight long.
+template <typename T, bool kTall, bool kWhole, bool kAlone>
+__global__ void __launch_bounds__(kThreadsFor<kAlone>, 1) newton_schulz_cluster_kernel(const __grid_constant__ ClusterParams p)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
-    const int slabs = p.slabs, C = p.cluster, rank = (int)blockIdx.x % C, columns = slabs * 64;
+    constexpr int kThreads = kThreadsFor<kAlone>;
+    const int slabs = p.slabs, C = kAlone ? 1 : p.cluster, rank = (int)blockIdx.x % C, columns = slabs * 64;
     unsigned char *const x = smem, *const a = x + slabs * kSlabBytes, *const b = a + kSquare;
     float *const exchange = reinterpret_cast<float *>(b + kSquare);
     ClusterShared &sh = *reinterpret_cast<ClusterShared *>(b + kSquare + (C > 1 ? kExchange : 0));
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q = warp & 3, row = q * 32 + lane;
+    constexpr int parts = kThreads / kSide;                            // a warp takes every second part of 32 columns of its 32 rows, or every fourth
+    const int part0 = warp >> 2;
     const int64_t matrix = blockIdx.x / C;
     const uint32_t tmemColumns = columns <= 128 ? 256 : 512;           // 128 for the squares, the rest for X
 
@@ -220,20 +227,19 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const float alpha = down * (f * f);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 4 / parts; ++h) {
+            const int part = part0 + h * parts;
             uint32_t v[32];
-            const int col = half * 64 + h * 32;
-            sums_of((uint32_t)col, v);
+            sums_of((uint32_t)(part * 32), v);
             if (C == 1) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     auto z = [&](int j) { return __uint_as_float(v[8 * k + j]) * alpha; };
-                    *reinterpret_cast<uint4 *>(a + half * kSlabBytes + slab_at(row, 4 * h + k)) = make_uint4(halves(z(0), z(1)), halves(z(2), z(3)), halves(z(4), z(5)), halves(z(6), z(7)));
+                    *reinterpret_cast<uint4 *>(a + part / 2 * kSlabBytes + slab_at(row, part % 2 * 4 + k)) = make_uint4(halves(z(0), z(1)), halves(z(2), z(3)), halves(z(4), z(5)), halves(z(6), z(7)));
                 }
             } else {
                 // a row's 128 sums are four times 128 bytes: those of my own rows where they are added up, the others' in the places of that row of A and B
-                const int piece = 2 * half + h;
-                unsigned char *const to = row / owned == rank ? (unsigned char *)exchange + ((rank * 4 + piece) * owned + row % owned) * 128 : quarter(piece) + row * 128;
+                unsigned char *const to = row / owned == rank ? (unsigned char *)exchange + ((rank * 4 + part) * owned + row % owned) * 128 : quarter(part) + row * 128;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) *reinterpret_cast<uint4 *>(to + ((k ^ (row & 7)) << 4)) = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
             }
@@ -248,10 +254,11 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
                 push(cluster_addr(exchange + (rank * 4 + piece) * owned * 32, owner), quarter(piece) + owner * owned * 128, (uint32_t)owned * 128, cluster_addr(&sh.sums, owner));
             }
             if (!(ok = all_wait_for(&sh.sums, i & 1, &sh))) break;
-            // 2 C threads a row, 64 / C columns each: four at a time
-            const int r = threadIdx.x / (2 * C), mine = rank * owned + r, share = 64 / C;
-            for (int col = threadIdx.x % (2 * C) * share, end = col + share; col < end; col += 4) {
+            // four columns at a time, 32 pieces of a row
+            for (int piece = threadIdx.x; piece < owned * 32; piece += kThreads) {
+                const int r = piece / 32, mine = rank * owned + r, col = piece % 32 * 4;
                 float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
                 for (int k = 0; k < C; ++k) {
                     const float4 from = *reinterpret_cast<const float4 *>(exchange + ((k * 4 + col / 32) * owned + r) * 32 + (((col % 32 / 4) ^ (mine & 7)) << 2));
                     z.x += from.x; z.y += from.y; z.z += from.z; z.w += from.w;
@@ -279,12 +286,13 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const float polyAlpha = c[2] * down, polyBeta = c[1];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 4 / parts; ++h) {
+            const int part = part0 + h * parts;
             uint32_t v[32];
-            sums_of((uint32_t)(half * 64 + h * 32), v);
+            sums_of((uint32_t)(part * 32), v);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int at = half * kSlabBytes + slab_at(row, 4 * h + k);
+                const int at = part / 2 * kSlabBytes + slab_at(row, part % 2 * 4 + k);
                 const uint4 old = *reinterpret_cast<const uint4 *>(a + at);
                 const uint32_t w[4] = {old.x, old.y, old.z, old.w};
                 uint32_t z[4];
@@ -309,7 +317,8 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const bool last = i == p.steps - 1;
         const float xAlpha = (last ? down * down : down) * f, xBeta = (last ? down : 1.0f) * c[0] * f;
-        for (int n = 0; n < slabs; ++n) {
+        for (int part = part0; part < 2 * slabs; part += parts) {
+            const int n = part / 2, half = part % 2;
             uint32_t v[32];
             sums_of((uint32_t)(kSide + 64 * n + half * 32), v);
 #pragma unroll
@@ -354,11 +363,13 @@ __global__ void __launch_bounds__(kThreads, 1) newton_schulz_cluster_kernel(cons
 int shared_bytes(int cluster, int slabs) { return slabs * kSlabBytes + 2 * kSquare + (cluster > 1 ? kExchange : 0) + (int)sizeof(ClusterShared); }
 
 typedef void (*ClusterKernel)(ClusterParams);
-template <typename T>
+template <typename T, bool kAlone>
 ClusterKernel kernel_for(bool tall, bool whole)
 {
-    return tall ? newton_schulz_cluster_kernel<T, true, false> : whole ? newton_schulz_cluster_kernel<T, false, true> : newton_schulz_cluster_kernel<T, false, false>;
+    return tall ? newton_schulz_cluster_kernel<T, true, false, kAlone> : whole ? newton_schulz_cluster_kernel<T, false, true, kAlone> : newton_schulz_cluster_kernel<T, false, false, kAlone>;
 }
+template <typename T>
+ClusterKernel kernel_for(bool alone, bool tall, bool whole) { return alone ? kernel_for<T, true>(tall, whole) : kernel_for<T, false>(tall, whole); }
 
 }  // namespace
 
@@ -367,7 +378,7 @@ static bool sixteen(rcd_ctx *ctx)
 {
     if (ctx->clusterSixteen < 0) {
         ctx->clusterSixteen = 0;
-        auto *kernel = newton_schulz_cluster_kernel<float, true, false>;
+        auto *kernel = newton_schulz_cluster_kernel<float, true, false, false>;
         const int bytes = shared_bytes(kMostCluster, kMostSlabs);
         int n = 0;
         cudaLaunchAttribute attr;
@@ -376,7 +387,7 @@ static bool sixteen(rcd_ctx *ctx)
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cudaLaunchConfig_t config{};
         config.gridDim = dim3(kMostCluster);
-        config.blockDim = dim3(kThreads);
+        config.blockDim = dim3(kMostThreads);
         config.dynamicSmemBytes = (size_t)bytes;
         config.attrs = &attr;
         config.numAttrs = 1;
@@ -419,8 +430,10 @@ rcd_status launch_cluster(rcd_ctx *ctx, const rcd_orthogonalize_args &a, int clu
     for (int i = 0; i < 3 * a.steps; ++i) p.coefficients[i] = a.coefficients_host[i];
     const int64_t eb = elem_bytes(a.type);
     const bool whole = rows_aligned(a.g_dev, a.ld_g, eb, 16) && a.cols % 8 == 0 && (a.batch == 1 || a.step_g * eb % 16 == 0);
-    const ClusterKernel kernel = a.type == RCD_ELEM_BF16 ? kernel_for<__nv_bfloat16>(p.tall, whole) : a.type == RCD_ELEM_F16 ? kernel_for<__half>(p.tall, whole) : kernel_for<float>(p.tall, whole);
-    const int bit = 3 * (a.type == RCD_ELEM_BF16 ? 0 : a.type == RCD_ELEM_F16 ? 1 : 2) + (p.tall ? 0 : whole ? 1 : 2);
+    const bool alone = cluster == 1;
+    const ClusterKernel kernel = a.type == RCD_ELEM_BF16 ? kernel_for<__nv_bfloat16>(alone, p.tall, whole) : a.type == RCD_ELEM_F16 ? kernel_for<__half>(alone, p.tall, whole)
+                                                                                                                          : kernel_for<float>(alone, p.tall, whole);
+    const int bit = 3 * (a.type == RCD_ELEM_BF16 ? 0 : a.type == RCD_ELEM_F16 ? 1 : 2) + (p.tall ? 0 : whole ? 1 : 2) + (alone ? 9 : 0);
     if (!(ctx->clusterReady >> bit & 1)) {
         RCD_CUDA(ctx, allow_shared(kernel, shared_bytes(2, kMostSlabs)));
         RCD_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
@@ -434,7 +447,7 @@ rcd_status launch_cluster(rcd_ctx *ctx, const rcd_orthogonalize_args &a, int clu
     attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t config{};
     config.gridDim = dim3((unsigned)(a.batch * cluster));
-    config.blockDim = dim3(kThreads);
+    config.blockDim = dim3(alone ? kThreadsFor<true> : kThreadsFor<false>);
     config.dynamicSmemBytes = (size_t)shared_bytes(cluster, p.slabs);
     config.stream = st;
     config.attrs = attrs;
