@@ -32,9 +32,10 @@ constexpr int kEpiWarps = 8;
 // fp32 outputs: 512 k (2.4e-6 within a chunk, bf16 2.3e-7, and half a unit of fp32 at most for each of them).  16-bit outputs: 2048 k (1.3e-5)
 // where a piece has more than 4096, up to which the loss is a twentieth of fp16's half step.  (Gradients of 2048 x 2048 weights over 600 000
 // rows: 3.56 ms in chunks, 3.45 in one sum.)
-// Logits whose gradients are summed over the rows in fp32 (a head's dbias, where p and the labels nearly cancel): 256 k.  Of 5000 x 2048 over 1000 classes dbias is
-// 1.5e-5 off in one sum, 3.3e-6 in chunks of 512, 1.6e-6 of 256, 7.8e-7 of 128 (fp32 products 8e-7); the call takes 89, 96, 99 and 106 us.
-constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32, kChunkSlabsSums = 4;
+// Logits whose gradients are summed over the rows in fp32 (a head's dbias, where p and the labels nearly cancel, and what all rows' z have lost adds up): 128 k, which is as exact as
+// fp32 products.  Of 5000 x 2048 over 1000 classes dbias is 1.5e-5 off in one sum, 3.3e-6 in chunks of 512, 1.6e-6 of 256, 7.8e-7 of 128, 4.3e-7 of 64 (fp32 products 8.1e-7); the call
+// takes 89, 96, 100, 106 and 117 us.  What is left comes from the chunks: with exp to the last bit it is the same.
+constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32, kChunkSlabsSums = 2;
 constexpr int kFirstEpiWarp = 4;                        // (a warpgroup for the two that issue: registers are handed over by warpgroups)
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
 // Registers per thread at launch (65536 over 12 warps in whole eights), and how the warpgroups split them: 128 x 40 + 256 x 232 = 384 x 168.  (With 168 for all, sums of
