@@ -115,7 +115,6 @@ __global__ void __launch_bounds__(kThreadsFor<kAlone>, 1) newton_schulz_cluster_
     const int64_t matrix = blockIdx.x / C;
     const uint32_t tmemColumns = columns <= 128 ? 256 : 512;           // 128 for the squares, the rest for X
 
-    after_the_one_before();
     if (threadIdx.x == 0) {
         mbar_init(&sh.product, 1);
         mbar_init(&sh.sums, 1);
@@ -127,6 +126,9 @@ __global__ void __launch_bounds__(kThreadsFor<kAlone>, 1) newton_schulz_cluster_
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_addr(&sh.tmemBase)), "r"(tmemColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    // The launch behind this one may begin when all CTAs have their tensor memory: it may ask for all of it, and keeps it while it waits for this one's end.
+    __syncthreads();
+    after_the_one_before();
 
     // The norm: each CTA's columns, then the cluster's in their order.
     const T *const g = (const T *)p.g + matrix * p.stepG;
