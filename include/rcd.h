@@ -499,7 +499,7 @@ RCD_API rcd_status rcd_linear_cross_entropy(rcd_ctx *ctx, const rcd_cross_entrop
  *   p = exp(z - lse),  dz = (dloss + dlse) p, less dloss in the label's column;  dx = dz w,  dw = dz^T x,  dbias = sum over the rows of dz.
  * dloss counts as 0 where the label is negative (or n or more: RCD_ERR_INVALID_ARG from rcd_sync_status); p is 0 where lse is -infinity, and dz where dloss
  * and dlse are 0.  (x of such rows has to be finite all the same: dw multiplies it by 0.)  dz is rounded to `type` for the products, as a
- * tensor-core operand has to be (fp16: times a power of two by the largest dloss + dlse, so that 2^-38 of that is still held); dbias takes it unrounded.
+ * tensor-core operand has to be (fp16: times a power of two by the largest finite |dloss| + |dlse|, so that 2^-38 of that is still held); dbias takes it unrounded.
  * Workspace: dz of a piece, and where there are several dx in fp32. */
 typedef struct {
     int64_t rows, n, k;

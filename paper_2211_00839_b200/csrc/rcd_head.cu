@@ -49,20 +49,26 @@ __global__ void __launch_bounds__(1024) join_loss_kernel(const float2 *__restric
 }
 
 // fp16: a power of two that brings the largest gradient of a logit to 2^13..2^14, so that those 2^-38 of it are still held (p is small almost
-// everywhere, and a mean's dloss is 1 / rows); up[1] takes it out of the products again.
-__global__ void __launch_bounds__(1024) choose_up_kernel(const float *__restrict__ dloss, const float *__restrict__ dlse, int64_t rows, float *__restrict__ up)
+// everywhere, and a mean's dloss is 1 / rows); up[1] takes it out of the products again.  dloss counts where a row's gradients take it, and what is not
+// finite does not: other rows keep their digits beside it.
+__global__ void __launch_bounds__(1024) choose_up_kernel(const float *__restrict__ dloss, const float *__restrict__ dlse, const int32_t *__restrict__ labels, int32_t classes, int64_t rows,
+                                                         float *__restrict__ up)
 {
     after_the_one_before();
     __shared__ float sh[32];
     float most = 0.0f;
-    for (int64_t r = threadIdx.x; r < rows; r += 1024) most = fmaxf(most, fabsf(dloss ? dloss[r] : 1.0f) + (dlse ? fabsf(dlse[r]) : 0.0f));
+    for (int64_t r = threadIdx.x; r < rows; r += 1024) {
+        const int32_t label = labels[r];
+        const float g = label < 0 || label >= classes ? 0.0f : dloss ? fabsf(dloss[r]) : 1.0f, size = g + (dlse ? fabsf(dlse[r]) : 0.0f);
+        if (size < INFINITY) most = fmaxf(most, size);
+    }
     for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = most;
     __syncthreads();
     if (threadIdx.x) return;
     for (int i = 1; i < 32; ++i) most = fmaxf(most, sh[i]);
     int e = 0;
-    if (most > 0.0f && most < INFINITY) e = 13 - ilogbf(most);
+    if (most > 0.0f) e = 13 - ilogbf(most);
     e = max(-100, min(100, e));
     up[0] = ldexpf(1.0f, e);
     up[1] = ldexpf(1.0f, -e);
@@ -334,7 +340,8 @@ extern "C" rcd_status rcd_linear_cross_entropy_backward(rcd_ctx *ctx, const rcd_
     unsigned char *ws = (unsigned char *)workspace_dev;
     BackPlan b = back_plan(ctx, a, ws, 0);
     if (a.type == RCD_ELEM_F16) {
-        RCD_TRY(launch_early(ctx, choose_up_kernel, dim3(1), 1024, st, a.dloss_dev_or_null, a.dlse_dev_or_null, a.rows, (float *)(ws + b.up)));
+        RCD_TRY(launch_early(ctx, choose_up_kernel, dim3(1), 1024, st, a.dloss_dev_or_null, a.dlse_dev_or_null, a.labels_dev, (int32_t)a.n, a.rows,
+                             (float *)(ws + b.up)));
     }
     if (b.packX) RCD_TRY(launch_pack(ctx, a.x_dev, a.ldx, a.rows, a.k, eb, ws + b.x, b.ldPacked, st));
     for (int64_t i = 0; i < b.pieces; ++i) {
