@@ -44,10 +44,12 @@ __global__ void __launch_bounds__(256) join_kernel(const void *__restrict__ part
         if (e.ws) z[j] *= e.ws[n + j];
         if (e.bias) z[j] += e.bias[n + j];
     }
-    const int64_t eb = e.type == RCD_ELEM_F32 ? 4 : 2;
-    auto whole = [&](const void *base, int64_t ld2) { return n + 4 <= N && (((uintptr_t)base + (uintptr_t)((m * ld2 + n) * eb)) % (4 * eb)) == 0; };
+    auto whole = [&](const void *base, int64_t ld2, rcd_elem type) {
+        const int64_t eb = type == RCD_ELEM_F32 ? 4 : 2;
+        return n + 4 <= N && (((uintptr_t)base + (uintptr_t)((m * ld2 + n) * eb)) % (4 * eb)) == 0;
+    };
     auto put = [&](void *base, int64_t ld2, const float (&v)[4]) {
-        if (whole(base, ld2)) store_typed<4>(base, m * ld2 + n, e.type, v);
+        if (whole(base, ld2, e.type)) store_typed<4>(base, m * ld2 + n, e.type, v);
         else
             for (int j = 0; j < 4 && n + j < N; ++j) { const float o[1] = {v[j]}; store_typed<1>(base, m * ld2 + n + j, e.type, o); }
     };
@@ -56,9 +58,10 @@ __global__ void __launch_bounds__(256) join_kernel(const void *__restrict__ part
     const float f = sc.factor ? *sc.factor : 1.0f, beta = sc.beta * (sc.betaPower == 0 ? 1.0f : sc.betaPower == 1 ? f : f * f);
     if (e.residual) {
         float r[4] = {0, 0, 0, 0};
-        if (whole(e.residual, e.ldr)) load_typed<4>(r, e.residual, m * e.ldr + n, e.type);
+        // (its type may be another: an update's last product adds fp16 to what leaves as bf16)
+        if (whole(e.residual, e.ldr, sc.residualType)) load_typed<4>(r, e.residual, m * e.ldr + n, sc.residualType);
         else
-            for (int j = 0; j < 4 && n + j < N; ++j) { float o[1]; load_typed<1>(o, e.residual, m * e.ldr + n + j, e.type); r[j] = o[0]; }
+            for (int j = 0; j < 4 && n + j < N; ++j) { float o[1]; load_typed<1>(o, e.residual, m * e.ldr + n + j, sc.residualType); r[j] = o[0]; }
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[j] = fmaf(beta, r[j], z[j]);
     }
