@@ -32,9 +32,12 @@ constexpr int kEpiWarps = 8;
 // fp32 outputs: 512 k (2.4e-6 within a chunk, bf16 2.3e-7, and half a unit of fp32 at most for each of them).  16-bit outputs: 2048 k (1.3e-5)
 // where a piece has more than 4096, up to which the loss is a twentieth of fp16's half step.  (Gradients of 2048 x 2048 weights over 600 000
 // rows: 3.56 ms in chunks, 3.45 in one sum.)
-// Logits whose gradients are summed over the rows in fp32 (a head's dbias, where p and the labels nearly cancel, and what all rows' z have lost adds up): 128 k, which is as exact as
-// fp32 products.  Of 5000 x 2048 over 1000 classes dbias is 1.5e-5 off in one sum, 3.3e-6 in chunks of 512, 1.6e-6 of 256, 7.8e-7 of 128, 4.3e-7 of 64 (fp32 products 8.1e-7); the call
-// takes 89, 96, 100, 106 and 117 us.  What is left comes from the chunks: with exp to the last bit it is the same.
+// Logits whose gradients are summed over the rows in fp32 (a head's dbias, where p and the labels nearly cancel, and what all rows' z have lost adds up): 128 k, which from some 1000
+// classes on is as exact as fp32 products.  Of 5000 x 2048 over 1000 classes dbias is 1.5e-5 off in one sum, 3.3e-6 in chunks of 512, 1.6e-6 of 256, 7.8e-7 of 128, 4.3e-7 of 64 (fp32
+// products 8.4e-7); the call takes 89, 98, 102, 106 and 119 us.  What is left comes from the chunks: with exp to the last bit it is the same.  Fewer classes have larger p, which
+// lose the same way in every row: 12 237 x 1914 over 97 classes 2.2e-6 in chunks of 128 and 1.3e-6 of 64 (0.7e-6), 20 000 x 2048 over ten 4.5e-6 and 2.5e-6 (0.7e-6; 117 and 128 us).
+// The loss adds up 512 k; its lse is 2e-6 low, and dbias from it off by 2.7e-6 and 1.5e-5 of the true one on 1000 and 10 classes.  With chunks of 128 in the loss, too, those would be 2e-7,
+// but 8192 x 4096 over 32 768 classes would take 2.15 ms for 1.46, 5000 x 2048 over 1000 40 us for 30.
 constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32, kChunkSlabsSums = 2;
 constexpr int kFirstEpiWarp = 4;                        // (a warpgroup for the two that issue: registers are handed over by warpgroups)
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
