@@ -192,8 +192,8 @@ RCD_API rcd_status rcd_sync_status(rcd_ctx *ctx, void *cuda_stream);
  * quotas end before its samples: they have to record that and to write no outputs (RCD_ERR_INTERNAL otherwise; waits for
  * the stream).  Then it enqueues a one-CTA kernel that arrives at a grid barrier expecting two
  * arrivals, one whose threads wait for copies that nobody makes (the loop in rounds: all have to leave at the same
- * step), and two that wait so as the norms, the products and the
- * orthogonalised updates do.  The waits give up after a few thousand polls and record the
+ * step), and three that wait so as the norms and products, the orthogonalised
+ * updates' count over the grid and their clusters do.  The waits give up after a few thousand polls and record the
  * timeout in the context's status words, so the next rcd_sync_status returns RCD_ERR_TIMEOUT (RCD_ERR_INTERNAL if the threads did not leave together) and the context
  * stays usable.  Nothing faults or hangs. */
 RCD_API rcd_status rcd_selftest_bounded_wait(rcd_ctx *ctx, void *cuda_stream);

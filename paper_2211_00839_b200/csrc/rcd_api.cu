@@ -562,7 +562,8 @@ rcd_status rcd_selftest_bounded_wait(rcd_ctx *ctx, void *cuda_stream)
     rs = launch_bounded_wait_selftest(ctx, (unsigned *)(ctx->statusOwn + 8), ctx->statusOwn, st);
     if (rs == RCD_OK) rs = launch_step_wait_selftest(ctx, ctx->statusOwn, st);
     if (rs == RCD_OK) rs = launch_operator_wait_selftest(ctx, ctx->statusOwn + kOperatorStatus, st);
-    return rs == RCD_OK ? launch_fused_wait_selftest(ctx, ctx->statusOwn + kOperatorStatus, st) : rs;
+    if (rs == RCD_OK) rs = launch_fused_wait_selftest(ctx, ctx->statusOwn + kOperatorStatus, st);
+    return rs == RCD_OK ? launch_cluster_wait_selftest(ctx, ctx->statusOwn + kOperatorStatus, st) : rs;
 }
 
 rcd_status rcd_get_profile(rcd_ctx *ctx, rcd_profile *out)

@@ -393,6 +393,7 @@ rcd_status launch_bounded_wait_selftest(rcd_ctx *ctx, unsigned *counter, int32_t
 rcd_status launch_step_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st);
 rcd_status launch_operator_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st);
 rcd_status launch_fused_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st);
+rcd_status launch_cluster_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st);
 
 // graph-cut objective: the whole greedy loop, and f from an assignment (selftest: in step, on two CTAs, whatever the plan says)
 rcd_status launch_cut_stopped_selftest(rcd_ctx *ctx, const Sizes &sz, const Workspace &ws, int32_t *assignment, int32_t *order, cudaStream_t st);

@@ -30,9 +30,9 @@ struct __align__(16) ClusterShared {
     int32_t abort;
 };
 
-__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, ClusterShared *sh)
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, ClusterShared *sh, uint32_t turns)
 {
-    for (uint32_t turn = 0; turn < kWaitTurns; ++turn) {
+    for (uint32_t turn = 0; turn < turns; ++turn) {
         uint32_t ok;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity), "r"(20000) : "memory");
@@ -43,7 +43,10 @@ __device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Cluster
     return false;
 }
 // All threads: whether all have seen the phase end.
-__device__ __forceinline__ bool all_wait_for(uint64_t *bar, uint32_t parity, ClusterShared *sh) { return __syncthreads_and(wait_for(bar, parity, sh)); }
+__device__ __forceinline__ bool all_wait_for(uint64_t *bar, uint32_t parity, ClusterShared *sh, uint32_t turns = kWaitTurns)
+{
+    return __syncthreads_and(wait_for(bar, parity, sh, turns));
+}
 __device__ __forceinline__ uint32_t cluster_addr(const void *p, int rank)
 {
     uint32_t a;
@@ -362,6 +365,22 @@ __global__ void __launch_bounds__(kThreadsFor<kAlone>, 1) newton_schulz_cluster_
     if (threadIdx.x == 0 && !ok) atomicOr(p.status, kDevTimeout);
 }
 
+// A cluster's waits for sums that nobody sends: the first has to run out for every thread, and the one behind it to be given up at once.
+__global__ void __launch_bounds__(64) cluster_wait_selftest_kernel(int32_t *status)
+{
+    __shared__ ClusterShared sh;
+    if (threadIdx.x == 0) {
+        mbar_init(&sh.sums, 1);
+        mbar_init(&sh.square, 1);
+        sh.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    const bool came = all_wait_for(&sh.sums, 0, &sh, 1u << 5);
+    const bool then = all_wait_for(&sh.square, 0, &sh);
+    if (threadIdx.x == 0) atomicOr(status, came || then || !sh.abort ? kDevBadState : kDevTimeout);
+}
+
 int shared_bytes(int cluster, int slabs) { return slabs * kSlabBytes + 2 * kSquare + (cluster > 1 ? kExchange : 0) + (int)sizeof(ClusterShared); }
 
 typedef void (*ClusterKernel)(ClusterParams);
@@ -374,6 +393,14 @@ template <typename T>
 ClusterKernel kernel_for(bool alone, bool tall, bool whole) { return alone ? kernel_for<T, true>(tall, whole) : kernel_for<T, false>(tall, whole); }
 
 }  // namespace
+
+rcd_status launch_cluster_wait_selftest(rcd_ctx *ctx, int32_t *status, cudaStream_t st)
+{
+    cluster_wait_selftest_kernel<<<1, 64, 0, st>>>(status);
+    ctx->kernelLaunches++;
+    RCD_CUDA(ctx, cudaGetLastError());
+    return RCD_OK;
+}
 
 // Whether the device takes a cluster of 16 that fill an SM each.
 static bool sixteen(rcd_ctx *ctx)
