@@ -252,8 +252,8 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a, unsigned 
     b.dw.out.type = a.dw_type;
     b.dw.out.y = a.dw_dev_or_null ? (unsigned char *)a.dw_dev_or_null + first * a.ld_dw * elem_bytes(a.dw_type) : nullptr;
     b.dw.out.ldy = a.ld_dw;
-    b.dx.scaling = {1.0f, 1.0f, up ? up + 1 : nullptr, 1, 0, b.dx.out.type};
-    b.dw.scaling = {1.0f, 0.0f, up ? up + 1 : nullptr, 1, 0, b.dw.out.type};
+    b.dx.scaling = {1.0f, 1.0f, up ? up + 1 : nullptr, 1, 0, b.dx.out.type, nullptr};
+    b.dw.scaling = {1.0f, 0.0f, up ? up + 1 : nullptr, 1, 0, b.dw.out.type, nullptr};
     size_t most = product_workspace(ctx, b.z);
     if (a.dx_dev_or_null) most = std::max(most, product_workspace(ctx, b.dx));
     if (a.dw_dev_or_null) most = std::max(most, product_workspace(ctx, b.dw));

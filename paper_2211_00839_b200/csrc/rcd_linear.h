@@ -11,8 +11,9 @@ namespace rcd {
 
 // How a product ends.  kPlain: rcd_linear's epilogue, or partial sums as they are.  kLoss: every row's logits of a tile to a
 // reference and a sum of exponentials; nothing else leaves the SM.  kLogitGrads: logits to their gradients.  kScaled: alpha times the product
-// plus beta times the residual, symmetric ones from their lower half; a batch of matrices.
-enum Form { kPlain, kLoss, kLogitGrads, kScaled };
+// plus beta times the residual, symmetric ones from their lower half; a batch of matrices.  kScaledLow: the same (Product says kScaled) where the residual has a second part: a kernel
+// of its own, since those instructions in all of kScaled's cost every product 0.5 us (8 updates of 1024 x 2048 454 -> 467 us).
+enum Form { kPlain, kLoss, kLogitGrads, kScaled, kScaledLow };
 
 // What is done with an accumulator on its way out: z = acc [* xs[m] * ws[n]] + bias[n], y = act(z) + residual.
 struct Epilogue {
@@ -41,7 +42,9 @@ struct Scaling {
     const float *factor;                   // one for every matrix of the batch, or null: 1
     int32_t alphaPower, betaPower;
     rcd_elem residualType;
+    const void *low;                       // fp16, laid out as the residual, or null: what that lacks, times 2^kLowUp
 };
+constexpr int kLowUp = 11;                 // (half a step of fp16 at most of the residual's entries: as large as they are, then)
 
 // C[m][n] = sum over k of A(m, k) B(n, k).  An operand has its k elements next to each other (rows lie `ld` apart), or, with
 // `across`, its m or n elements (and steps of k are `ld` apart).
@@ -60,8 +63,8 @@ struct Product {
 };
 struct KernelChoice { const void *kernel; int bit; };          // bit: of rcd_ctx::productReady
 KernelChoice head_kernel(Form form, int wide, bool pair);
-KernelChoice scaled_kernel(int order, int wide, bool pair);
-constexpr int kPlainKernels = 20, kHeadKernels = 8;            // (and 18 scaled ones)
+KernelChoice scaled_kernel(int order, int wide, bool pair, bool low);
+constexpr int kPlainKernels = 20, kHeadKernels = 8, kScaledKernels = 18;       // (and 8 with a second part of the residual)
 
 size_t product_workspace(rcd_ctx *ctx, const Product &p);
 int64_t product_tile_columns(rcd_ctx *ctx, const Product &p);          // kLoss: of what parts holds

@@ -64,6 +64,11 @@ __global__ void __launch_bounds__(256) join_kernel(const void *__restrict__ part
             for (int j = 0; j < 4 && n + j < N; ++j) { float o[1]; load_typed<1>(o, e.residual, m * e.ldr + n + j, sc.residualType); r[j] = o[0]; }
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[j] = fmaf(beta, r[j], z[j]);
+        if (sc.low) {                                      // (rows of whole 64s)
+            load_pack<4>(r, (const __half *)sc.low + m * e.ldr + n);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] = fmaf(beta * (1.0f / (1 << kLowUp)), r[j], z[j]);
+        }
     }
     put(e.y, e.ldy, z);
 }
@@ -376,10 +381,10 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     const int order = !p.a.across && !p.b.across ? 0 : !p.a.across ? 1 : 2;
     if (p.a.across && !p.b.across) return fail(ctx, RCD_ERR_INTERNAL, "no product takes these orders");
     const int wide = !chunks ? 0 : q.e.type == RCD_ELEM_F32 ? 32 : 64;
-    const KernelChoice c = p.form == kPlain ? plain_kernel(i8, order, wide, plan.pair) : p.form == kScaled ? scaled_kernel(order, wide, plan.pair) : head_kernel(p.form, wide, plan.pair);
+    const KernelChoice c = p.form == kPlain ? plain_kernel(i8, order, wide, plan.pair) : p.form == kScaled ? scaled_kernel(order, wide, plan.pair, p.scaling.low && !q.raw) : head_kernel(p.form, wide, plan.pair);
     const rcd_status rs = run_product(ctx, c, grid, smem, maps, q, st);
     if (rs != RCD_OK || !q.raw) return rs;
-    const Scaling scaling = p.form == kScaled ? p.scaling : Scaling{1.0f, 1.0f, nullptr, 0, 0, p.out.type};
+    const Scaling scaling = p.form == kScaled ? p.scaling : Scaling{1.0f, 1.0f, nullptr, 0, 0, p.out.type, nullptr};
     const int64_t threads = p.M * ((p.N + 3) / 4);
     return launch_early(ctx, i8 ? join_kernel<true> : join_kernel<false>, dim3((unsigned)((threads + 255) / 256)), 256, st, ws + plan.partAt, plan.splits, (int32_t)p.M, plan.rowsPart,
                         (int32_t)p.N, plan.ldPart, p.out, scaling);

@@ -5,7 +5,9 @@
 // The products run on the tensor cores in fp16 with sums in fp32, and X, A and B stand between them as fp16 times 2^10: entries of X are at most 1.2
 // or so and some 1 / sqrt(cols) mostly, which is well inside the type's normal range then, and 11 bits are kept where bf16 would keep 8 (each
 // rounding grows by up to a per step where X is small: 1.1e-3 of the result's norm in fp16 for 1024 x 1024 normal values, 8.9e-3 in bf16; rounding the result
-// itself to bf16 takes 1.7e-3).  G is brought into range by a power of two alone, so that a 16-bit G is held exactly; what is left of its norm, a factor between 1 and 2, goes into the
+// itself to bf16 takes 1.7e-3).  X's roundings in the sum a X are what counts, and the earliest most, where a few strong directions make the entries and the weak ones grow: so the first
+// step adds G itself, an fp32 one as two fp16 (one direction a hundred times as strong as the noise: 2.1e-2 -> 5e-3; 8 of 1024 x 2048: 474 -> 491 us), while A and the product B X take its
+// first part alone.  G is brought into range by a power of two alone, so that a 16-bit G is held exactly; what is left of its norm, a factor between 1 and 2, goes into the
 // first step's products as a number that their epilogue reads.  A and B are symmetric: tiles on and below the diagonal are computed and
 // stored both ways.
 //
@@ -17,7 +19,14 @@
 
 namespace rcd {
 
-KernelChoice scaled_kernel(int order, int wide, bool pair) { return product_choice_by_order<kScaled>(order, wide, pair, kPlainKernels + kHeadKernels); }
+// (what has a second part is the last product of an update's step: X times a square or the other way, with an output of 16 bits)
+KernelChoice scaled_kernel(int order, int wide, bool pair, bool low)
+{
+    constexpr int bit = kPlainKernels + kHeadKernels, lowBit = bit + kScaledKernels;
+    if (!low) return product_choice_by_order<kScaled>(order, wide, pair, bit);
+    if (order == 0) return wide ? product_choice<kScaledLow, false, false, false, 64>(pair, lowBit) : product_choice<kScaledLow, false, false, false, 0>(pair, lowBit + 2);
+    return wide ? product_choice<kScaledLow, false, false, true, 64>(pair, lowBit + 4) : product_choice<kScaledLow, false, false, true, 0>(pair, lowBit + 6);
+}
 
 namespace {
 
@@ -55,9 +64,10 @@ __global__ void __launch_bounds__(256) squares_kernel(Gradient g, double *__rest
     }
 }
 
-// G times the power of two that brings |G| + eps to 2^(kUp - 1) .. 2^kUp, and the factor that is left of 2^kUp / (|G| + eps); zeros up to whole 64 rows and columns.
+// G times the power of two that brings |G| + eps to 2^(kUp - 1) .. 2^kUp, and the factor that is left of 2^kUp / (|G| + eps); zeros up to whole 64 rows and columns.  Of an
+// fp32 G also what fp16 leaves of it.
 template <typename T, int kVec>
-__global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double *__restrict__ parts, int32_t count, float eps, __half *__restrict__ x, int32_t rowsX, int32_t colsX,
+__global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double *__restrict__ parts, int32_t count, float eps, __half *__restrict__ x, __half *__restrict__ low, int32_t rowsX, int32_t colsX,
                                                        float *__restrict__ factor, uint32_t *__restrict__ counter)
 {
     after_the_one_before();
@@ -99,6 +109,11 @@ __global__ void __launch_bounds__(256) bring_up_kernel(Gradient g, const double 
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = v[j] * up0 * up1;
         store_pack<8>(to + r * colsX + c, v);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (v[j] - __half2float(__float2half_rn(v[j]))) * (float)(1 << kLowUp);
+            store_pack<8>(low + (int64_t)blockIdx.y * rowsX * colsX + r * colsX + c, v);
+        }
     }
 }
 
@@ -143,7 +158,7 @@ struct Layout {
     int32_t parts;
     FusedPlan fused;
     bool inOne;                            // all steps in one launch
-    size_t x[2], a, b, squares, factor, counter, product, bytes;
+    size_t x[2], low, a, b, squares, factor, counter, product, bytes;
 };
 // Step i's products; (first of them, second, third).
 struct Step { Product gram, poly, x; };
@@ -201,6 +216,7 @@ Step step_of(const rcd_orthogonalize_args &a, const Layout &l, unsigned char *ws
     s.x.scaling.beta = c[0];
     s.x.scaling.factor = factor;
     s.x.scaling.alphaPower = s.x.scaling.betaPower = 1;
+    s.x.scaling.low = i == 0 && a.type == RCD_ELEM_F32 ? ws + l.low : nullptr;
     if (direct) {
         s.x.M = a.rows;
         s.x.N = a.cols;
@@ -228,6 +244,7 @@ Layout layout_of(rcd_ctx *ctx, const rcd_orthogonalize_args &a)
     size_t at = 0;
     auto place = [&](size_t bytes) { const size_t here = at; at += align_up(bytes); return here; };
     for (size_t &x : l.x) x = place((size_t)(a.batch * l.rows * l.cols) * 2);
+    l.low = place(a.type == RCD_ELEM_F32 ? (size_t)(a.batch * l.rows * l.cols) * 2 : 0);
     l.a = place((size_t)(a.batch * l.side * l.side) * 2);
     l.b = place((size_t)(a.batch * l.side * l.side) * 2);
     l.squares = place((size_t)(a.batch * l.parts) * 8);
@@ -297,7 +314,7 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
         constexpr int kVec = decltype(vec)::value;
         RCD_TRY(launch_early(ctx, squares_kernel<T, kVec>, dim3((unsigned)l.parts, (unsigned)a.batch), 256, st, g, (double *)(ws + l.squares)));
         const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((l.rows * l.cols / 8 + 255) / 256, 8 * ctx->smCount / a.batch));
-        return launch_early(ctx, bring_up_kernel<T, kVec>, dim3(grid, (unsigned)a.batch), 256, st, g, (const double *)(ws + l.squares), l.parts, a.eps, (__half *)(ws + l.x[0]), (int32_t)l.rows,
+        return launch_early(ctx, bring_up_kernel<T, kVec>, dim3(grid, (unsigned)a.batch), 256, st, g, (const double *)(ws + l.squares), l.parts, a.eps, (__half *)(ws + l.x[0]), (__half *)(ws + l.low), (int32_t)l.rows,
                             (int32_t)l.cols, (float *)(ws + l.factor), l.inOne ? (uint32_t *)(ws + l.counter) : nullptr);
     };
     auto by_type = [&](auto t) {
@@ -308,6 +325,7 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
         FusedParams p{};
         p.x0 = (__half *)(ws + l.x[0]);
         p.x1 = (__half *)(ws + l.x[1]);
+        p.low = a.type == RCD_ELEM_F32 ? (const __half *)(ws + l.low) : nullptr;
         p.a = (__half *)(ws + l.a);
         p.b = (__half *)(ws + l.b);
         p.factor = (const float *)(ws + l.factor);

@@ -20,6 +20,7 @@ constexpr int kFusedUnits = 8;             // tiles per CTA and phase at most
 struct FusedPlan { bool possible; int32_t grid, cluster; double stepUs; FusedPhase phases[3]; };        // stepUs: an estimate
 struct FusedParams {
     __half *x0, *x1, *a, *b;               // [batch][rows][cols] twice, [batch][side][side] twice; whole 64s
+    const __half *low;                     // what x0 lacks of an fp32 G, times 2^kLowUp, or null
     const float *factor;                   // [batch], of the first step
     uint32_t *counter;                     // zero
     __nv_bfloat16 *o;

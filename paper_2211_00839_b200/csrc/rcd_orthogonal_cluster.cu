@@ -332,9 +332,16 @@ __global__ void __launch_bounds__(kThreadsFor<kAlone>, 1) newton_schulz_cluster_
                 const uint4 old = *at;
                 const uint32_t w[4] = {old.x, old.y, old.z, old.w};
                 float z[8];
+                [[maybe_unused]] Pack<T, 8> whole;                     // (an fp32 G itself in the first step's sum: fp16 leaves 11 bits of it)
+                if constexpr (sizeof(T) == 4) {
+                    if (i == 0) whole = load_eight<T, kTall, kWhole>(g, p.ldG, row, first + 64 * n + half * 32 + 8 * k, p.side, p.len);
+                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float2 r = floats(w[j]);
+                    float2 r = floats(w[j]);
+                    if constexpr (sizeof(T) == 4) {
+                        if (i == 0) r = make_float2(whole.v[2 * j] * up0 * up1, whole.v[2 * j + 1] * up0 * up1);
+                    }
                     z[2 * j] = fmaf(xBeta, r.x, __uint_as_float(v[8 * k + 2 * j]) * xAlpha);
                     z[2 * j + 1] = fmaf(xBeta, r.y, __uint_as_float(v[8 * k + 2 * j + 1]) * xAlpha);
                 }

@@ -247,6 +247,12 @@ newton_schulz_kernel(const __grid_constant__ CUtensorMap mapX0, const __grid_con
                             z[2 * j] = fmaf(beta, v.x, z[2 * j]);
                             z[2 * j + 1] = fmaf(beta, v.y, z[2 * j + 1]);
                         }
+                        if (ph == 2 && p.low) {
+                            float l[8];
+                            load_pack<8>(l, p.low + t.batch * whole + at);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) z[j] = fmaf(beta * (1.0f / (1 << kLowUp)), l[j], z[j]);
+                        }
                     }
                     if (last) {
                         __nv_bfloat16 *const o = p.o + t.batch * p.stepO + (int64_t)row * p.ldO + col;

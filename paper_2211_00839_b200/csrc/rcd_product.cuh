@@ -294,6 +294,7 @@ __device__ __forceinline__ float column_sum(const float (&v)[32], float *place)
 template <Form kForm, bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks, bool kPair>
 __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUtensorMap &mapB, const CUtensorMap &mapY, const CUtensorMap &mapZ, const CUtensorMap &mapR, const TcParams &p)
 {
+    constexpr bool kIsScaled = kForm == kScaled || kForm == kScaledLow;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char *const tiles = smem;
     unsigned char *const staging = smem + (size_t)p.stages * p.stageBytes;
@@ -348,7 +349,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         for (int u = first; u < p.units && ok; u += step) {
             const Unit t = unit_of(p.walk, u);
             const int m0 = t.m * rowsPerTile + rank * kRows, n0 = t.n * p.tn + rank * nMine;
-            const int aRow = kForm == kScaled ? t.batch * p.aStep : 0, bRow = kForm == kScaled ? t.batch * p.bStep : 0;
+            const int aRow = kIsScaled ? t.batch * p.aStep : 0, bRow = kIsScaled ? t.batch * p.bStep : 0;
             const int end = min(p.slabs, (t.split + 1) * p.slabsPerSplit);
             for (int kb = t.split * p.slabsPerSplit; kb < end; ++kb) {
                 if (!warp_wait_for(&sh.empty[s], phase, &sh)) { ok = false; break; }
@@ -439,8 +440,8 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         auto piece_of = [&](const Unit &t, int k, Piece *o) {
             o->row = t.m * rowsPerTile + rank * kRows + q * 32;
             o->col = t.n * p.tn + k * wide;
-            o->base = kForm == kScaled ? t.batch * p.yStep : 0;
-            o->from = kForm == kScaled ? t.batch * p.rStep : 0;
+            o->base = kIsScaled ? t.batch * p.yStep : 0;
+            o->from = kIsScaled ? t.batch * p.rStep : 0;
             return o->row < p.M && o->col < p.N;
         };
         // the residual of the next piece that has one, from piece k of t, which is unit u, on, is on its way into buffer `to`
@@ -458,7 +459,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 k = half;
             }
         };
-        const bool mirrors = kForm == kScaled && p.walk.subM != 0;
+        const bool mirrors = kIsScaled && p.walk.subM != 0;
         const bool sums = kForm == kLogitGrads && p.head.sums != nullptr;
         const bool alternate = p.places == 2 && e.z == nullptr && !mirrors && !sums;      // two places in turn, or one for y and one for z, the transpose or sums; or only the one
         uint32_t nt = 0, turn = 0;
@@ -548,7 +549,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                     r.atLabel = g * up;
                 }
             }
-            if constexpr (kForm == kScaled) {
+            if constexpr (kIsScaled) {
                 const Scaling &sc = p.s;
                 const float f = sc.factor ? sc.factor[t.batch] : 1.0f;
                 auto power = [&](int n) { return n == 0 ? 1.0f : n == 1 ? f : f * f; };
@@ -562,10 +563,25 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         auto finish = [&](float (&z)[32], const Row &r, int h, int c, const Piece &o) {
             if (p.raw) {
                 // (as they are)
-            } else if constexpr (kForm == kScaled) {
+            } else if constexpr (kIsScaled) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j) z[j] *= r.alpha;
                 if (e.residual) add_row(yPiece, lane, h / 8, z, p.s.residualType, r.beta);
+                if (kForm == kScaledLow && o.row + lane < p.M) {       // (rows of whole 64s: straight from memory, in one product of an update)
+                    const uint4 *const low = reinterpret_cast<const uint4 *>((const __half *)p.s.low + ((int64_t)o.from + o.row + lane) * e.ldr + o.col + h);
+                    const float beta = r.beta * (1.0f / (1 << kLowUp));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 x = low[i];
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 f = unpack2(w[j], RCD_ELEM_F16);
+                            z[8 * i + 2 * j] = fmaf(beta, f.x, z[8 * i + 2 * j]);
+                            z[8 * i + 2 * j + 1] = fmaf(beta, f.y, z[8 * i + 2 * j + 1]);
+                        }
+                    }
+                }
                 if (r.mirror) {                                        // (rows of 64 bytes: a lane's row is a column there)
 #pragma unroll
                     for (int j = 0; j < 32; j += 2) {
@@ -646,7 +662,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 }
             };
             send(p.tmaY, &mapY, yPiece, e.y, e.ldy, rowBase + o.base);
-            if (kForm == kScaled) {
+            if (kIsScaled) {
                 if (t.mirror && lane == 0) tma_store_2d(&mapZ, zPiece, o.row, o.base + o.col);
             } else if (e.z) {
                 send(p.tmaZ, &mapZ, zPiece, e.z, e.ldz, 0);
