@@ -188,14 +188,14 @@ rcd_status check_floats(rcd_ctx *ctx, const char *name, const float *p)
     return RCD_OK;
 }
 
-static bool meet(const Area &a, const Area &b) { return ranges_meet(a.p, a.rows, a.ld, a.len, a.bytes, b.p, b.rows, b.ld, b.len, b.bytes); }
+bool areas_meet(const Area &a, const Area &b) { return ranges_meet(a.p, a.rows, a.ld, a.len, a.bytes, b.p, b.rows, b.ld, b.len, b.bytes); }
 rcd_status check_apart(rcd_ctx *ctx, const Area *out, int outs, const Area *in, int ins)
 {
     for (int i = 0; i < outs; ++i) {
         for (int j = 0; j < ins; ++j)
-            if (meet(out[i], in[j])) return fail(ctx, RCD_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
+            if (areas_meet(out[i], in[j])) return fail(ctx, RCD_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
         for (int j = 0; j < i; ++j)
-            if (meet(out[i], out[j])) return fail(ctx, RCD_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
+            if (areas_meet(out[i], out[j])) return fail(ctx, RCD_ERR_INVALID_ARG, "an output or the workspace overlaps another argument");
     }
     return RCD_OK;
 }

@@ -119,6 +119,7 @@ inline void begin_operator(rcd_ctx *ctx)
 
 // Checks of arguments.  An area: a rectangle of memory that a call reads or writes.
 struct Area { const void *p; int64_t rows, ld, len, bytes; };
+bool areas_meet(const Area &a, const Area &b);
 rcd_status check_apart(rcd_ctx *ctx, const Area *out, int outs, const Area *in, int ins);
 rcd_status check_sizes(rcd_ctx *ctx, int64_t rows, int64_t n, int64_t k);
 rcd_status check_floats(rcd_ctx *ctx, const char *name, const float *p);

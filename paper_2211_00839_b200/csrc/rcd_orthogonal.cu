@@ -294,14 +294,20 @@ extern "C" rcd_status rcd_orthogonalize(rcd_ctx *ctx, const rcd_orthogonalize_ar
     if (a.batch == 0 || a.rows == 0 || a.cols == 0) return RCD_OK;
     RCD_TRY(check_workspace(ctx, workspace_dev, workspace_bytes, need));
     const int64_t eb = elem_bytes(a.type);
-    // (of a batch the bytes from the first matrix to the last; of one its rows)
-    auto area = [&](const void *p, int64_t ld, int64_t step, int64_t bytes) {
-        const int64_t all = (a.batch - 1) * step + (a.rows - 1) * ld + a.cols;
-        return a.batch > 1 ? Area{p, 1, all, all, bytes} : Area{p, a.rows, ld, a.cols, bytes};
+    // (two views of a batch: its matrices, one for each step; and, where they lie whole rows apart, its rows and those between them.  Either may show that nothing is shared.)
+    auto matrices = [&](const void *p, int64_t ld, int64_t step, int64_t bytes) { return Area{p, a.batch, step, (a.rows - 1) * ld + a.cols, bytes}; };
+    auto rows = [&](const void *p, int64_t ld, int64_t step, int64_t bytes) {
+        if (a.batch > 1 && step % ld) return matrices(p, ld, step, bytes);
+        return Area{p, (a.batch > 1 ? (a.batch - 1) * (step / ld) : 0) + a.rows, ld, a.cols, bytes};
     };
-    const Area out[] = {area(a.o_dev, a.ld_o, a.step_o, 2), {need ? workspace_dev : nullptr, 1, (int64_t)need, (int64_t)need, 1}};
-    const Area in[] = {area(a.g_dev, a.ld_g, a.step_g, eb)};
-    RCD_TRY(check_apart(ctx, out, 2, in, 1));
+    const Area o = matrices(a.o_dev, a.ld_o, a.step_o, 2), g0 = matrices(a.g_dev, a.ld_g, a.step_g, eb);
+    const Area out[] = {{need ? workspace_dev : nullptr, 1, (int64_t)need, (int64_t)need, 1}};
+    const Area in[] = {o, g0};
+    RCD_TRY(check_apart(ctx, out, 1, in, 2));
+    if (areas_meet(o, g0)) {
+        const Area outRows[] = {rows(a.o_dev, a.ld_o, a.step_o, 2)}, inRows[] = {rows(a.g_dev, a.ld_g, a.step_g, eb)};
+        RCD_TRY(check_apart(ctx, outRows, 1, inRows, 1));
+    }
     cudaStream_t st = (cudaStream_t)cuda_stream;
     RCD_CUDA(ctx, cudaSetDevice(ctx->device));
     if (const int cluster = cluster_for(ctx, a.rows, a.cols)) return launch_cluster(ctx, a, cluster, st);
