@@ -500,10 +500,11 @@ RCD_API rcd_status rcd_linear_cross_entropy(rcd_ctx *ctx, const rcd_cross_entrop
  * dloss counts as 0 where the label is negative (or n or more: RCD_ERR_INVALID_ARG from rcd_sync_status); p is 0 where lse is -infinity, and dz where dloss
  * and dlse are 0.  (x of such rows has to be finite all the same: dw multiplies it by 0.)  dz is rounded to `type` for the products, as a
  * tensor-core operand has to be (fp16: times a power of two by the largest finite |dloss| + |dlse|, so that 2^-38 of that is still held); dbias takes it unrounded.
- * The logits' sums run over up to 4096 k in the tensor cores, which loses less than dz's rounding; where dbias is wanted over 128 k, so that dx and dw may round another way then.
- * dbias adds up rows that nearly cancel, and what a logit has lost has the same sign in every row.  Measured at normal values with logits up to 8 or so, as a part of dbias's norm: 1e-6
- * from 1000 classes on (as fp32 products), up to 6e-6 from 10 to 500 and 8e-6 for two, as far as the given lse is right; with the lse of rcd_linear_cross_entropy, whose sums
- * run over 512 k and which is some 2e-6 low, up to 4e-6, 2e-5 and 4e-5 off the loss's own gradient.  It grows with the logits.
+ * The logits' sums run over up to 4096 k in the tensor cores, which loses less than dz's rounding; where dbias is wanted over 128 or 512 k, so that dx and dw may round another way then.
+ * dbias adds up rows that nearly cancel, and what a logit has lost has the same sign in every row.  Up to 256 classes (in one piece) p is divided by its sum where that is one but for such
+ * losses (within 2^-18 |lse| + 2^-16): dbias is within 1e-6 of its norm then.  With more it is within 1e-6 (from 1000 classes on) or 2e-6, as fp32 products or twice that, as far as the
+ * given lse is right; that of rcd_linear_cross_entropy, whose sums run over 512 k, is some 2e-6 low and leaves it up to 5e-6 off the loss's own gradient.  (Measured at normal
+ * values with logits up to 8 or so; it grows with them.)
  * Workspace: dz of a piece, and where there are several dx in fp32. */
 typedef struct {
     int64_t rows, n, k;

@@ -10,8 +10,10 @@
 
 namespace rcd {
 
-KernelChoice head_kernel(Form form, int wide, bool pair)
+KernelChoice head_kernel(Form form, bool oneTile, int wide, bool pair)
 {
+    constexpr int oneBit = kPlainKernels + kHeadKernels + kScaledKernels + kScaledLowKernels;
+    if (oneTile) return wide ? product_choice<kOneTile, false, false, false, 64>(pair, oneBit) : product_choice<kOneTile, false, false, false, 0>(pair, oneBit + 2);
     if (form == kLoss) return wide ? product_choice<kLoss, false, false, false, 32>(pair, kPlainKernels + 2) : product_choice<kLoss, false, false, false, 0>(pair, kPlainKernels);
     return wide ? product_choice<kLogitGrads, false, false, false, 64>(pair, kPlainKernels + 6) : product_choice<kLogitGrads, false, false, false, 0>(pair, kPlainKernels + 4);
 }
@@ -186,6 +188,9 @@ int64_t piece_of(const rcd_cross_entropy_back_args &a)
     return piece >= a.n ? a.n : std::max<int64_t>(piece / 64 * 64, 64);      // (dz's rows of whole 128 bytes)
 }
 
+// Classes that a tile may have all of.  (dx and dw are far from showing what is gained.)
+constexpr int kMostOneTile = 256;
+
 // Where the parts of a backward pass's workspace lie, and the products of the piece of classes from `first` on.
 struct BackPlan {
     int64_t piece, pieces, ldDz, ldSum;
@@ -223,6 +228,7 @@ BackPlan back_plan(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a, unsigned 
     const void *x = b.packX ? ws + b.x : a.x_dev, *w = b.packW ? ws + b.w : (const unsigned char *)a.w_dev + first * a.ldw * eb;
     const int64_t ldx = b.packX ? b.ldPacked : a.ldx, ldw = b.packW ? b.ldPacked : a.ldw;
     b.z = logits(a.rows, n, a.k, a.type, x, ldx, w, ldw, a.bias_dev_or_null ? a.bias_dev_or_null + first : nullptr, kLogitGrads);
+    b.z.oneTile = a.dbias_dev_or_null && a.n <= kMostOneTile && b.pieces == 1;
     b.z.out.y = ws + b.dz;
     b.z.out.ldy = b.ldDz;
     b.z.head.labels = a.labels_dev;

@@ -10,10 +10,10 @@ namespace rcd {
 #define RCD_TRY(call) do { const rcd_status rs__ = (call); if (rs__ != RCD_OK) return rs__; } while (0)
 
 // How a product ends.  kPlain: rcd_linear's epilogue, or partial sums as they are.  kLoss: every row's logits of a tile to a
-// reference and a sum of exponentials; nothing else leaves the SM.  kLogitGrads: logits to their gradients.  kScaled: alpha times the product
+// reference and a sum of exponentials; nothing else leaves the SM.  kLogitGrads: logits to their gradients (kOneTile: where a tile has all classes, Product::oneTile).  kScaled: alpha times the product
 // plus beta times the residual, symmetric ones from their lower half; a batch of matrices.  kScaledLow: the same (Product says kScaled) where the residual has a second part: a kernel
 // of its own, since those instructions in all of kScaled's cost every product 0.5 us (8 updates of 1024 x 2048 454 -> 467 us).
-enum Form { kPlain, kLoss, kLogitGrads, kScaled, kScaledLow };
+enum Form { kPlain, kLoss, kLogitGrads, kScaled, kScaledLow, kOneTile };
 
 // What is done with an accumulator on its way out: z = acc [* xs[m] * ws[n]] + bias[n], y = act(z) + residual.
 struct Epilogue {
@@ -57,14 +57,15 @@ struct Product {
     Form form;                             // kPlain where nothing is said
     Head head;
     Scaling scaling;
+    bool oneTile;                          // kLogitGrads: the N columns are all classes and go into one tile
     bool symmetric;                        // kScaled: the output is, and M is N; both halves of it are written
     int64_t batch;                         // kScaled: matrices (0: one), whose rows lie below one another, in every argument this many apart:
     int64_t aStep, bStep, yStep, rStep;
 };
 struct KernelChoice { const void *kernel; int bit; };          // bit: of rcd_ctx::productReady
-KernelChoice head_kernel(Form form, int wide, bool pair);
+KernelChoice head_kernel(Form form, bool oneTile, int wide, bool pair);
 KernelChoice scaled_kernel(int order, int wide, bool pair, bool low);
-constexpr int kPlainKernels = 20, kHeadKernels = 8, kScaledKernels = 18;       // (and 8 with a second part of the residual)
+constexpr int kPlainKernels = 20, kHeadKernels = 8, kScaledKernels = 18, kScaledLowKernels = 8;    // (and 4 of kOneTile)
 
 size_t product_workspace(rcd_ctx *ctx, const Product &p);
 int64_t product_tile_columns(rcd_ctx *ctx, const Product &p);          // kLoss: of what parts holds

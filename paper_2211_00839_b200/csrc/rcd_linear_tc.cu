@@ -152,6 +152,7 @@ Plan make_plan(const rcd_ctx *ctx, const Product &p, bool packA, bool packB)
         for (int tn = 64; tn <= 256; tn += p.form == kLoss && !pair ? 32 : 64) {       // (rounds of 64 columns where whole pieces of 16-bit output are stored)
             if (pair && p.b.across && tn % 128 != 0) continue;         // (boxes of 64 columns per CTA)
             if (pair && ctx->smCount < 2) continue;
+            if (p.oneTile && tn < p.N) continue;
             const int64_t tilesM = (p.M + (pair ? 256 : 128) - 1) / (pair ? 256 : 128), tilesN = (p.N + tn - 1) / tn;
             const int64_t slots = pair ? ctx->smCount / 2 : ctx->smCount;
             int64_t tiles = tilesM * tilesN;
@@ -217,7 +218,7 @@ const Plan &plan_product(rcd_ctx *ctx, const Product &p)
     PlanCache &c = *reinterpret_cast<PlanCache *>(ctx->productPlans);      // (zeros at first: how 0 is nobody's)
     const int64_t eb = elem_bytes(p.type);
     const bool packA = !rows_mappable(p.a.p, p.a.ld, eb), packB = !rows_mappable(p.b.p, p.b.ld, eb);
-    const int how = 1 | (int)p.type << 1 | (int)p.a.across << 3 | (int)p.b.across << 4 | (int)packA << 5 | (int)packB << 6 | (int)p.form << 7 | (int)p.symmetric << 9;
+    const int how = 1 | (int)p.type << 1 | (int)p.a.across << 3 | (int)p.b.across << 4 | (int)packA << 5 | (int)packB << 6 | (int)p.form << 7 | (int)p.symmetric << 9 | (int)p.oneTile << 10;
     for (const PlanCache::Entry &e : c.of)
         if (e.how == how && e.M == p.M && e.N == p.N && e.K == p.K && e.ldA == p.a.ld && e.ldB == p.b.ld && e.batch == p.batch) return e.plan;
     PlanCache::Entry &e = c.of[c.next++ % 16];
@@ -336,15 +337,15 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     q.slabs = (int32_t)plan.slabs;
     q.slabsPerSplit = plan.slabsPerSplit;
     q.tn = plan.tn;
-    const int chunk = p.head.sums ? kChunkSlabsSums : p.out.type == RCD_ELEM_F32 ? kChunkSlabs : kChunkSlabs16;
-    const bool chunks = !i8 && plan.slabsPerSplit > (p.head.sums || p.out.type == RCD_ELEM_F32 ? chunk : 2 * chunk);
+    const int chunk = p.oneTile || p.out.type == RCD_ELEM_F32 ? kChunkSlabs : p.head.sums ? kChunkSlabsSums : kChunkSlabs16;
+    const bool chunks = !i8 && plan.slabsPerSplit > (chunk == kChunkSlabs16 ? 2 * chunk : chunk);
     q.chunk = chunks ? chunk : q.slabs;
     q.aRows = aRows;
     q.e = p.out;
     q.raw = plan.splits > 1;
     // What the ring leaves room for.  A second place per warp hides a store's way out behind the next piece, which does not matter where a tile's slabs take longer than
     // its end; with one, and without columns, 256 x 256 tiles have a ring of six stages for four.
-    q.columnBytes = !q.raw && (q.e.bias || (i8 && q.e.ws)) ? kColumnBytes : 0;
+    q.columnBytes = !q.raw && (q.e.bias || (i8 && q.e.ws) || p.oneTile) ? kColumnBytes : 0;
     q.places = !q.raw && (q.e.z || p.symmetric || p.head.sums) ? 2 : plan.slabsPerSplit >= kOnePlaceFrom ? 1 : 2;
     q.stagingBytes = p.form == kLoss ? kJoinStaging : kEpiWarps * q.places * kPiece;
     const OperandRing ring = ring_of(q.aRows, plan.pair ? plan.tn / 2 : plan.tn, q.stagingBytes + q.columnBytes + kFixedShared);
@@ -381,7 +382,7 @@ rcd_status launch_product(rcd_ctx *ctx, const Product &p, void *workspace, cudaS
     const int order = !p.a.across && !p.b.across ? 0 : !p.a.across ? 1 : 2;
     if (p.a.across && !p.b.across) return fail(ctx, RCD_ERR_INTERNAL, "no product takes these orders");
     const int wide = !chunks ? 0 : q.e.type == RCD_ELEM_F32 ? 32 : 64;
-    const KernelChoice c = p.form == kPlain ? plain_kernel(i8, order, wide, plan.pair) : p.form == kScaled ? scaled_kernel(order, wide, plan.pair, p.scaling.low && !q.raw) : head_kernel(p.form, wide, plan.pair);
+    const KernelChoice c = p.form == kPlain ? plain_kernel(i8, order, wide, plan.pair) : p.form == kScaled ? scaled_kernel(order, wide, plan.pair, p.scaling.low && !q.raw) : head_kernel(p.form, p.oneTile, wide, plan.pair);
     const rcd_status rs = run_product(ctx, c, grid, smem, maps, q, st);
     if (rs != RCD_OK || !q.raw) return rs;
     const Scaling scaling = p.form == kScaled ? p.scaling : Scaling{1.0f, 1.0f, nullptr, 0, 0, p.out.type, nullptr};

@@ -34,10 +34,10 @@ constexpr int kEpiWarps = 8;
 // rows: 3.56 ms in chunks, 3.45 in one sum.)
 // Logits whose gradients are summed over the rows in fp32 (a head's dbias, where p and the labels nearly cancel, and what all rows' z have lost adds up): 128 k, which from some 1000
 // classes on is as exact as fp32 products.  Of 5000 x 2048 over 1000 classes dbias is 1.5e-5 off in one sum, 3.3e-6 in chunks of 512, 1.6e-6 of 256, 7.8e-7 of 128, 4.3e-7 of 64 (fp32
-// products 8.4e-7); the call takes 89, 98, 102, 106 and 119 us.  What is left comes from the chunks: with exp to the last bit it is the same.  Fewer classes have larger p, which
-// lose the same way in every row: 12 237 x 1914 over 97 classes 2.2e-6 in chunks of 128 and 1.3e-6 of 64 (0.7e-6), 20 000 x 2048 over ten 4.5e-6 and 2.5e-6 (0.7e-6; 117 and 128 us).
-// The loss adds up 512 k; its lse is 2e-6 low, and dbias from it off by 2.7e-6 and 1.5e-5 of the true one on 1000 and 10 classes.  With chunks of 128 in the loss, too, those would be 2e-7,
-// but 8192 x 4096 over 32 768 classes would take 2.15 ms for 1.46, 5000 x 2048 over 1000 40 us for 30.
+// products 8.4e-7); the call takes 89, 98, 102, 106 and 119 us.  What is left comes from the chunks: with exp to the last bit it is the same.  The loss adds up 512 k; its lse is 2e-6 low,
+// and dbias from it 2.7e-6 off the loss's own gradient.  (With chunks of 128 in the loss, too, 2e-7; but 5000 x 2048 over 1000 classes would take 40 us for 30 there, and 8192 x 4096 over
+// 32 768 2.15 ms for 1.46.)  Fewer classes have larger p, which lose more: 20 000 x 2048 over ten in chunks of 128 4.5e-6 off, and 1.5e-5 with the loss's lse.  Where one tile has them
+// all (kOneTile) the logits are the loss's, in chunks of 512, and p is brought to a sum of one: 5.2e-7 and 5.4e-7 (111 us for 117).
 constexpr int kChunkSlabs = 8, kChunkSlabs16 = 32, kChunkSlabsSums = 2;
 constexpr int kFirstEpiWarp = 4;                        // (a warpgroup for the two that issue: registers are handed over by warpgroups)
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
@@ -53,7 +53,7 @@ struct __align__(8) ProductShared {
     uint64_t full[kMostStages], empty[kMostStages];     // full: CTA 0's of a pair
     uint64_t accFull[2], accEmpty[2];                   // accEmpty: CTA 0's of a pair
     uint64_t residual[kEpiWarps][2];
-    uint64_t handed[4][2];                              // kLoss: the quarter's second warp has left its half of a tile, two tiles in turn
+    uint64_t handed[4][2];                              // kLoss: the quarter's second warp has left its half of a tile, two tiles in turn; kOneTile: both have
     uint32_t tmemBase;
     int32_t abort;
 };
@@ -294,7 +294,7 @@ __device__ __forceinline__ float column_sum(const float (&v)[32], float *place)
 template <Form kForm, bool kInt8, bool kAcrossA, bool kAcrossB, int kChunks, bool kPair>
 __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUtensorMap &mapB, const CUtensorMap &mapY, const CUtensorMap &mapZ, const CUtensorMap &mapR, const TcParams &p)
 {
-    constexpr bool kIsScaled = kForm == kScaled || kForm == kScaledLow;
+    constexpr bool kIsScaled = kForm == kScaled || kForm == kScaledLow, kIsGrads = kForm == kLogitGrads || kForm == kOneTile;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char *const tiles = smem;
     unsigned char *const staging = smem + (size_t)p.stages * p.stageBytes;
@@ -312,7 +312,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
         for (int s = 0; s < kMostStages; ++s) { mbar_init(&sh.full[s], 1); mbar_init(&sh.empty[s], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&sh.accFull[b], 1); mbar_init(&sh.accEmpty[b], (kPair ? 2 : 1) * kEpiWarps); }
         for (int w = 0; w < kEpiWarps; ++w) { mbar_init(&sh.residual[w][0], 1); mbar_init(&sh.residual[w][1], 1); }
-        for (int w = 0; w < 4; ++w) { mbar_init(&sh.handed[w][0], 1); mbar_init(&sh.handed[w][1], 1); }
+        for (int w = 0; w < 4; ++w) { mbar_init(&sh.handed[w][0], kForm == kOneTile ? 2 : 1); mbar_init(&sh.handed[w][1], kForm == kOneTile ? 2 : 1); }
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -460,7 +460,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             }
         };
         const bool mirrors = kIsScaled && p.walk.subM != 0;
-        const bool sums = kForm == kLogitGrads && p.head.sums != nullptr;
+        const bool sums = kIsGrads && p.head.sums != nullptr;
         const bool alternate = p.places == 2 && e.z == nullptr && !mirrors && !sums;      // two places in turn, or one for y and one for z, the transpose or sums; or only the one
         uint32_t nt = 0, turn = 0;
         [[maybe_unused]] uint32_t tile = 0;
@@ -518,8 +518,8 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 if constexpr (kInt8) {
                     if (e.xs) r.sx = e.xs[row];
                 }
-                if constexpr (kForm == kLoss || kForm == kLogitGrads) r.label = p.head.labels[row];
-                if constexpr (kForm == kLogitGrads) {
+                if constexpr (kForm == kLoss || kIsGrads) r.label = p.head.labels[row];
+                if constexpr (kIsGrads) {
                     r.lse = p.head.lse[row];
                     r.dloss = p.head.dloss ? p.head.dloss[row] : 1.0f;
                     if (p.head.dlse) r.dlse = p.head.dlse[row];
@@ -534,14 +534,14 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             float alpha, beta;                                         // kScaled
             bool mirror;
         };
-        [[maybe_unused]] const float up = kForm == kLogitGrads && p.head.up ? *p.head.up : 1.0f;
+        [[maybe_unused]] const float up = kIsGrads && p.head.up ? *p.head.up : 1.0f;
         auto row_of = [&](const Unit &t, const Asked &asked) {
             Row r{};
             r.sx = asked.sx;
-            if constexpr (kForm == kLoss || kForm == kLogitGrads) {
+            if constexpr (kForm == kLoss || kIsGrads) {
                 const bool valid = asked.label >= 0 && asked.label < p.head.classes;
                 r.label = valid ? asked.label - p.head.firstClass : -1;          // (another piece's: outside 0..N-1)
-                if constexpr (kForm == kLogitGrads) {
+                if constexpr (kIsGrads) {
                     if (asked.label >= p.head.classes && t.n == 0) atomicOr(p.status, kDevBadLabel);
                     const float g = valid ? asked.dloss : 0.0f;
                     r.lse = asked.lse == -INFINITY ? INFINITY : asked.lse;         // (a row without a class that is open: p is 0)
@@ -558,6 +558,23 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 r.mirror = t.mirror;
             }
             return r;
+        };
+        // kLogitGrads: the logits of 32 columns to exp(z - lse)
+        [[maybe_unused]] auto exponentials = [&](float (&z)[32], float lse, int c) {
+            if (e.bias) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 b = reinterpret_cast<const float4 *>(biases + c * 32)[j / 4];
+                    z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
+                }
+            }
+            const Two less = two(-lse, -lse), log2e = two(kLog2e, kLog2e);
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+                const float2 a = parts(mul2(add2(two(z[j], z[j + 1]), less), log2e));
+                z[j] = exp2_fast(a.x);
+                z[j + 1] = exp2_fast(a.y);
+            }
         };
         // 32 columns of the lane's row, from column h of the piece on, the warp's c-th
         auto finish = [&](float (&z)[32], const Row &r, int h, int c, const Piece &o) {
@@ -590,19 +607,12 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                         *reinterpret_cast<uint16_t *>(zPiece + (h + j + 1) * 64 + lane * 2) = (uint16_t)(two >> 16);
                     }
                 }
-            } else if constexpr (kForm == kLogitGrads) {
-                if (e.bias) {
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        const float4 b = reinterpret_cast<const float4 *>(biases + c * 32)[j / 4];
-                        z[j] += b.x; z[j + 1] += b.y; z[j + 2] += b.z; z[j + 3] += b.w;
-                    }
-                }
-                const Two less = two(-r.lse, -r.lse), log2e = two(kLog2e, kLog2e), weight = two(r.weight, r.weight);
+            } else if constexpr (kIsGrads) {
+                exponentials(z, r.lse, c);
+                const Two weight = two(r.weight, r.weight);
 #pragma unroll
                 for (int j = 0; j < 32; j += 2) {
-                    const float2 a = parts(mul2(add2(two(z[j], z[j + 1]), less), log2e));
-                    const float2 dz = parts(mul2(two(exp2_fast(a.x), exp2_fast(a.y)), weight));
+                    const float2 dz = parts(mul2(two(z[j], z[j + 1]), weight));
                     z[j] = dz.x;
                     z[j + 1] = dz.y;
                 }
@@ -641,7 +651,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
                 if (e.residual) add_row(yPiece, lane, h / 8, z, e.type, 1.0f);
             }
             put_row(yPiece, lane, h / 8, z, e.type);
-            if constexpr (kForm == kLogitGrads) {
+            if constexpr (kIsGrads) {
                 if (p.head.sums) {
                     const float sum = column_sum(z, reinterpret_cast<float *>(zPiece)), down = 1.0f / up;           // (powers of two)
                     if (o.col + h + lane < p.N) p.head.sums[(int64_t)(o.row / 32) * p.N + o.col + h + lane] = sum * down;
@@ -694,7 +704,7 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             const int row = t.m * rowsPerTile + rank * kRows + q * 32 + lane;
             const uint32_t lanes = (uint32_t)(q * 32) << 16;
             ask_columns(t);
-            const Row mineRow = row_of(t, asked);
+            Row mineRow = row_of(t, asked);
             [[maybe_unused]] SumOfExp terms = no_terms();
             [[maybe_unused]] float picked = 0.0f;
             [[maybe_unused]] bool found = false;
@@ -758,6 +768,38 @@ __device__ __forceinline__ void product_body(const CUtensorMap &mapA, const CUte
             }
             have_columns();
             if (u + step < p.units) askedNext = ask_row(next);
+            if constexpr (kForm == kOneTile) {
+                // All classes are here, so p's sum is known: where it is one but for what the sums of other logits than lse's have lost, p is divided by it, and what is left in dbias is
+                // what the classes have lost unlike one another.  Both warps of a quarter leave their half's sum and read the other's; the places are free again two tiles later,
+                // since a warp is a tile ahead at most.
+                float mass = 0.0f;
+                for (int k = half; k < pieces; k += 2) {
+                    Piece o;
+                    if (!piece_of(t, k, &o)) continue;
+                    for (int h = 0; h < wide; h += 32) {
+                        uint32_t v[32];
+                        tmem_load_32cols(tmemBase + buf * 256 + lanes + (uint32_t)(k * wide + h), v);
+                        tmem_load_wait();
+                        float z[32], some[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(v[j]);
+                        exponentials(z, mineRow.lse, wide == 64 ? (k - half) + h / 32 : (k - half) / 2);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) some[j & 3] += o.col + h + j < p.N ? z[j] : 0.0f;
+                        mass += (some[0] + some[1]) + (some[2] + some[3]);
+                    }
+                }
+                const int at = 128 + (int)(tile & 1) * 32 + lane;      // (of the warp's columns, behind the biases)
+                columns[ew * 256 + at] = mass;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.handed[q][tile & 1]);
+                if (!warp_wait_for(&sh.handed[q][tile & 1], (tile >> 1) & 1, &sh)) { ok = false; break; }
+                mass += columns[(ew ^ 4) * 256 + at];
+                ++tile;
+                // (from what lse's rounding and the exponentials explain up to 2^-18 of a logit and 2^-16, far above what a sum has lost; an lse of more classes than these is left alone)
+                const float far = fabsf(mass - 1.0f), size = fabsf(mineRow.lse);
+                if (far > fmaf(size, 0x1p-24f, 0x1p-21f) && far <= fminf(fmaf(size, 0x1p-18f, 0x1p-16f), 0x1p-10f)) mineRow.weight /= mass;
+            }
             for (int k = half; k < pieces; k += 2) {
                 Piece o;
                 if (!piece_of(t, k, &o)) continue;

@@ -1,7 +1,7 @@
 """What the sums of the logits lose, where it shows: a head's dbias, whose rows nearly cancel, on real values.
 
 Errors are parts of the norm.  Against the lse that the call is given: as good as fp32 products within a factor of two from 1000 classes on (sums of 128 k;
-in sums of 512 k it would be four times as much), and what the header states for fewer.  Against the loss itself the forward call's lse adds its own."""
+in sums of 512 k it would be four times as much).  Against the loss itself the forward call's lse adds its own, but for up to 256 classes, where p's sum is known."""
 import pytest
 
 from test_gpu_norm import ctx, half_step, kind, rcd, seeded  # noqa: F401  (fixtures)
@@ -31,10 +31,11 @@ def off(got, want):
     return float((got.double() - want).norm() / want.norm())
 
 
-# rows, k, classes, type; dbias from the given lse and from the call's own: what the header states, and a quarter more (a half for two classes: 300 rows)
-CASES = [(5000, 2048, 1000, "bf16", 1e-6, 5e-6), (1300, 1001, 5003, "fp16", 1e-6, 5e-6), (32, 512, 1000, "bf16", 1e-6, 5e-6), (50000, 1024, 1000, "bf16", 1e-6, 5e-6),
-         (20000, 1024, 500, "bf16", 8e-6, 2.5e-5), (12237, 1914, 97, "fp16", 8e-6, 2.5e-5), (50000, 512, 10, "bf16", 8e-6, 2.5e-5), (20000, 2048, 10, "fp16", 8e-6, 2.5e-5),
-         (300, 512, 2, "bf16", 1.2e-5, 5e-5)]
+# rows, k, classes, type; dbias from the right lse and from the call's own: what the header states and a quarter more
+CASES = [(5000, 2048, 1000, "bf16", 1.25e-6, 5e-6), (1300, 1001, 5003, "fp16", 1.25e-6, 5e-6), (32, 512, 1000, "bf16", 1.25e-6, 5e-6), (50000, 1024, 1000, "bf16", 1.25e-6, 5e-6),
+         (20000, 1024, 500, "bf16", 2.5e-6, 6e-6), (12237, 1914, 257, "fp16", 2.5e-6, 6e-6),
+         (12237, 1914, 256, "fp16", 1.25e-6, 1.25e-6), (12237, 1914, 97, "fp16", 1.25e-6, 1.25e-6), (20000, 4096, 128, "bf16", 1.25e-6, 1.25e-6), (50000, 512, 10, "bf16", 1.25e-6, 1.25e-6),
+         (20000, 2048, 10, "fp16", 1.25e-6, 1.25e-6), (300, 512, 2, "bf16", 1.25e-6, 1.25e-6), (3000, 8192, 30, "bf16", 1.25e-6, 1.25e-6), (40, 700, 200, "fp16", 1.25e-6, 1.25e-6)]
 
 
 @pytest.mark.parametrize("m,k,n,dtype,given,own", CASES)
@@ -53,6 +54,25 @@ def test_dbias(rcd, ctx, m, k, n, dtype, given, own):
     _, mine = ctx.rcd_linear_cross_entropy(x, w, y, bias=b)
     _, _, db = ctx.rcd_linear_cross_entropy_backward(x, w, y, mine, bias=b, dloss=dloss)
     assert off(db, dbias_of(z, lse, y, dloss.double())) <= own
+    ctx.sync_status()
+
+
+@pytest.mark.parametrize("m,k,n,dtype", [(700, 512, 10, "bf16"), (5000, 1024, 100, "fp16"), (40, 64, 250, "bf16"), (300, 200, 1, "bf16")])
+@pytest.mark.parametrize("more", [2.0 ** -7, 0.25, 3.0, -0.5])
+@pytest.mark.parametrize("bias", [True, False])
+def test_lse_of_more_classes_than_these(rcd, ctx, m, k, n, dtype, more, bias):
+    """An lse that takes in classes elsewhere (or any other): p stays exp(z - lse), whose sum is not one."""
+    import torch
+    x, w, y, b, dloss = trained(seeded("more", m, n, dtype), m, k, n, kind(dtype))
+    b = b if bias else None
+    z = x.double() @ w.double().t() + (0 if b is None else b.double())
+    lse = (torch.logsumexp(z, 1) + more).float()
+    _, _, db = ctx.rcd_linear_cross_entropy_backward(x, w, y, lse, bias=b, dloss=dloss)
+    want = dbias_of(z, lse.double(), y, dloss.double())
+    # (p as a whole is far from one, nothing cancels: 2e-5 of the sums of sizes is far more than sums of up to 1024 k lose, and a twentieth of the least that taking p's sum out would change)
+    p = torch.exp(z - lse.double()[:, None])
+    sizes = (p * dloss.double()[:, None]).sum(0) + torch.zeros(n, device="cuda", dtype=torch.float64).index_add_(0, y.long(), dloss.double())
+    assert float(((db.double() - want).abs() - 2e-5 * sizes).max()) <= 0
     ctx.sync_status()
 
 
