@@ -180,7 +180,8 @@ rcd_status check_back(rcd_ctx *ctx, const rcd_cross_entropy_back_args &a)
     return check_floats(ctx, "dlse", a.dlse_dev_or_null);
 }
 
-// Classes whose dz is in memory at once: 512 MB of it where the caller does not say.  (Fewer and larger pieces: dx's sum goes through memory once a piece.)
+// Classes whose dz is in memory at once: 512 MB of it where the caller does not say.  (Fewer and larger pieces: dx's sum goes through memory once a piece.  8192 x 4096 over 32 768 classes: 4.3 to 5.0 ms in one piece, 5.3
+// in four; over 131 072 19.7 to 20.5 in one, in four and in eight.)
 constexpr int64_t kPieceBytes = 512LL << 20;
 int64_t piece_of(const rcd_cross_entropy_back_args &a)
 {

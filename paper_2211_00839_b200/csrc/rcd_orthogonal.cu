@@ -12,8 +12,8 @@
 // stored both ways.
 //
 // Three forms: a side of at most 128 in a cluster per matrix (rcd_orthogonal_cluster.cu); all steps in one launch (rcd_orthogonal_fused.cu), where the time goes into the
-// steps' waiting for one another; launches of their own with tiles of up to 256 x 256 on pairs of SMs, where it goes into the products (4096 x 4096: 1.16 ms, 1.18 PFLOP/s of
-// what has to be computed, 71 % of cuBLAS's rate in bursts).
+// steps' waiting for one another; launches of their own with tiles of up to 256 x 256 on pairs of SMs, where it goes into the products (4096 x 4096: 1.15 ms, 1.19 PFLOP/s of
+// what has to be computed, 72 % of cuBLAS's rate in bursts).
 #include "rcd_orthogonal.h"
 #include "rcd_product.cuh"
 
@@ -251,8 +251,8 @@ Layout layout_of(rcd_ctx *ctx, const rcd_orthogonalize_args &a)
     l.factor = place((size_t)a.batch * 4);
     l.fused = fused_plan(ctx, a.batch, l.rows, l.cols, l.tall);
     if (l.fused.possible) {
-        // Launches of their own take 4.3 us each besides the products.  (Both measured: 512 x 512 97 us in one launch, 123 in 17; 1024 x 2048 192 and 190; 1536 x 1536
-        // 341 and 214.)
+        // Launches of their own take 4.3 us each besides the products.  (Both measured: 512 x 512 103 us in one launch, 133 in 17; 1024 x 2048 189 and 204; 1536 x 1536
+        // 304 and 228.)
         const Step s = step_of(a, l, nullptr, 0, false);
         double us = 0.0;
         for (const Product *p : {&s.gram, &s.poly, &s.x}) us += 4.3 + product_cycles(ctx, *p) / 1900.0;

@@ -1,4 +1,4 @@
-// The product on the tensor cores that rcd_linear, the loss of a head and the orthogonalised update share:  C = A B^T, finished in one of four
+// The product on the tensor cores that rcd_linear, the loss of a head and the orthogonalised update share:  C = A B^T, finished in one of several
 // forms (see Form).
 //
 // Persistent CTAs (one per SM), or pairs of CTAs on one tile (cta_group::2: each holds half of A's rows and half of B's, so an
