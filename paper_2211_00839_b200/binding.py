@@ -752,7 +752,8 @@ class Context:
         """Gradients of ``rcd_linear_cross_entropy`` from those of loss and lse ([...] float32; None: ones, zeros): (dx [..., k], dw [n, k],
         dbias [n] float32), None where not wanted.  lse: what the forward call returned for the same x, w and bias.
 
-        The logits are made again, ``piece`` classes at a time (0: as many as take 512 MB of workspace).  ``dw_dtype``: default x's type, or float32."""
+        The logits are made again, ``piece`` classes at a time (0: as many as take 512 MB of workspace), and their gradients rounded to x's type for dx and dw,
+        not for dbias; with dbias dx and dw may differ in their last bits.  ``dw_dtype``: default x's type, or float32."""
         torch = _torch()
         f32 = torch.float32
         xk, rows, k, ldx = self._rows(x, "x")
